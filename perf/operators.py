@@ -1,0 +1,425 @@
+"""What a decoder layer does between its vector-quantized products, as cases whose time can be measured.
+
+Around the products (q, k, v, o, gate, up, down) a model that is served from a paged cache of keys and values
+  * rotates the new queries and keys by their positions and appends keys and values to the cache (kv_append),
+  * lets every new token attend to what its sequence holds there (attention): one token of many sequences when decoding, a few
+    drafted ones, or a prompt, the latter also in chunks behind what is there already; all of it, or a window of the last
+    tokens and a few first ones,
+  * adds a block's output to the residual stream and normalises it for the next block (residual_norm).
+The cache is held in 8 bits (e4m3) with one scale for each page and head, keys and values apart, or in 16 bits.  Keys are stored
+[page][head][token][element], values [page][head][element][token].
+
+run() computes these in plain torch operations (own = False), or calls the package (own = True).
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+E4M3_MAX = 448.0
+
+
+# ---- cases ------------------------------------------------------------------------------------------------------------
+def _append(seqs, new, length, q_heads, kv_heads, head_dim, page, bits, interleaved=False, ragged=False):
+    return dict(op="append", seqs=seqs, new=new, length=length, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page=page, bits=bits,
+                interleaved=interleaved, ragged=ragged)
+
+
+def _attend(seqs, new, length, q_heads, kv_heads, head_dim, page, bits, window=0, sinks=0, ragged=False):
+    return dict(op="attention", seqs=seqs, new=new, length=length, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page=page, bits=bits,
+                window=window, sinks=sinks, ragged=ragged)
+
+
+def listed():
+    """7B-shaped layers have 32 heads of 128 elements for queries and for keys, 70B-shaped ones 64 and 8 (`length`: what the
+    longest sequence holds, the new tokens included; `ragged`: the sequences bring different numbers of new tokens)."""
+    return [
+        # One user's decoding step on a 7B-shaped layer: one token, in the middle of a page.  Launch and host time are all of it.
+        dict(name="append, one token", **_append(1, 1, 2041, 32, 32, 128, 16, 8)),
+        # Sixteen users of a 70B-shaped layer, each with a token and four drafted ones, some of which begin a page.
+        dict(name="append, drafted tokens", **_append(16, 5, 2048, 64, 8, 128, 32, 8)),
+        # The prompts of four users of a 7B-shaped layer, of different lengths.
+        dict(name="append, prompts", **_append(4, 1024, 1024, 32, 32, 128, 16, 8, ragged=True)),
+        # One user's decoding step after a short prompt on a 7B-shaped layer: the smallest call.
+        dict(name="decode, one sequence", **_attend(1, 1, 509, 32, 32, 128, 16, 8)),
+        # Sixteen users of a 70B-shaped layer, one token each, contexts up to 4096.
+        dict(name="decode, 16 sequences", **_attend(16, 1, 4096, 64, 8, 128, 16, 8)),
+        # One user with a long document on a 70B-shaped layer.
+        dict(name="decode, long context", **_attend(1, 1, 131071, 64, 8, 128, 64, 8)),
+        # Sixteen long chats of which only the last 1024 tokens and the first four are kept; smaller heads.
+        dict(name="decode, window and sinks", **_attend(16, 1, 8192, 32, 8, 64, 16, 8, window=1024, sinks=4)),
+        # Four users of a 7B-shaped layer whose drafted tokens are checked, four rows each, from a 16-bit cache.
+        dict(name="drafted tokens, 16 bits", **_attend(4, 4, 2047, 32, 32, 128, 16, 16)),
+        # A whole prompt on a 7B-shaped layer.
+        dict(name="prompt, 2048 tokens", **_attend(1, 2048, 2048, 32, 32, 128, 16, 8)),
+        # Chunks of three long prompts of a 70B-shaped layer behind what the cache holds already: the largest call.
+        dict(name="prompt chunks, ragged", **_attend(3, 1024, 16384, 64, 8, 128, 64, 8, ragged=True)),
+        # The residual sum and norm of one decoded token.
+        dict(name="norm, one token", op="norm", rows=1, width=4096, post=False, gate="none", stream=16, scale=1.0),
+        # Norms on both sides of a 70B-shaped block for a prompt, with a gate for each channel and the residual stream in 32 bits.
+        dict(name="norms, 2048 tokens", op="norm", rows=2048, width=8192, post=True, gate="channel", stream=32, scale=0.5),
+    ]
+
+
+def _size(rng, low, high, multiple=1):
+    """A size between low and high, even over its logarithm, rounded to a multiple."""
+    if high <= low:
+        return low
+    return min(high, max(low, int(math.exp(rng.uniform(math.log(low), math.log(high))) / multiple + 0.5) * multiple))
+
+
+HEADS = ((32, 32), (32, 32), (64, 8), (64, 8), (32, 8), (40, 40), (28, 4), (8, 1), (16, 2))
+#: What the largest listed cases cost: a drawn one stays below.
+MOST_BYTES, MOST_FLOPS, MOST_PLAIN = 268e6, 8e11, 3 * 64 * 1024 * 16384
+
+
+def draw(rng):
+    op = rng.choice(("append", "decode", "decode", "draft", "prompt", "prompt", "norm"))
+    if op == "norm":
+        width = rng.choice((64, 512, 1024, 2048, 4096, 5120, 8192, 14336, 16384, rng.randrange(65, 2048), rng.randrange(257, 8192)))
+        return {"op": "norm", "rows": _size(rng, 1, 2048 * 8192 // max(width, 4096)), "width": width, "post": rng.random() < 0.5,
+                "gate": rng.choice(("none", "channel", "token")), "stream": rng.choice((16, 32)), "scale": rng.choice((1.0, 0.5, 0.125))}
+    q_heads, kv_heads = rng.choice(HEADS)
+    head_dim, page, bits = rng.choice((64, 128, 128)), rng.choice((16, 16, 32, 64, 128)), rng.choice((8, 8, 16))
+    if op == "append":
+        seqs = _size(rng, 1, 64)
+        new = rng.choice((1, 1, rng.randrange(2, 9), _size(rng, 9, 2048)))
+        new = min(new, 4096 // seqs)
+        return _append(seqs, new, max(new, _size(rng, new, 8192 // max(1, seqs // 8))), q_heads, kv_heads, head_dim, page, bits,
+                       interleaved=rng.random() < 0.3, ragged=new > 1 and rng.random() < 0.5)
+    window, sinks = rng.choice(((0, 0), (0, 0), (_size(rng, 64, 4096), rng.choice((0, 4, 5)))))
+    if op in ("decode", "draft"):
+        seqs = _size(rng, 1, 64)
+        new = 1 if op == "decode" else rng.randrange(2, 17)
+        token = 2 * kv_heads * head_dim * bits // 8
+        most = min(131072, int(MOST_BYTES / (seqs * token)), MOST_PLAIN // (seqs * q_heads * new))
+        return _attend(seqs, new, _size(rng, new, most), q_heads, kv_heads, head_dim, page, bits, window, sinks, ragged=new > 1 and rng.random() < 0.5)
+    seqs = rng.choice((1, 1, _size(rng, 2, 8)))
+    new = _size(rng, 17, 4096 // seqs)
+    most = min(32768, int(MOST_FLOPS / (4 * head_dim * q_heads * new * seqs)), MOST_PLAIN // (q_heads * new * seqs))
+    length = new if rng.random() < 0.4 or most <= new else _size(rng, new, most)
+    return _attend(seqs, new, length, q_heads, kv_heads, head_dim, page, bits, window, sinks, ragged=seqs > 1)
+
+
+def _lengths(case):
+    """What each sequence holds, and how many of that are new: the first has the case's numbers, the others spread from a quarter
+    of them up, all of them ragged where the case is."""
+    n, new, length = case["seqs"], case["new"], case["length"]
+    part = [(i * 0.6180339887) % 1.0 for i in range(n)]
+    news = [new if not case["ragged"] or i == 0 else max(1, int(new * (1.0 - 0.75 * part[i]))) for i in range(n)]
+    kept = [length - new if i == 0 else int((length - new) * (1.0 - 0.75 * part[i])) for i in range(n)]
+    return [k + m for k, m in zip(kept, news)], news
+
+
+def _visible(case):
+    """Number of (new token, token that it sees) pairs, and of tokens that any new one sees, over the sequences."""
+    pairs = seen = 0
+    for length, new in zip(*_lengths(case)):
+        at = np.arange(length - new, length)
+        if not case["window"]:
+            pairs, seen = pairs + int((at + 1).sum()), seen + length
+            continue
+        first = np.maximum(0, at - case["window"] + 1)
+        pairs += int((at + 1 - first + np.minimum(first, case["sinks"])).sum())
+        seen += int(length - first[0] + min(first[0], case["sinks"]))
+    return pairs, seen
+
+
+# ---- inputs -----------------------------------------------------------------------------------------------------------
+def _pages(case, seed):
+    """The sequences' pages, scattered over the pool as they come and go in a server; -1: given back, as nothing will look at
+    it again (everything that a window has left behind but for the first tokens)."""
+    lengths, news = _lengths(case)
+    page, window, sinks = case["page"], case.get("window", 0), case.get("sinks", 0)
+    per = [-(-n // page) for n in lengths]
+    table = np.full((len(per), max(per)), -1, np.int32)
+    used = []
+    for b, n in enumerate(per):
+        first = max(0, lengths[b] - news[b] - window + 1) // page if window else 0
+        used += [(b, i) for i in range(n) if i >= first or i * page < sinks]
+    pool = len(used) + 3
+    at = np.array(used)
+    table[at[:, 0], at[:, 1]] = np.random.default_rng(seed).permutation(pool)[: len(used)]
+    return lengths, news, pool, table
+
+
+def _power(amax):
+    """The smallest power of two times 448 that is no smaller (32 bits; 2^-64 at least)."""
+    mantissa, exponent = torch.frexp(amax / E4M3_MAX)
+    power = exponent - (mantissa == 0.5).int()
+    return torch.where(amax > 0, torch.ldexp(torch.ones_like(amax), power.clamp(min=-64)), torch.full_like(amax, 2.0 ** -64))
+
+
+def _cache(pool, heads, rows, columns, bits, gain, generator):
+    """Pages of normal values whose channels are of different sizes, as keys' are, and their scales."""
+    x = torch.randn((pool, heads, rows, columns), device="cuda", generator=generator)
+    x *= gain
+    if bits == 16:
+        return x.half(), None
+    scale = _power(x.abs().amax((2, 3)))
+    return (x / scale[:, :, None, None]).to(torch.float8_e4m3fn), scale
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    if case["op"] == "norm":
+        rows, width = case["rows"], case["width"]
+        stream = torch.float16 if case["stream"] == 16 else torch.float32
+        state = {"op": "norm", "scale": case["scale"], "eps": 1e-5}
+        state["x"] = (torch.randn((rows, width), device="cuda", generator=g) * 4).to(stream)
+        state["h"] = torch.randn((rows, width), device="cuda", generator=g).half()
+        weight = lambda: (1 + 0.2 * torch.randn(width, device="cuda", generator=g)).half()  # noqa: E731
+        state["pre"], state["post"] = weight(), weight() if case["post"] else None
+        shape = {"none": None, "channel": (width,), "token": (rows, width)}[case["gate"]]
+        state["gate"] = torch.randn(shape, device="cuda", generator=g).half() if shape else None
+        return state
+    lengths, news, pool, table = _pages(case, seed)
+    heads, d, tokens = case["kv_heads"], case["head_dim"], sum(news)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    k_gain = torch.exp(0.5 * torch.randn((1, heads, 1, d), device="cuda", generator=g))
+    state = {"op": case["op"], "page_table": torch.from_numpy(table).cuda(), "lengths": ints(lengths), "max_new": max(news), "max_length": max(lengths),
+             "starts": ints([0] + list(np.cumsum(news))) if case["ragged"] else None}
+    state["k_pages"], state["k_scales"] = _cache(pool, heads, case["page"], d, case["bits"], k_gain, g)
+    state["v_pages"], state["v_scales"] = _cache(pool, heads, d, case["page"], case["bits"], 1.0, g)
+    state["q"] = torch.randn((tokens, case["q_heads"], d), device="cuda", generator=g).half()
+    if case["op"] == "attention":
+        state.update(window=case["window"], sinks=case["sinks"])
+        return state
+    state["k"] = (torch.randn((tokens, heads, d), device="cuda", generator=g) * k_gain[0, :, 0]).half()
+    state["v"] = torch.randn((tokens, heads, d), device="cuda", generator=g).half()
+    angles = torch.arange(max(lengths), device="cuda", dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, d, 2, device="cuda", dtype=torch.float64) / d)
+    state["cos"], state["sin"], state["interleaved"] = angles.cos().float(), angles.sin().float(), case["interleaved"]
+    return state
+
+
+# ---- one pass ---------------------------------------------------------------------------------------------------------
+def _tokens_of(state):
+    """For every sequence and every number t below the most new tokens: the row of its token t among the new ones, whether there
+    is one, and its place in the sequence; and for every row its sequence and t."""
+    lengths, most = state["lengths"].long(), state["max_new"]
+    n, rows = lengths.numel(), state["q"].shape[0]
+    starts = state["starts"].long() if state["starts"] is not None else torch.arange(n + 1, device="cuda") * most
+    new = starts[1:] - starts[:-1]
+    t = torch.arange(most, device="cuda")
+    row, real = (starts[:-1, None] + t).clamp(max=rows - 1), t < new[:, None]
+    place = (lengths - new)[:, None] + t
+    at = torch.arange(rows, device="cuda")
+    seq = torch.searchsorted(starts, at, right=True) - 1
+    return row, real, place, seq, at - starts[seq], new
+
+
+def _rotated(x, cos, sin, interleaved):
+    x = x.float()
+    c, s = cos[:, None], sin[:, None]
+    if interleaved:
+        a, b = x[..., 0::2], x[..., 1::2]
+        return torch.stack((a * c - b * s, b * c + a * s), -1).flatten(-2)
+    a, b = x.chunk(2, -1)
+    return torch.cat((a * c - b * s, b * c + a * s), -1)
+
+
+def _into_pages(new, pages, scales, page, first, length, starts, table, transposed):
+    """The pages that hold a sequence's new tokens, from the first of them on, as they are with those tokens, written back.  Where a
+    sequence touches fewer pages than others its last one stands in for the rest."""
+    size = pages.shape[3 if transposed else 2]
+    slots = torch.arange((page - 1) // size + 2, device="cuda")
+    block = torch.minimum((first // size)[:, None] + slots, ((length - 1) // size)[:, None])
+    where = table.gather(1, block).long()
+    place = block[..., None] * size + torch.arange(size, device="cuda")
+    is_new = (place >= first[:, None, None]) & (place < length[:, None, None])
+    is_old = place < first[:, None, None]
+    rows = (starts[:, None, None] + place - first[:, None, None]).clamp(0, new.shape[0] - 1)
+    values = new[rows].transpose(2, 3)                                   # [sequence][block][head][token][element]
+    raw = pages.view(torch.uint8) if scales is not None else pages
+    held = raw[where]
+    if transposed:
+        values = values.transpose(3, 4)
+        is_new, is_old = is_new[:, :, None, None, :], is_old[:, :, None, None, :]
+    else:
+        is_new, is_old = is_new[:, :, None, :, None], is_old[:, :, None, :, None]
+    if scales is None:
+        raw[where] = torch.where(is_new, values.to(pages.dtype), held)
+        return
+    before = scales[where]
+    amax = torch.where(is_new, values.abs(), torch.zeros((), device="cuda")).amax((3, 4))
+    scale = torch.where(is_old.flatten(2).any(2)[..., None], torch.maximum(before, _power(amax)), _power(amax))
+    old = held.view(torch.float8_e4m3fn).float() * (before / scale)[..., None, None]
+    code = torch.where(is_new, values / scale[..., None, None], old).to(torch.float8_e4m3fn).view(torch.uint8)
+    raw[where] = torch.where(is_new | is_old, code, held)
+    scales[where] = scale
+
+
+def _plain_append(s):
+    row, real, place, seq, t, new = _tokens_of(s)
+    lengths = s["lengths"].long()
+    first = lengths - new
+    at = first[seq] + t
+    q = _rotated(s["q"], s["cos"][at], s["sin"][at], s["interleaved"]).half()
+    k = _rotated(s["k"], s["cos"][at], s["sin"][at], s["interleaved"])
+    _into_pages(k, s["k_pages"], s["k_scales"], s["max_new"], first, lengths, row[:, 0], s["page_table"], False)
+    _into_pages(s["v"].float(), s["v_pages"], s["v_scales"], s["max_new"], first, lengths, row[:, 0], s["page_table"], True)
+    return q
+
+
+def _plain_attention(s):
+    row, real, place, seq, t, _ = _tokens_of(s)
+    table = s["page_table"].long().clamp(min=0)
+    n, blocks = table.shape
+    heads, size, d = s["k_pages"].shape[1:]
+
+    def held(pages, scales):
+        if scales is None:
+            return pages[table].float()
+        return pages.view(torch.uint8)[table].view(torch.float8_e4m3fn).float() * scales[table][..., None, None]
+    K = held(s["k_pages"], s["k_scales"]).permute(0, 2, 1, 3, 4).reshape(n, heads, blocks * size, d)
+    V = held(s["v_pages"], s["v_scales"]).permute(0, 2, 1, 4, 3).reshape(n, heads, blocks * size, d)
+    most, q_heads = row.shape[1], s["q"].shape[1]
+    group = q_heads // heads
+    Q = s["q"][row].float().reshape(n, most, heads, group, d).permute(0, 2, 3, 1, 4).reshape(n, heads, group * most, d)
+    j = torch.arange(blocks * size, device="cuda")
+    sees = (j <= place[..., None]) & real[..., None]
+    if s["window"]:
+        sees &= (j > place[..., None] - s["window"]) | (j < s["sinks"])
+    score = (Q @ K.transpose(2, 3)).mul_(d ** -0.5).view(n, heads, group, most, -1).masked_fill_(~sees[:, None, None], -math.inf)
+    top = score.amax(-1, keepdim=True)
+    p = score.sub_(torch.where(top > -math.inf, top, torch.zeros((), device="cuda"))).exp_()
+    total = p.sum(-1, keepdim=True)
+    out = (p.view(n, heads, group * most, -1) @ V).view(n, heads, group, most, d) / torch.where(total > 0, total, torch.ones((), device="cuda"))
+    return out.permute(0, 3, 1, 2, 4).reshape(n, most, q_heads, d)[seq, t].half()
+
+
+def _plain_norm(s):
+    normed = lambda x, w: x * torch.rsqrt(x.square().mean(-1, keepdim=True) + s["eps"]) * w.float()  # noqa: E731
+    h = s["h"].float()
+    if s["post"] is not None:
+        h = normed(h, s["post"])
+    if s["gate"] is not None:
+        h = h * s["gate"].float()
+    y = s["x"].float() + s["scale"] * h
+    return y.to(s["x"].dtype), normed(y, s["pre"]).half()
+
+
+def run(state):
+    s = state
+    if own:
+        import paper_2409_17066_amd as vq
+    if s["op"] == "norm":
+        if own:
+            return vq.residual_norm(s["h"], s["x"], pre=s["pre"], post=s["post"], gate=s["gate"], scale=s["scale"], eps=s["eps"])
+        return _plain_norm(s)
+    if s["op"] == "attention":
+        if own:
+            return vq.attention(s["q"], s["k_pages"], s["v_pages"], s["page_table"], s["lengths"], s["k_scales"], s["v_scales"], starts=s["starts"],
+                                window=s["window"], sinks=s["sinks"], max_new=s["max_new"], max_length=s["max_length"])
+        return _plain_attention(s)
+    if own:
+        q = vq.kv_append(s["k"], s["v"], s["k_pages"], s["v_pages"], s["page_table"], s["lengths"], s["k_scales"], s["v_scales"], q=s["q"],
+                         cos=s["cos"], sin=s["sin"], interleaved=s["interleaved"], starts=s["starts"], max_new=s["max_new"])
+    else:
+        q = _plain_append(s)
+    return {"q": q, "k": s["k_pages"], "v": s["v_pages"], "k_scales": s["k_scales"], "v_scales": s["v_scales"]}
+
+
+# ---- the definitions in 64 bits ---------------------------------------------------------------------------------------
+def _exact_scale(values, before):
+    amax = float(values.abs().max())
+    power = 2.0 ** max(-64, math.ceil(math.log2(amax / E4M3_MAX))) if amax else 2.0 ** -64
+    return max(power, before)
+
+
+def _exact_append(case, s):
+    lengths, news = _lengths(case)
+    size, table = case["page"], s["page_table"].cpu().numpy()
+    out = {"q": s["q"].double(), "k": s["k_pages"].double(), "v": s["v_pages"].double(),
+           "k_scales": None if s["k_scales"] is None else s["k_scales"].double(), "v_scales": None if s["v_scales"] is None else s["v_scales"].double()}
+    row = 0
+    for length, new, pages in zip(lengths, news, table):
+        for i in range(new):
+            at = length - new + i
+            c, w = s["cos"][at].double(), s["sin"][at].double()
+            both = {}
+            for name in ("q", "k"):
+                x, y = s[name][row + i].double(), torch.empty(s[name].shape[1:], dtype=torch.float64, device="cuda")
+                first, second = (slice(0, None, 2), slice(1, None, 2)) if s["interleaved"] else (slice(0, x.shape[1] // 2), slice(x.shape[1] // 2, None))
+                y[:, first], y[:, second] = x[:, first] * c - x[:, second] * w, x[:, first] * w + x[:, second] * c
+                both[name] = y
+            out["q"][row + i] = both["q"]
+            page, offset = int(pages[at // size]), at % size
+            # the values, in place; their division by the scale follows page by page
+            out["k"][page, :, offset], out["v"][page, :, :, offset] = both["k"], s["v"][row + i].double()
+        if case["bits"] == 8:
+            for block in range((length - new) // size, (length - 1) // size + 1):
+                page, begin, end = int(pages[block]), max(0, length - new - block * size), min(size, length - block * size)
+                for h in range(case["kv_heads"]):
+                    for name, fresh, old in (("k", out["k"][page, h, begin:end], out["k"][page, h, :begin]),
+                                             ("v", out["v"][page, h, :, begin:end], out["v"][page, h, :, :begin])):
+                        before = float(out[name + "_scales"][page, h])
+                        scale = _exact_scale(fresh, before if begin else 0.0)
+                        fresh /= scale
+                        old *= before / scale
+                        out[name + "_scales"][page, h] = scale
+        row += new
+    return out
+
+
+def _exact_attention(case, s):
+    lengths, news = _lengths(case)
+    size, heads, d, group = case["page"], case["kv_heads"], case["head_dim"], case["q_heads"] // case["kv_heads"]
+    table = s["page_table"].cpu().numpy()
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda")
+    row = 0
+    for length, new, pages in zip(lengths, news, table):
+        at = torch.arange(length, device="cuda")
+        low = max(0, length - new - case["window"] + 1) if case["window"] else 0
+        keys = at[(at >= low) | (at < case["sinks"])]
+        page = torch.from_numpy(np.maximum(pages, 0)).cuda().long()[keys // size]
+        for h in range(heads):
+            k, v = s["k_pages"][:, h].double(), s["v_pages"][:, h].double()
+            if case["bits"] == 8:
+                k, v = k * s["k_scales"][:, h].double()[:, None, None], v * s["v_scales"][:, h].double()[:, None, None]
+            K, V = k[page, keys % size], v[page, :, keys % size]
+            for begin in range(0, new, 256):
+                end = min(new, begin + 256)
+                q = s["q"][row + begin: row + end, h * group:(h + 1) * group].double().reshape(-1, d)
+                here = torch.arange(length - new + begin, length - new + end, device="cuda").repeat_interleave(group)[:, None]
+                sees = keys <= here
+                if case["window"]:
+                    sees &= (keys > here - case["window"]) | (keys < case["sinks"])
+                w = torch.softmax(torch.where(sees, q @ K.T.contiguous() / math.sqrt(d), -math.inf), -1)
+                out[row + begin: row + end, h * group:(h + 1) * group] = (w @ V).view(end - begin, group, d)
+        row += new
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "append":
+        return _exact_append(case, s) if sum(_lengths(case)[1]) * case["kv_heads"] <= 140000 else None
+    if case["op"] == "attention":
+        return _exact_attention(case, s) if 4 * case["head_dim"] * case["q_heads"] * _visible(case)[0] <= 2e12 else None
+    h = s["h"].double()
+    if s["post"] is not None:
+        h = h / torch.sqrt(h.pow(2).sum(1, keepdim=True) / h.shape[1] + s["eps"]) * s["post"].double()
+    y = s["x"].double() + (h if s["gate"] is None else h * s["gate"].double()) * s["scale"]
+    return y, y / torch.sqrt(y.pow(2).sum(1, keepdim=True) / y.shape[1] + s["eps"]) * s["pre"].double()
+
+
+# ---- what a pass cannot do without -------------------------------------------------------------------------------------
+def work(case):
+    if case["op"] == "norm":
+        n, width, stream = case["rows"] * case["width"], case["width"], case["stream"] // 8
+        gate = {"none": 0, "channel": width, "token": n}[case["gate"]]
+        return {"bytes": n * (2 + 2 + 2 * stream) + 2 * (width * (1 + case["post"]) + gate), "flops": n * (5 + 4 * case["post"])}
+    lengths, news = _lengths(case)
+    tokens, heads, q_heads, d, size = sum(news), case["kv_heads"], case["q_heads"], case["head_dim"], case["bits"] // 8
+    fixed = sum(-(-n // case["page"]) for n in lengths) * 4 + 4 * len(lengths)
+    if case["op"] == "append":
+        pages = sum((n - 1) // case["page"] - (n - m) // case["page"] + 1 for n, m in zip(lengths, news))
+        scales = pages * heads * 8 if case["bits"] == 8 else 0
+        return {"bytes": tokens * d * (4 * q_heads + 2 * heads * (2 + size)) + tokens * 4 * d + scales + pages * 4, "flops": tokens * d * 3 * (q_heads + heads)}
+    pairs, seen = _visible(case)
+    if case["bits"] == 8:
+        fixed += -(-seen // case["page"]) * heads * 8
+    return {"bytes": 2 * seen * heads * d * size + 4 * tokens * q_heads * d + fixed, "flops": 4 * d * q_heads * pairs}
