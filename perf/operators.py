@@ -37,29 +37,29 @@ def listed():
     longest sequence holds, the new tokens included; `ragged`: the sequences bring different numbers of new tokens)."""
     return [
         # One user's decoding step on a 7B-shaped layer: one token, in the middle of a page.  Launch and host time are all of it.
-        dict(name="append, one token", **_append(1, 1, 2041, 32, 32, 128, 16, 8)),
+        dict(name="append one token", **_append(1, 1, 2041, 32, 32, 128, 16, 8)),
         # Sixteen users of a 70B-shaped layer, each with a token and four drafted ones, some of which begin a page.
-        dict(name="append, drafted tokens", **_append(16, 5, 2048, 64, 8, 128, 32, 8)),
+        dict(name="append drafted tokens", **_append(16, 5, 2048, 64, 8, 128, 32, 8)),
         # The prompts of four users of a 7B-shaped layer, of different lengths.
-        dict(name="append, prompts", **_append(4, 1024, 1024, 32, 32, 128, 16, 8, ragged=True)),
+        dict(name="append prompts", **_append(4, 1024, 1024, 32, 32, 128, 16, 8, ragged=True)),
         # One user's decoding step after a short prompt on a 7B-shaped layer: the smallest call.
-        dict(name="decode, one sequence", **_attend(1, 1, 509, 32, 32, 128, 16, 8)),
+        dict(name="decode one sequence", **_attend(1, 1, 509, 32, 32, 128, 16, 8)),
         # Sixteen users of a 70B-shaped layer, one token each, contexts up to 4096.
-        dict(name="decode, 16 sequences", **_attend(16, 1, 4096, 64, 8, 128, 16, 8)),
+        dict(name="decode 16 sequences", **_attend(16, 1, 4096, 64, 8, 128, 16, 8)),
         # One user with a long document on a 70B-shaped layer.
-        dict(name="decode, long context", **_attend(1, 1, 131071, 64, 8, 128, 64, 8)),
+        dict(name="decode long context", **_attend(1, 1, 131071, 64, 8, 128, 64, 8)),
         # Sixteen long chats of which only the last 1024 tokens and the first four are kept; smaller heads.
-        dict(name="decode, window and sinks", **_attend(16, 1, 8192, 32, 8, 64, 16, 8, window=1024, sinks=4)),
+        dict(name="decode window and sinks", **_attend(16, 1, 8192, 32, 8, 64, 16, 8, window=1024, sinks=4)),
         # Four users of a 7B-shaped layer whose drafted tokens are checked, four rows each, from a 16-bit cache.
-        dict(name="drafted tokens, 16 bits", **_attend(4, 4, 2047, 32, 32, 128, 16, 16)),
+        dict(name="drafted tokens 16 bits", **_attend(4, 4, 2047, 32, 32, 128, 16, 16)),
         # A whole prompt on a 7B-shaped layer.
-        dict(name="prompt, 2048 tokens", **_attend(1, 2048, 2048, 32, 32, 128, 16, 8)),
+        dict(name="prompt 2048 tokens", **_attend(1, 2048, 2048, 32, 32, 128, 16, 8)),
         # Chunks of three long prompts of a 70B-shaped layer behind what the cache holds already: the largest call.
-        dict(name="prompt chunks, ragged", **_attend(3, 1024, 16384, 64, 8, 128, 64, 8, ragged=True)),
+        dict(name="prompt chunks ragged", **_attend(3, 1024, 16384, 64, 8, 128, 64, 8, ragged=True)),
         # The residual sum and norm of one decoded token.
-        dict(name="norm, one token", op="norm", rows=1, width=4096, post=False, gate="none", stream=16, scale=1.0),
+        dict(name="norm one token", op="norm", rows=1, width=4096, post=False, gate="none", stream=16, scale=1.0),
         # Norms on both sides of a 70B-shaped block for a prompt, with a gate for each channel and the residual stream in 32 bits.
-        dict(name="norms, 2048 tokens", op="norm", rows=2048, width=8192, post=True, gate="channel", stream=32, scale=0.5),
+        dict(name="norms 2048 tokens", op="norm", rows=2048, width=8192, post=True, gate="channel", stream=32, scale=0.5),
     ]
 
 
