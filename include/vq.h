@@ -283,6 +283,91 @@ size_t vq_gemm_default_workspace_bytes(const vq_layer_desc *desc, int32_t tokens
 int vq_gemm_default(const vq_layer_desc *desc, const void *X, int64_t ldx, int32_t tokens,
                     void *Y, int64_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ---- between a decoder layer's products -------------------------------------------------------------------------------
+ * The paper measures its layers inside a decoding model (its section on inference throughput); the three calls below are what such a
+ * model does between the products above: new queries and keys are rotated by their positions and keys and values are
+ * appended to a paged cache, new tokens attend to what their sequence holds there, and a block's output is added to the
+ * residual stream and normalised for the next block.  Conventions (device pointers, streams, errors, no allocation) as above.
+ *
+ * Paged cache.  The cache is a pool of n_pages pages of page_tokens tokens; place p of sequence b is token p % page_tokens of page
+ * page_table[b][p / page_tokens].  Element i of head h of a page's token t is k_pages[page * k_page_stride + (h * page_tokens + t) *
+ * head_dim + i] for keys and v_pages[page * v_page_stride + (h * head_dim + i) * page_tokens + t] for values, whose tokens thus lie next to each
+ * other (what the matrix cores want of the second product of attention).  type VQ_KV_FP16: binary16.
+ * VQ_KV_E4M3: 8-bit e4m3 codes (no infinities; 0x7f and 0xff are NaN) times k_scales / v_scales[page][head], binary32 powers of two.
+ * New tokens.  Sequence b brings new_b = starts[b + 1] - starts[b] of them (starts NULL: n_tokens / n_seqs each), rows starts[b] ...
+ * of the matrices that hold new tokens; lengths[b] is what the sequence holds with them, so that row starts[b] + t is place
+ * lengths[b] - new_b + t.  max_new and max_length bound new_b and lengths[b] and size the launches.
+ * The arrays in device memory are not checked on the host.  What they name outside of these bounds is left out: rows beyond
+ * n_tokens or a sequence's max_new, lengths beyond max_length, entries of page_table outside [0, n_pages) (what would be stored
+ * there is dropped, and its keys are seen by no token: give -1 for pages that a window has left behind).  A sequence of length 0
+ * (an idle slot of a captured graph) stores and sees nothing.                                                     */
+typedef enum vq_kv_type { VQ_KV_FP16 = 0, VQ_KV_E4M3 = 1 } vq_kv_type;
+
+typedef struct vq_kv_desc {
+  uint32_t struct_size;                    /* = sizeof(vq_kv_desc)                                         */
+  int32_t type;                            /* vq_kv_type                                                   */
+  int32_t kv_heads, head_dim;              /* >= 1; head_dim a multiple of 16, at most 256                 */
+  int32_t page_tokens;                     /* 16, 32, 64, 128 or 256                                       */
+  int32_t n_pages;                         /* pages in the pool                                            */
+  int32_t n_seqs, n_tokens;                /* sequences and new tokens of this call                        */
+  int32_t max_new, max_length;             /* of one sequence; max_length <= table_pages * page_tokens     */
+  int32_t table_pages;                     /* entries of a row of page_table                               */
+  int32_t reserved;                        /* 0                                                            */
+  void *k_pages, *v_pages;                 /* 16-byte aligned                                              */
+  int64_t k_page_stride, v_page_stride;    /* elements from page to page; a page's bytes are a multiple of 16 */
+  float *k_scales, *v_scales;              /* [n_pages][kv_heads]; VQ_KV_E4M3 only                         */
+  const int32_t *page_table; int64_t table_stride;   /* [n_seqs][table_stride]                             */
+  const int32_t *lengths;                  /* [n_seqs]                                                     */
+  const int32_t *starts;                   /* [n_seqs + 1], ascending, or NULL                             */
+} vq_kv_desc;
+
+/* Rotary positions.  cos, sin: binary32 [positions][rotary_dim / 2], rows ld apart; rotary_dim even, at most head_dim (elements past it
+ * stay as they are).  Pair i is elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with interleaved != 0; (a, b) becomes (a c - b s, b c +
+ * a s), binary32, every operation rounded.  Token at place p takes row p, or position[row of the token] where position is given; rows outside [0,
+ * positions) are taken from the nearest one.                                                                    */
+typedef struct vq_rotary {
+  const float *cos, *sin;
+  int64_t ld;
+  int32_t positions, rotary_dim, interleaved;
+  const int32_t *position;                 /* [n_tokens] or NULL                                           */
+} vq_rotary;
+
+/* Appends new keys and values.  k, v: fp16 [n_tokens][ldk / ldv], head h at elements h * head_dim; the keys are rotated (rotary NULL: not)
+ * and stored.  q (may be NULL): fp16 [n_tokens][ldq], q_heads heads, is rotated into q_out (may be q), rounded once.
+ * 8-bit codes: a page's scale for a head is the smallest power of two S (2^-64 at least) with |x| <= 448 S for all finite elements x of the
+ * new tokens in it, or the page's scale so far if that is larger and the page holds earlier tokens of the sequence, which are
+ * otherwise re-encoded to S (exact but for codes that become subnormal).  A code is x / S rounded to nearest even; what is not
+ * finite becomes NaN.  Codes of places behind the sequence's end are left alone.  Two sequences must not share a page that
+ * either appends to.  Doing the same call again changes nothing.
+ * k, v, q and q_out are 2-byte aligned, cos and sin 4-byte; q_out must not overlap anything else that is read.        */
+int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void *v, int64_t ldv, const void *q, int64_t ldq,
+                 int32_t q_heads, void *q_out, int64_t ldq_out, const vq_rotary *rotary, void *hip_stream);
+
+/* Attention of the new tokens over the cache (which holds them already).  q: fp16 [n_tokens][ldq], q_heads heads (a multiple of
+ * kv_heads: query head h reads key head h / (q_heads / kv_heads)), out: fp16 [n_tokens][ldo].
+ *     out[t][h] = sum_j softmax_j(softmax_scale * q[t][h] . K[j]) V[j]
+ * over the places j that token t at place p sees: j <= p, and with window > 0 also j > p - window or j < sinks.  A token that sees
+ * nothing gets zeros.  lse (may be NULL): binary32 [n_tokens][q_heads], the logarithm of the sum of exp(score), -inf for such tokens.
+ * Scores, statistics and sums are binary32; the probabilities (relative to the largest so far) are rounded to binary16 for the matrix cores, the result once.
+ * Keys and values nobody sees may hold anything, NaN included.  softmax_scale must be finite and positive.
+ * Workspace (device memory, 256-byte aligned, contents undefined afterwards): with vq_attention_workspace_bytes bytes a
+ * sequence's keys are cut into parts where that fills the chip, and a second kernel joins them; with less or NULL each
+ * sequence's keys are taken in one part.  Results are deterministic run to run for the same sizes and workspace.  */
+size_t vq_attention_workspace_bytes(const vq_kv_desc *cache, int32_t q_heads, int32_t window, int32_t sinks);
+int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, int32_t window, int32_t sinks,
+                 void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Residual sum and norms between two blocks, for every row r < rows of `width` elements:
+ *     y = x + scale * gate * post(h)      post(h) = h * rsqrt(mean(h^2) + eps) * w_post, or h where w_post is NULL
+ *     z = y * rsqrt(mean(y^2) + eps) * w_pre
+ * h: fp16 [rows][ldh], the block's output, may be NULL (y = x; gate and w_post NULL).  x, y: the residual stream, fp16, or binary32 with stream32 != 0;
+ * y may be x, or NULL if only z is wanted.  gate: fp16 [width] (ldgate 0) or [rows][ldgate], may be NULL (1).  w_pre, w_post: fp16 [width].  z: fp16
+ * [rows][ldz], may be NULL (then w_pre too).  z may be h.  Sums and statistics are binary32; z is computed from y before y is rounded.
+ * width in 1 .. 32768; pointers aligned to their elements.  */
+int vq_residual_norm(const void *h, int64_t ldh, const void *x, int64_t ldx, const void *w_post, const void *gate, int64_t ldgate, float scale,
+                     const void *w_pre, float eps, int32_t stream32, int32_t rows, int32_t width, void *y, int64_t ldy, void *z, int64_t ldz,
+                     void *hip_stream);
+
 /* Text for a status code (static storage).  */
 const char *vq_status_string(int status);
 /* Library version, major*10000 + minor*100 + patch. */

@@ -31,6 +31,25 @@ class vq_layer_desc(ctypes.Structure):
     ]
 
 
+VQ_KV_FP16, VQ_KV_E4M3 = 0, 1
+
+
+class vq_kv_desc(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("type", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+        ("max_new", ctypes.c_int32), ("max_length", ctypes.c_int32), ("table_pages", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_page_stride", ctypes.c_int64), ("v_page_stride", ctypes.c_int64),
+        ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+    ]
+
+
+class vq_rotary(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("ld", ctypes.c_int64), ("positions", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("position", ctypes.c_void_p)]
+
+
 class VQError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -86,6 +105,18 @@ def load():
                                       ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
                                       ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
     L.vq_quantize_columns.restype = ctypes.c_int
+    K = ctypes.POINTER(vq_kv_desc)
+    L.vq_kv_append.argtypes = [K, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32,
+                               ctypes.c_void_p, ctypes.c_int64, ctypes.POINTER(vq_rotary), ctypes.c_void_p]
+    L.vq_attention_workspace_bytes.argtypes = [K, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
+    L.vq_attention_workspace_bytes.restype = ctypes.c_size_t
+    L.vq_attention.argtypes = [K, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                               ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    L.vq_residual_norm.argtypes = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                   ctypes.c_float, ctypes.c_void_p, ctypes.c_float, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                   ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
+    for f in (L.vq_kv_append, L.vq_attention, L.vq_residual_norm):
+        f.restype = ctypes.c_int
     L.vq_status_string.argtypes = [ctypes.c_int]
     L.vq_status_string.restype = ctypes.c_char_p
     L.vq_version.restype = ctypes.c_int
@@ -96,7 +127,7 @@ def load():
 
 
 EXPORTED = ["vq_validate", "vq_dequant", "vq_gemv", "vq_gemv_workspace_bytes", "vq_gemv_with_workspace", "vq_gemv_static_workspace", "vq_gemv_multi", "vq_gemm", "vq_gemm_default", "vq_gemm_workspace_bytes", "vq_gemm_fast_workspace_bytes",
-            "vq_gemm_default_workspace_bytes", "vq_gemm_default", "vq_assign", "vq_assign_down", "vq_quantize_columns", "vq_quantize_columns_workspace_bytes", "vq_status_string", "vq_version"]
+            "vq_gemm_default_workspace_bytes", "vq_gemm_default", "vq_assign", "vq_assign_down", "vq_quantize_columns", "vq_quantize_columns_workspace_bytes", "vq_kv_append", "vq_attention_workspace_bytes", "vq_attention", "vq_residual_norm", "vq_status_string", "vq_version"]
 
 
 # ---- the C entry points, same names, raw pointers (ints) and sizes ---------------------------------------
@@ -178,6 +209,27 @@ def vq_gemm_default_workspace_bytes(desc, tokens):
     return load().vq_gemm_default_workspace_bytes(ctypes.byref(desc), tokens)
 
 
+def vq_kv_append(cache, k_ptr, ldk, v_ptr, ldv, q_ptr=None, ldq=0, q_heads=0, q_out_ptr=None, ldq_out=0, rotary=None, stream=None):
+    return load().vq_kv_append(ctypes.byref(cache) if cache is not None else None, k_ptr, ldk, v_ptr, ldv, q_ptr, ldq, q_heads, q_out_ptr, ldq_out,
+                               ctypes.byref(rotary) if rotary is not None else None, stream)
+
+
+def vq_attention_workspace_bytes(cache, q_heads, window=0, sinks=0):
+    return load().vq_attention_workspace_bytes(ctypes.byref(cache), q_heads, window, sinks)
+
+
+def vq_attention(cache, q_ptr, ldq, q_heads, softmax_scale, window, sinks, out_ptr, ldo, lse_ptr=None, workspace_ptr=None, workspace_bytes=0,
+                 stream=None):
+    return load().vq_attention(ctypes.byref(cache) if cache is not None else None, q_ptr, ldq, q_heads, softmax_scale, window, sinks, out_ptr, ldo,
+                               lse_ptr, workspace_ptr, workspace_bytes, stream)
+
+
+def vq_residual_norm(h_ptr, ldh, x_ptr, ldx, w_post_ptr, gate_ptr, ldgate, scale, w_pre_ptr, eps, stream32, rows, width, y_ptr, ldy, z_ptr, ldz,
+                     stream=None):
+    return load().vq_residual_norm(h_ptr, ldh, x_ptr, ldx, w_post_ptr, gate_ptr, ldgate, scale, w_pre_ptr, eps, stream32, rows, width, y_ptr, ldy,
+                                   z_ptr, ldz, stream)
+
+
 def vq_status_string(status):
     return load().vq_status_string(status).decode()
 
@@ -199,7 +251,8 @@ def _native():
         from . import _binding as b
         b.bind({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value
                 for name in ("vq_gemv", "vq_gemv_with_workspace", "vq_gemv_multi", "vq_gemm", "vq_gemm_default", "vq_gemm_workspace_bytes",
-                             "vq_gemm_default_workspace_bytes", "vq_lend_gemv_bytes", "vq_lend_gemm_least_bytes", "vq_dequant", "vq_lend_assign")})
+                             "vq_gemm_default_workspace_bytes", "vq_lend_gemv_bytes", "vq_lend_gemm_least_bytes", "vq_dequant", "vq_lend_assign",
+                             "vq_kv_append", "vq_attention", "vq_attention_workspace_bytes", "vq_residual_norm")})
         _bound = b
     return _bound
 
@@ -420,3 +473,42 @@ def gemm(dl: DeviceLayer, X, out=None, workspace=None):
     if rc != VQ_OK:
         raise VQError(rc, "vq_gemm")
     return Y
+
+
+# ---- between a decoder layer's products: a paged cache, attention over it, residual sums with norms ---------------------
+# A cache is two tensors of pages, k_pages [pages][kv_heads][page_tokens][head_dim] and v_pages [pages][kv_heads][head_dim][page_tokens], of
+# float16 or float8_e4m3fn, the latter with float32 scales [pages][kv_heads]; page_table: int32 [sequences][pages of a sequence], lengths: int32
+# [sequences], what each holds with its new tokens; starts: int32 [sequences + 1], first row of each sequence's new tokens (None: as many for
+# each).  max_new and max_length bound a sequence's new tokens and its length (the caller knows them; None: all tokens, the table's size).
+
+def kv_append(k, v, k_pages, v_pages, page_table, lengths, k_scales=None, v_scales=None, q=None, cos=None, sin=None, position=None,
+              interleaved=False, starts=None, max_new=None, max_length=None, q_out=None):
+    """Rotates k (and q) by position and stores k, v: fp16 [tokens][heads][head_dim] device tensors; cos, sin: fp32 [positions][pairs] (None: no
+    rotation), position: int32 [tokens] (None: the place in the sequence).  -> q rotated (q_out, which may be q, or a new tensor), None without q."""
+    r = (_bound or _native()).kv_append(k_pages, v_pages, page_table, lengths, k_scales, v_scales, starts, max_new, max_length, k, v, q, q_out,
+                                        cos, sin, position, interleaved)
+    if r.__class__ is int:
+        raise VQError(r, "vq_kv_append")
+    return r
+
+
+def attention(q, k_pages, v_pages, page_table, lengths, k_scales=None, v_scales=None, starts=None, scale=None, window=0, sinks=0, max_new=None,
+              max_length=None, out=None, return_lse=False, workspace=None):
+    """q: fp16 [tokens][heads][head_dim] device tensor -> fp16 of the same sizes, with return_lse also the logarithms of the softmax's sums, fp32
+    [tokens][heads].  scale: None for head_dim ** -0.5; window, sinks: only the last `window` tokens and the first `sinks` ones are seen
+    (0: all).  workspace: a uint8 device tensor; None borrows what vq_attention_workspace_bytes asks for from torch's allocator, an empty
+    tensor leaves the library without."""
+    r = (_bound or _native()).attention(k_pages, v_pages, page_table, lengths, k_scales, v_scales, starts, max_new, max_length, q, scale, window,
+                                        sinks, out, return_lse, workspace)
+    if r.__class__ is int:
+        raise VQError(r, "vq_attention")
+    return r
+
+
+def residual_norm(h, x, pre=None, post=None, gate=None, scale=1.0, eps=1e-5, y=None, z=None):
+    """x + scale * gate * post-norm(h) and its norm: h: fp16 [rows][width] or None (x alone), x: fp16 or fp32, pre, post: fp16 [width] weights or
+    None (no norm), gate: fp16 [width] or [rows][width] or None -> (y of x's type, z fp16 or None without pre).  y may be x and z may be h."""
+    r = (_bound or _native()).residual_norm(h, x, pre, post, gate, scale, eps, y, z)
+    if r.__class__ is int:
+        raise VQError(r, "vq_residual_norm")
+    return r

@@ -1,5 +1,6 @@
 // C-ABI entry points: descriptor validation and dispatch.  All device work is in the kernel files.
 #include "vq_common.hpp"
+#include "vq_kv.hpp"
 #include "vq_lend.h"
 #include <cstdlib>
 #include <cstring>
@@ -363,6 +364,112 @@ extern "C" int vq_quantize_columns(void *W, int64_t ldw, int32_t rows, int32_t c
                                      static_cast<const __half *>(codebook), v, k, static_cast<const __half *>(codebook_res), k_res, block,
                                      static_cast<unsigned char *>(idx), idx_row_stride, static_cast<unsigned char *>(idx_res),
                                      idx_res_row_stride, static_cast<float *>(T), ldt, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+// ---- paged cache, attention, norms ----
+namespace vq {
+
+int make_kv_params(const vq_kv_desc *d, KvParams *p) {
+  if (!d) return VQ_ERR_NULL;
+  if (d->struct_size != sizeof(vq_kv_desc) || d->reserved != 0) return VQ_ERR_SHAPE;
+  if (d->type != VQ_KV_FP16 && d->type != VQ_KV_E4M3) return VQ_ERR_SHAPE;
+  const bool e4m3 = d->type == VQ_KV_E4M3;
+  if (d->kv_heads < 1 || d->kv_heads > 65536 || d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16 != 0) return VQ_ERR_SHAPE;
+  int shift = 4;
+  while (shift < 8 && (1 << shift) != d->page_tokens) ++shift;
+  if ((1 << shift) != d->page_tokens) return VQ_ERR_SHAPE;
+  if (d->n_pages < 1 || d->n_seqs < 1 || d->n_tokens < 1 || d->max_new < 1 || d->max_new > d->n_tokens || d->max_length < 0) return VQ_ERR_SHAPE;
+  if (d->table_pages < 0 || d->max_length > (long long)d->table_pages * d->page_tokens || d->table_stride < d->table_pages) return VQ_ERR_SHAPE;
+  if (!d->starts && (d->n_tokens % d->n_seqs != 0 || d->max_new < d->n_tokens / d->n_seqs)) return VQ_ERR_SHAPE;
+  if (!d->k_pages || !d->v_pages || !d->lengths || (!d->page_table && d->table_pages) || (e4m3 && (!d->k_scales || !d->v_scales))) return VQ_ERR_NULL;
+  const long long page = (long long)d->kv_heads * d->page_tokens * d->head_dim, element = e4m3 ? 1 : 2, most = 0x7fffffffffffffffll / 4;
+  if (d->k_page_stride < page || d->v_page_stride < page || d->k_page_stride > most || d->v_page_stride > most) return VQ_ERR_SHAPE;
+  if (!aligned(d->k_pages, 16) || !aligned(d->v_pages, 16) || d->k_page_stride * element % 16 || d->v_page_stride * element % 16) return VQ_ERR_ALIGNMENT;
+  if (!aligned(d->lengths, 4) || !aligned(d->page_table, 4) || !aligned(d->starts, 4) || (e4m3 && (!aligned(d->k_scales, 4) || !aligned(d->v_scales, 4))))
+    return VQ_ERR_ALIGNMENT;
+  KvParams q{};
+  q.e4m3 = e4m3;
+  q.kv_heads = d->kv_heads; q.head_dim = d->head_dim; q.page_shift = shift; q.n_pages = d->n_pages;
+  q.n_seqs = d->n_seqs; q.n_tokens = d->n_tokens; q.max_new = d->max_new; q.max_length = d->max_length; q.table_pages = d->table_pages;
+  q.each = d->starts ? 0 : d->n_tokens / d->n_seqs;
+  q.k_pages = static_cast<unsigned char *>(d->k_pages); q.v_pages = static_cast<unsigned char *>(d->v_pages);
+  q.k_page_bytes = d->k_page_stride * element; q.v_page_bytes = d->v_page_stride * element; q.table_stride = d->table_stride;
+  q.k_scales = e4m3 ? d->k_scales : nullptr; q.v_scales = e4m3 ? d->v_scales : nullptr;
+  q.page_table = d->page_table; q.lengths = d->lengths; q.starts = d->starts;
+  if (p) *p = q;
+  return VQ_OK;
+}
+
+// Query heads, window and first tokens of a call of vq_attention.
+static int make_attention_params(const KvParams &c, int32_t q_heads, int32_t window, int32_t sinks, AttentionParams *a) {
+  if (q_heads < 1 || q_heads > 65536 || q_heads % c.kv_heads != 0 || window < 0 || sinks < 0) return VQ_ERR_SHAPE;
+  *a = AttentionParams{};
+  a->q_heads = q_heads; a->group = q_heads / c.kv_heads;
+  a->window = window; a->sinks = window ? sinks : 0;
+  return VQ_OK;
+}
+
+}  // namespace vq
+
+extern "C" int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void *v, int64_t ldv, const void *q, int64_t ldq,
+                            int32_t q_heads, void *q_out, int64_t ldq_out, const vq_rotary *rotary, void *hip_stream) {
+  vq::KvParams c;
+  const int rc = vq::make_kv_params(cache, &c);
+  if (rc != VQ_OK) return rc;
+  if (!k || !v || (q && !q_out)) return VQ_ERR_NULL;
+  const long long kv_width = (long long)c.kv_heads * c.head_dim;
+  if (ldk < kv_width || ldv < kv_width) return VQ_ERR_SHAPE;
+  if (q && (q_heads < 1 || q_heads > 65536 || ldq < (long long)q_heads * c.head_dim || ldq_out < (long long)q_heads * c.head_dim)) return VQ_ERR_SHAPE;
+  if (!aligned(k, 2) || !aligned(v, 2) || (q && (!aligned(q, 2) || !aligned(q_out, 2)))) return VQ_ERR_ALIGNMENT;
+  vq::Rotary r{};
+  if (rotary) {
+    if (!rotary->cos || !rotary->sin) return VQ_ERR_NULL;
+    if (rotary->positions < 1 || rotary->rotary_dim < 2 || rotary->rotary_dim % 2 != 0 || rotary->rotary_dim > c.head_dim || rotary->ld < rotary->rotary_dim / 2)
+      return VQ_ERR_SHAPE;
+    if (!aligned(rotary->cos, 4) || !aligned(rotary->sin, 4) || !aligned(rotary->position, 4)) return VQ_ERR_ALIGNMENT;
+    r = vq::Rotary{rotary->cos, rotary->sin, rotary->ld, rotary->positions, rotary->rotary_dim, rotary->interleaved != 0, rotary->position};
+  }
+  return vq::launch_kv_append(c, static_cast<const __half *>(k), ldk, static_cast<const __half *>(v), ldv, static_cast<const __half *>(q), ldq,
+                              q ? q_heads : 0, static_cast<__half *>(q_out), ldq_out, r, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" size_t vq_attention_workspace_bytes(const vq_kv_desc *cache, int32_t q_heads, int32_t window, int32_t sinks) {
+  vq::KvParams c;
+  vq::AttentionParams a;
+  if (vq::make_kv_params(cache, &c) != VQ_OK || vq::make_attention_params(c, q_heads, window, sinks, &a) != VQ_OK) return 0;
+  return vq::attention_workspace_bytes(c, a);
+}
+
+extern "C" int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, int32_t window, int32_t sinks,
+                            void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  vq::KvParams c;
+  vq::AttentionParams a;
+  int rc = vq::make_kv_params(cache, &c);
+  if (rc != VQ_OK) return rc;
+  if (!q || !out) return VQ_ERR_NULL;
+  if ((rc = vq::make_attention_params(c, q_heads, window, sinks, &a)) != VQ_OK) return rc;
+  const long long width = (long long)q_heads * c.head_dim;
+  if (ldq < width || ldo < width || !(softmax_scale > 0.f && softmax_scale <= 1e30f)) return VQ_ERR_SHAPE;
+  if (!aligned(q, 2) || !aligned(out, 2) || !aligned(lse, 4) || !aligned(workspace, 256)) return VQ_ERR_ALIGNMENT;
+  a.q = static_cast<const __half *>(q); a.ldq = ldq;
+  a.out = static_cast<__half *>(out); a.ldo = ldo;
+  a.lse = lse;
+  a.scale = softmax_scale * 1.4426950408889634f;
+  return vq::launch_attention(c, a, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int vq_residual_norm(const void *h, int64_t ldh, const void *x, int64_t ldx, const void *w_post, const void *gate, int64_t ldgate,
+                                float scale, const void *w_pre, float eps, int32_t stream32, int32_t rows, int32_t width, void *y, int64_t ldy,
+                                void *z, int64_t ldz, void *hip_stream) {
+  if (!x || (!y && !z) || (z && !w_pre) || (!h && (w_post || gate))) return VQ_ERR_NULL;
+  if (rows < 1 || width < 1 || width > 32768 || ldx < width || (h && ldh < width) || (y && ldy < width) || (z && ldz < width)) return VQ_ERR_SHAPE;
+  if ((gate && ldgate != 0 && ldgate < width) || !(eps >= 0.f)) return VQ_ERR_SHAPE;
+  const uintptr_t stream = stream32 ? 4 : 2;
+  if (!aligned(x, stream) || !aligned(y, stream) || !aligned(h, 2) || !aligned(z, 2) || !aligned(w_post, 2) || !aligned(gate, 2) || !aligned(w_pre, 2))
+    return VQ_ERR_ALIGNMENT;
+  return vq::launch_residual_norm(static_cast<const __half *>(h), ldh, x, ldx, static_cast<const __half *>(w_post), static_cast<const __half *>(gate), ldgate,
+                                  scale, static_cast<const __half *>(w_pre), eps, stream32 != 0, rows, width, y, ldy, static_cast<__half *>(z), ldz,
+                                  static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" const char *vq_status_string(int status) {
