@@ -1,0 +1,80 @@
+// What the attention kernels share: which keys a tile of rows looks at, and how partial results are passed on (internal).
+#pragma once
+#include "vq_kv.hpp"
+
+namespace vq {
+
+// How a sequence's keys are cut into parts: as many as `parts`, or fewer where a part would get less than `least` chunks of 64 keys.
+struct Split {
+  int parts, least;
+  float *o, *ml;               // partial outputs [seq][kv head][part][row][head_dim], maxima and sums [seq][kv head][part][row][2]
+};
+
+int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
+int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
+
+#ifdef __HIPCC__
+// The rows of a key head are (new token t, query head of its group), t * group + g.  A tile of them sees keys [low, end) and [0, sinks), of
+// which some rows may see fewer; they are looked at in chunks of 64 keys: `sink_chunks` from 0 on, the others from `first` on.
+struct Span {
+  int place_min, place_max, low, end, first, sink_chunks, chunks;
+  __device__ __forceinline__ int chunk(int i) const { return i < sink_chunks ? i : first + i - sink_chunks; }
+};
+__device__ __forceinline__ Span span_of(const AttentionParams &a, const Sequence &s, int row0, int rows) {
+  Span v;
+  v.place_min = s.first + row0 / a.group;
+  v.place_max = s.first + (min(row0 + rows, s.rows * a.group) - 1) / a.group;
+  v.end = max(min(v.place_max + 1, s.end), 0);
+  v.low = a.window > 0 ? max(v.place_min - a.window + 1, 0) : 0;
+  v.first = v.low >> 6;
+  v.sink_chunks = min((min(a.sinks, v.low) + 63) >> 6, v.first);
+  v.chunks = v.end > 0 ? v.sink_chunks + max(((v.end + 63) >> 6) - v.first, 0) : 0;
+  return v;
+}
+// Chunks of each part, and how many parts there are (one at least).
+__device__ __forceinline__ int part_chunks(const Split &s, int chunks) { return max((chunks + s.parts - 1) / s.parts, s.least); }
+__device__ __forceinline__ int parts_of(const Split &s, int chunks) {
+  const int per = part_chunks(s, chunks);
+  return max((chunks + per - 1) / per, 1);
+}
+
+// Maximum and sum over the four rows of sixteen lanes, in every lane.  (The exchanged words are named before they are reinterpreted: a bit cast of
+// a vector's element was compiled as that of its first.)
+__device__ __forceinline__ void across_halves(float x, float &low, float &high) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const unsigned a = r[0], b = r[1];
+  low = __uint_as_float(a);
+  high = __uint_as_float(b);
+}
+__device__ __forceinline__ void across_rows(float x, float &even, float &odd) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const unsigned a = r[0], b = r[1];
+  even = __uint_as_float(a);
+  odd = __uint_as_float(b);
+}
+__device__ __forceinline__ float rows_max(float x) {
+  float a, b;
+  across_halves(x, a, b);
+  across_rows(fmaxf(a, b), a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float rows_sum(float x) {
+  float a, b;
+  across_halves(x, a, b);
+  across_rows(a + b, a, b);
+  return a + b;
+}
+
+__device__ __forceinline__ half8v halves_of_e4m3(unsigned a, unsigned b, float scale) {
+  const half2v w = halves_of_e4m3<false>(a, scale), x = halves_of_e4m3<true>(a, scale), y = halves_of_e4m3<false>(b, scale), z = halves_of_e4m3<true>(b, scale);
+  return half8v{w.x, w.y, x.x, x.y, y.x, y.y, z.x, z.y};
+}
+
+// A finite stand-in for the maximum of a row that has seen nothing yet.
+__device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
+// One over a softmax's sum; zero for a row that sees nothing; what is not a number stays none.
+__device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.6931471805599453f; }
+#endif
+
+}  // namespace vq

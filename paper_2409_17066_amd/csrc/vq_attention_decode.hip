@@ -1,0 +1,324 @@
+// Attention of few rows a key head (one token or a few drafted ones, times the query heads that share it) over a paged cache: the decode path.
+//
+// Bytes of keys and values bound it, so nothing is staged: eight waves of a workgroup take chunks of 64 keys in turn, each lane loading sixteen bytes
+// that are already what it feeds to the matrix cores, and the next chunk's keys and values are on their way while this one's are used.  With
+// v_mfma_f32_16x16x32_f16 the scores come transposed, S^T = K Q^T: a lane (row n of sixteen, lane group g of four) gets four keys of
+// each of the chunk's four tiles.  Which key is which row of a tile is free: key 16 g + 4 tile + r makes a lane's sixteen scores those of keys 16 g ..
+// 16 g + 15, and the same lane group then holds exactly these keys of the values, whose tokens lie next to each other in the cache, as
+// operand A of O^T = V^T P^T.  Likewise the elements of a head are dealt to the lanes sixteen bytes at a time, in the queries as in the keys.  So there
+// are no shuffles but for the maximum over four lane groups, and the running maximum of a row scales registers of the same lane.
+#include "vq_attention.hpp"
+
+namespace vq {
+
+namespace {
+
+constexpr int WAVES = 8;
+
+// RT: tiles of sixteen rows; D: elements of a head.
+template <bool E4M3, int D, int RT>
+__global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles) {
+  constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
+  constexpr bool AHEAD = E4M3 || D == 64 || RT == 1;             // the next chunk is loaded ahead where there are registers for it
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  int at = (int)blockIdx.x;
+  const int part = at % split.parts;
+  at /= split.parts;
+  const int kv_head = at % c.kv_heads;
+  at /= c.kv_heads;
+  const int tile = at % tiles, b = at / tiles;
+  const Sequence s = sequence(c, b);
+  const int rows = s.rows * a.group, row0 = tile * 16 * RT, here = min(rows - row0, 16 * RT);
+  if (here <= 0) return;
+  const Span span = span_of(a, s, row0, 16 * RT);
+  const int per = part_chunks(split, span.chunks), begin = part * per, end = min(span.chunks, begin + per);
+  if (part > 0 && begin >= span.chunks) return;
+  const int active = min(max(end - begin, 0), WAVES);            // waves that have a chunk
+
+  // the rows of this lane: new token, query head, place
+  const int shift = c.page_shift, mask = (1 << shift) - 1;
+  half8v q[RT][STEPS];
+  int place[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = min(row0 + rt * 16 + n, rows - 1), t = r / a.group;
+    place[rt] = s.first + t;
+    const __half *x = a.q + (s.row0 + t) * a.ldq + ((long long)kv_head * a.group + r - t * a.group) * D;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i)
+      q[rt][i] = __builtin_bit_cast(half8v, (uint4v)*reinterpret_cast<const uint4b *>(x + (E4M3 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 32 + g * 8)));
+  }
+
+  float m[RT], l[RT];
+  float4v o[RT][DT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = -__builtin_inff();
+    l[rt] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[rt][dt] = float4v{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // page of sixteen places where a row looks at some of them, else page 0, whose contents are not used (nor its scale: it may be anything)
+  auto page_at = [&](int first_place, bool &there) {
+    const int block = first_place >> shift;
+    const int page = block < c.table_pages ? c.page_table[b * c.table_stride + block] : -1;
+    there = (unsigned)page < (unsigned)c.n_pages && first_place < span.end && (first_place + 15 >= span.low || first_place < a.sinks);
+    return there ? page : 0;
+  };
+  uint4v k[4][KL], v[DT][VL];
+  float k_scale = 1.f, v_scale = 1.f;
+  bool v_there = false;
+  int k_page = 0, v_page = 0;
+  bool unused, v_there_next = false;
+  auto pages_of = [&](int i) {
+    const int j0 = span.chunk(i) * 64;
+    k_page = page_at(j0 + 16 * (n >> 2), unused);
+    v_page = page_at(j0 + 16 * g, v_there_next);
+  };
+  auto load_k = [&](int i) {
+    const int j = span.chunk(i) * 64 + 16 * (n >> 2);
+    const unsigned char *from = c.k_pages + k_page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask) + (n & 3)) * (D * BYTES) + g * 16;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int w = 0; w < KL; ++w) k[t][w] = *reinterpret_cast<const uint4v *>(from + t * 4 * D * BYTES + w * 64);
+    if (E4M3) k_scale = c.k_scales[(long long)k_page * c.kv_heads + kv_head];
+  };
+  auto load_v = [&](int i) {
+    const int j = span.chunk(i) * 64 + 16 * g;
+    const unsigned char *from = c.v_pages + v_page * c.v_page_bytes + (((((long long)kv_head * D + n) << shift) + (j & mask)) * BYTES);
+    const int step = 16 * BYTES << shift;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int w = 0; w < VL; ++w) v[dt][w] = *reinterpret_cast<const uint4v *>(from + dt * step + w * 16);
+    if (E4M3) v_scale = v_there_next ? c.v_scales[(long long)v_page * c.kv_heads + kv_head] : 1.f;
+    v_there = v_there_next;
+  };
+
+  int i = begin + wave;
+  if (i < end) {
+    pages_of(i);
+    load_k(i);
+    if (AHEAD) load_v(i);
+  }
+  for (; i < end; i += WAVES) {
+    const int j0 = span.chunk(i) * 64, next = i + WAVES;
+    if (AHEAD && next < end) pages_of(next);
+    float4v sc[RT][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      half8v f[STEPS];
+#pragma unroll
+      for (int w = 0; w < KL; ++w) {
+        if constexpr (E4M3) {
+          f[2 * w] = halves_of_e4m3(k[t][w].x, k[t][w].y, k_scale);
+          f[2 * w + 1] = halves_of_e4m3(k[t][w].z, k[t][w].w, k_scale);
+        } else {
+          f[w] = __builtin_bit_cast(half8v, k[t][w]);
+        }
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float4v x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < STEPS; ++w) x = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[w], q[rt][w], x, 0, 0, 0);
+        sc[rt][t] = x;
+      }
+    }
+    if (AHEAD && next < end) load_k(next);
+    if (!AHEAD) load_v(i);
+    // keys that some row does not see: hidden from it; those that no row sees may hold anything, so their values are cleared
+    const bool all_there = __ballot(!v_there) == 0;
+    if (!all_there || j0 + 63 > span.place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= span.place_max - a.window)) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          float x[4] = {sc[rt][t].x, sc[rt][t].y, sc[rt][t].z, sc[rt][t].w};
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int j = j0 + 16 * g + 4 * t + r;
+            const bool sees = v_there && j <= place[rt] && j < s.end && (a.window <= 0 || j > place[rt] - a.window || j < a.sinks);
+            x[r] = sees ? x[r] : -__builtin_inff();
+          }
+          sc[rt][t] = float4v{x[0], x[1], x[2], x[3]};
+        }
+      unsigned keep[4 * VL];
+#pragma unroll
+      for (int w = 0; w < 4 * VL; ++w) {
+        keep[w] = 0;
+#pragma unroll
+        for (int r = 0; r < 4 / BYTES; ++r) {
+          const int j = j0 + 16 * g + w * (4 / BYTES) + r;
+          if (v_there && j < span.end && (j >= span.low || j < a.sinks)) keep[w] |= (E4M3 ? 0xffu : 0xffffu) << (8 * BYTES * r);
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int w = 0; w < VL; ++w) v[dt][w] &= uint4v{keep[4 * w], keep[4 * w + 1], keep[4 * w + 2], keep[4 * w + 3]};
+    }
+    half8v p[RT][2];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = fmaxf(fmaxf(fmaxf(sc[rt][0].x, sc[rt][0].y), fmaxf(sc[rt][0].z, sc[rt][0].w)), fmaxf(fmaxf(sc[rt][1].x, sc[rt][1].y), fmaxf(sc[rt][1].z, sc[rt][1].w)));
+      top = fmaxf(top, fmaxf(fmaxf(fmaxf(sc[rt][2].x, sc[rt][2].y), fmaxf(sc[rt][2].z, sc[rt][2].w)), fmaxf(fmaxf(sc[rt][3].x, sc[rt][3].y), fmaxf(sc[rt][3].z, sc[rt][3].w))));
+      const float now = fmaxf(m[rt], rows_max(top) * a.scale);
+      const float base = base_of(now);
+      if (__ballot(now > m[rt])) {
+        const float again = __builtin_amdgcn_exp2f(m[rt] - base);
+        l[rt] *= again;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= again;
+        m[rt] = now;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float e[8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const float4v x = sc[rt][2 * h + u];
+          e[4 * u] = __builtin_amdgcn_exp2f(__fmaf_rn(x.x, a.scale, -base));
+          e[4 * u + 1] = __builtin_amdgcn_exp2f(__fmaf_rn(x.y, a.scale, -base));
+          e[4 * u + 2] = __builtin_amdgcn_exp2f(__fmaf_rn(x.z, a.scale, -base));
+          e[4 * u + 3] = __builtin_amdgcn_exp2f(__fmaf_rn(x.w, a.scale, -base));
+        }
+        sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        // (rounded to nearest: what the matrix cores take; the sum is that of the unrounded ones)
+        p[rt][h] = half8v{(_Float16)e[0], (_Float16)e[1], (_Float16)e[2], (_Float16)e[3], (_Float16)e[4], (_Float16)e[5], (_Float16)e[6], (_Float16)e[7]};
+      }
+      l[rt] += sum;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      half8v f[2];
+      if constexpr (E4M3) {
+        f[0] = halves_of_e4m3(v[dt][0].x, v[dt][0].y, v_scale);
+        f[1] = halves_of_e4m3(v[dt][0].z, v[dt][0].w, v_scale);
+      } else {
+        f[0] = __builtin_bit_cast(half8v, v[dt][0]);
+        f[1] = __builtin_bit_cast(half8v, v[dt][VL - 1]);
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0], p[rt][0], o[rt][dt], 0, 0, 0);
+        o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1], p[rt][1], o[rt][dt], 0, 0, 0);
+      }
+    }
+    if (AHEAD && next < end) load_v(next);
+    if (!AHEAD && next < end) {
+      pages_of(next);
+      load_k(next);
+    }
+  }
+
+  // the waves' results, joined through LDS, sixteen rows at a time
+  float *ml = lds, *out = lds + 2 * 16 * WAVES;
+  const bool whole = parts_of(split, span.chunks) == 1;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int left = here - rt * 16;
+    if (left <= 0) break;
+    __syncthreads();
+    const float sum = rows_sum(l[rt]);
+    if (wave < active && lane < 16) {
+      ml[2 * (wave * 16 + n)] = m[rt];
+      ml[2 * (wave * 16 + n) + 1] = sum;
+    }
+    if (wave < active && n < left) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<float4v *>(out + (wave * 16 + n) * PITCH + dt * 16 + g * 4) = o[rt][dt];
+    }
+    __syncthreads();
+    for (int u = (int)threadIdx.x; u < min(left, 16) * (D / 4); u += 64 * WAVES) {
+      const int r = u / (D / 4), d = (u - r * (D / 4)) * 4;
+      float top = -__builtin_inff();
+      for (int w = 0; w < active; ++w) top = fmaxf(top, ml[2 * (w * 16 + r)]);
+      const float base = base_of(top);
+      float total = 0.f;
+      float4v x = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < active; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[2 * (w * 16 + r)] - base);
+        total = __fmaf_rn(ml[2 * (w * 16 + r) + 1], f, total);
+        const float4v y = *reinterpret_cast<const float4v *>(out + (w * 16 + r) * PITCH + d);
+        x.x = __fmaf_rn(y.x, f, x.x); x.y = __fmaf_rn(y.y, f, x.y); x.z = __fmaf_rn(y.z, f, x.z); x.w = __fmaf_rn(y.w, f, x.w);
+      }
+      const int row = row0 + rt * 16 + r;
+      if (whole) {
+        const int t = row / a.group, head = kv_head * a.group + row - t * a.group;
+        x *= inverse_of(total);
+        typedef _Float16 half4b __attribute__((ext_vector_type(4), aligned(2)));
+        *reinterpret_cast<half4b *>(a.out + (s.row0 + t) * a.ldo + (long long)head * D + d) = half4b{(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w};
+        if (a.lse && d == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
+      } else {
+        const long long to = (((long long)b * c.kv_heads + kv_head) * split.parts + part) * ((long long)c.max_new * a.group) + row;
+        *reinterpret_cast<float4v *>(split.o + to * D + d) = x;
+        if (d == 0) *reinterpret_cast<float2v *>(split.ml + to * 2) = float2v{top, total};
+      }
+    }
+  }
+}
+
+// Joins the parts of a sequence's keys: one wave to a row.
+__global__ __launch_bounds__(256) void attention_join_kernel(const KvParams c, const AttentionParams a, const Split split, int tile_rows) {
+  const int lane = (int)threadIdx.x & 63, rows_most = c.max_new * a.group;
+  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int row = (int)(at % rows_most), kv_head = (int)(at / rows_most % c.kv_heads), b = (int)(at / rows_most / c.kv_heads);
+  if (b >= c.n_seqs) return;
+  const Sequence s = sequence(c, b);
+  if (row >= s.rows * a.group) return;
+  const int parts = parts_of(split, span_of(a, s, row / tile_rows * tile_rows, tile_rows).chunks);
+  if (parts == 1) return;                                        // written already
+  const long long from = ((long long)b * c.kv_heads + kv_head) * split.parts * rows_most + row;
+  const int width = c.head_dim / 64;
+  // lane w < parts holds part w's maximum and sum (64 parts at most)
+  const float2v mine = lane < parts ? *reinterpret_cast<const float2v *>(split.ml + (from + (long long)lane * rows_most) * 2) : float2v{-__builtin_inff(), 0.f};
+  float top = mine.x;
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+  const float f = __builtin_amdgcn_exp2f(mine.x - base_of(top)), total = wave_sum(mine.y * f);
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int w = 0; w < parts; ++w) {
+    const float fw = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), w));
+    const float *o = split.o + (from + (long long)w * rows_most) * c.head_dim;
+    for (int i = 0; i < width; ++i) x[i] = __fmaf_rn(o[lane + 64 * i], fw, x[i]);
+  }
+  const int t = row / a.group, head = kv_head * a.group + row - t * a.group;
+  const float inverse = inverse_of(total);
+  for (int i = 0; i < width; ++i) a.out[(s.row0 + t) * a.ldo + (long long)head * c.head_dim + lane + 64 * i] = __float2half_rn(x[i] * inverse);
+  if (a.lse && lane == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
+}
+
+template <bool E4M3, int D, int RT>
+int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT);
+  const long long blocks = (long long)s.parts * c.kv_heads * tiles * c.n_seqs;
+  if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
+  const int lds = (2 * 16 + 16 * (D + 4)) * WAVES * 4;
+  VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT>));
+  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT>), dim3((unsigned)blocks), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
+  return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
+}
+
+}  // namespace
+
+int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  const bool two = c.max_new * (long long)a.group > 16;
+  if (c.head_dim == 64) return c.e4m3 ? (two ? launch<true, 64, 2>(c, a, s, stream) : launch<true, 64, 1>(c, a, s, stream))
+                                      : (two ? launch<false, 64, 2>(c, a, s, stream) : launch<false, 64, 1>(c, a, s, stream));
+  return c.e4m3 ? (two ? launch<true, 128, 2>(c, a, s, stream) : launch<true, 128, 1>(c, a, s, stream))
+                : (two ? launch<false, 128, 2>(c, a, s, stream) : launch<false, 128, 1>(c, a, s, stream));
+}
+
+int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream) {
+  const long long blocks = ((long long)c.n_seqs * c.kv_heads * c.max_new * a.group + 3) / 4;
+  if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
+  hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, c, a, s, tile_rows);
+  return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
+}
+
+}  // namespace vq
