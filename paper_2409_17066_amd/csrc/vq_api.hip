@@ -405,6 +405,8 @@ static int make_attention_params(const KvParams &c, int32_t q_heads, int32_t win
   if (q_heads < 1 || q_heads > 65536 || q_heads % c.kv_heads != 0 || window < 0 || sinks < 0) return VQ_ERR_SHAPE;
   *a = AttentionParams{};
   a->q_heads = q_heads; a->group = q_heads / c.kv_heads;
+  a->by_group = a->group > 1 ? (unsigned)((1ull << 32) / a->group) + 1 : 0;
+  if ((long long)c.max_new * a->group * a->group >= 1ll << 31) return VQ_ERR_SHAPE;          // (by_group is good for so many rows)
   a->window = window; a->sinks = window ? sinks : 0;
   return VQ_OK;
 }

@@ -97,20 +97,18 @@ namespace {
 
 // How a call is taken: `tile_rows` rows of a key head to a workgroup (0: the wave kernel), the keys in up to `parts` parts.
 struct Plan {
-  int tile_rows, parts, least;
+  int tile_rows, parts;
   size_t o_bytes, ml_bytes;
 };
 
 Plan plan_of(const KvParams &c, const AttentionParams &a) {
-  Plan p{0, 1, 1, 0, 0};
+  Plan p{0, 1, 0, 0};
   if (c.head_dim != 64 && c.head_dim != 128) return p;
   const long long rows = (long long)c.max_new * a.group;
-  p.tile_rows = rows > 16 ? 32 : 16;
-  p.least = 8;                                       // a chunk for every wave
+  p.tile_rows = attention_decode_rows(c, a);
   const long long seen = a.window > 0 ? std::min<long long>(c.max_length, (long long)a.window + a.sinks + p.tile_rows / a.group + 64) : c.max_length;
   const long long chunks = (seen + 63) / 64, groups = (long long)c.n_seqs * c.kv_heads * ((rows + p.tile_rows - 1) / p.tile_rows);
-  // Parts until there are two workgroups to a compute unit, of four chunks a wave at least: a second launch costs about 2 us.
-  const long long wanted = std::min((2LL * cu_count() + groups - 1) / groups, chunks / 32);
+  const long long wanted = std::min((long long)cu_count() / groups, chunks / 16);
   p.parts = (int)std::max(1LL, std::min(wanted, 64LL));
   if (p.parts > 1) {
     p.o_bytes = (size_t)c.n_seqs * c.kv_heads * p.parts * rows * c.head_dim * 4;
@@ -131,7 +129,7 @@ int launch_attention(const KvParams &c, const AttentionParams &a, void *workspac
   if (p.tile_rows) {
     const bool room = p.parts > 1 && workspace_bytes >= p.o_bytes + p.ml_bytes;
     float *o = static_cast<float *>(workspace);
-    const Split split{room ? p.parts : 1, p.least, o, room ? o + p.o_bytes / 4 : nullptr};
+    const Split split{room ? p.parts : 1, o, room ? o + p.o_bytes / 4 : nullptr};
     const int rc = launch_attention_decode(c, a, split, s);
     return rc != VQ_OK || !room ? rc : launch_attention_join(c, a, split, p.tile_rows, s);
   }

@@ -4,12 +4,15 @@
 
 namespace vq {
 
-// How a sequence's keys are cut into parts: as many as `parts`, or fewer where a part would get less than `least` chunks of 64 keys.
+// How a sequence's keys are cut into parts: part p takes every `parts`-th run of eight chunks of 64 keys from run p on, so that what a workgroup looks at
+// first does not depend on the sequence's length.
 struct Split {
-  int parts, least;
+  int parts;
   float *o, *ml;               // partial outputs [seq][kv head][part][row][head_dim], maxima and sums [seq][kv head][part][row][2]
 };
 
+// Rows of a key head to a workgroup of launch_attention_decode.
+int attention_decode_rows(const KvParams &c, const AttentionParams &a);
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
 
@@ -20,10 +23,12 @@ struct Span {
   int place_min, place_max, low, end, first, sink_chunks, chunks;
   __device__ __forceinline__ int chunk(int i) const { return i < sink_chunks ? i : first + i - sink_chunks; }
 };
+// The new token of a row of a key head.
+__device__ __forceinline__ int token_of(const AttentionParams &a, int row) { return a.group > 1 ? (int)__umulhi((unsigned)row, a.by_group) : row; }
 __device__ __forceinline__ Span span_of(const AttentionParams &a, const Sequence &s, int row0, int rows) {
   Span v;
-  v.place_min = s.first + row0 / a.group;
-  v.place_max = s.first + (min(row0 + rows, s.rows * a.group) - 1) / a.group;
+  v.place_min = s.first + token_of(a, row0);
+  v.place_max = s.first + token_of(a, min(row0 + rows, s.rows * a.group) - 1);
   v.end = max(min(v.place_max + 1, s.end), 0);
   v.low = a.window > 0 ? max(v.place_min - a.window + 1, 0) : 0;
   v.first = v.low >> 6;
@@ -31,12 +36,9 @@ __device__ __forceinline__ Span span_of(const AttentionParams &a, const Sequence
   v.chunks = v.end > 0 ? v.sink_chunks + max(((v.end + 63) >> 6) - v.first, 0) : 0;
   return v;
 }
-// Chunks of each part, and how many parts there are (one at least).
-__device__ __forceinline__ int part_chunks(const Split &s, int chunks) { return max((chunks + s.parts - 1) / s.parts, s.least); }
-__device__ __forceinline__ int parts_of(const Split &s, int chunks) {
-  const int per = part_chunks(s, chunks);
-  return max((chunks + per - 1) / per, 1);
-}
+constexpr int RUN = 8;
+// Parts that have chunks, one at least.
+__device__ __forceinline__ int parts_of(const Split &s, int chunks) { return max(min(s.parts, (chunks + RUN - 1) / RUN), 1); }
 
 // Maximum and sum over the four rows of sixteen lanes, in every lane.  (The exchanged words are named before they are reinterpreted: a bit cast of
 // a vector's element was compiled as that of its first.)

@@ -13,36 +13,41 @@ namespace vq {
 
 namespace {
 
-constexpr int WAVES = 8;
+constexpr int WAVES = RUN;
 
 // RT: tiles of sixteen rows; D: elements of a head.
 template <bool E4M3, int D, int RT>
 __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles) {
   constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
-  constexpr bool AHEAD = E4M3 || D == 64 || RT == 1;             // the next chunk is loaded ahead where there are registers for it
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  int at = (int)blockIdx.x;
-  const int part = at % split.parts;
-  at /= split.parts;
-  const int kv_head = at % c.kv_heads;
-  at /= c.kv_heads;
-  const int tile = at % tiles, b = at / tiles;
+  const int part = (int)blockIdx.z, kv_head = (int)blockIdx.y, b = tiles > 1 ? (int)blockIdx.x / tiles : (int)blockIdx.x, tile = tiles > 1 ? (int)blockIdx.x % tiles : 0;
+  const int shift = c.page_shift, mask = (1 << shift) - 1;
+  // Entries of the page table for places [of, of + 16).  Without a window the first ones do not depend on the sequence's length, and are asked for beside it.
+  auto entry = [&](int of) { return of >> shift < c.table_pages ? c.page_table[b * c.table_stride + (of >> shift)] : -1; };
+  int i = part * RUN + wave, k_entry = 0, v_entry = 0;
+  if (a.window == 0) {
+    k_entry = entry(i * 64 + 16 * (n >> 2));
+    v_entry = entry(i * 64 + 16 * g);
+  }
   const Sequence s = sequence(c, b);
   const int rows = s.rows * a.group, row0 = tile * 16 * RT, here = min(rows - row0, 16 * RT);
   if (here <= 0) return;
   const Span span = span_of(a, s, row0, 16 * RT);
-  const int per = part_chunks(split, span.chunks), begin = part * per, end = min(span.chunks, begin + per);
-  if (part > 0 && begin >= span.chunks) return;
+  const int begin = part * RUN, end = span.chunks, stride = split.parts * RUN;
+  if (part > 0 && begin >= end) return;
   const int active = min(max(end - begin, 0), WAVES);            // waves that have a chunk
+  if (a.window != 0 && i < end) {
+    k_entry = entry(span.chunk(i) * 64 + 16 * (n >> 2));
+    v_entry = entry(span.chunk(i) * 64 + 16 * g);
+  }
 
   // the rows of this lane: new token, query head, place
-  const int shift = c.page_shift, mask = (1 << shift) - 1;
   half8v q[RT][STEPS];
   int place[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int r = min(row0 + rt * 16 + n, rows - 1), t = r / a.group;
+    const int r = min(row0 + rt * 16 + n, rows - 1), t = token_of(a, r);
     place[rt] = s.first + t;
     const __half *x = a.q + (s.row0 + t) * a.ldq + ((long long)kv_head * a.group + r - t * a.group) * D;
 #pragma unroll
@@ -61,52 +66,47 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
   }
 
   // page of sixteen places where a row looks at some of them, else page 0, whose contents are not used (nor its scale: it may be anything)
-  auto page_at = [&](int first_place, bool &there) {
-    const int block = first_place >> shift;
-    const int page = block < c.table_pages ? c.page_table[b * c.table_stride + block] : -1;
-    there = (unsigned)page < (unsigned)c.n_pages && first_place < span.end && (first_place + 15 >= span.low || first_place < a.sinks);
-    return there ? page : 0;
+  auto page_at = [&](int of, int entry, bool &there) {
+    there = (unsigned)entry < (unsigned)c.n_pages && of < span.end && (of + 15 >= span.low || of < a.sinks);
+    return there ? entry : 0;
   };
   uint4v k[4][KL], v[DT][VL];
   float k_scale = 1.f, v_scale = 1.f;
   bool v_there = false;
-  int k_page = 0, v_page = 0;
-  bool unused, v_there_next = false;
-  auto pages_of = [&](int i) {
-    const int j0 = span.chunk(i) * 64;
-    k_page = page_at(j0 + 16 * (n >> 2), unused);
-    v_page = page_at(j0 + 16 * g, v_there_next);
+  auto entries_of = [&](int i) {
+    k_entry = entry(span.chunk(i) * 64 + 16 * (n >> 2));
+    v_entry = entry(span.chunk(i) * 64 + 16 * g);
   };
   auto load_k = [&](int i) {
     const int j = span.chunk(i) * 64 + 16 * (n >> 2);
-    const unsigned char *from = c.k_pages + k_page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask) + (n & 3)) * (D * BYTES) + g * 16;
+    bool there;
+    const int page = page_at(j, k_entry, there);
+    const unsigned char *from = c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask) + (n & 3)) * (D * BYTES) + g * 16;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int w = 0; w < KL; ++w) k[t][w] = *reinterpret_cast<const uint4v *>(from + t * 4 * D * BYTES + w * 64);
-    if (E4M3) k_scale = c.k_scales[(long long)k_page * c.kv_heads + kv_head];
+    if (E4M3) k_scale = c.k_scales[(long long)page * c.kv_heads + kv_head];
   };
   auto load_v = [&](int i) {
     const int j = span.chunk(i) * 64 + 16 * g;
-    const unsigned char *from = c.v_pages + v_page * c.v_page_bytes + (((((long long)kv_head * D + n) << shift) + (j & mask)) * BYTES);
+    const int page = page_at(j, v_entry, v_there);
+    const unsigned char *from = c.v_pages + page * c.v_page_bytes + (((((long long)kv_head * D + n) << shift) + (j & mask)) * BYTES);
     const int step = 16 * BYTES << shift;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int w = 0; w < VL; ++w) v[dt][w] = *reinterpret_cast<const uint4v *>(from + dt * step + w * 16);
-    if (E4M3) v_scale = v_there_next ? c.v_scales[(long long)v_page * c.kv_heads + kv_head] : 1.f;
-    v_there = v_there_next;
+    if (E4M3) v_scale = v_there ? c.v_scales[(long long)page * c.kv_heads + kv_head] : 1.f;
   };
 
-  int i = begin + wave;
   if (i < end) {
-    pages_of(i);
     load_k(i);
-    if (AHEAD) load_v(i);
+    load_v(i);
   }
-  for (; i < end; i += WAVES) {
-    const int j0 = span.chunk(i) * 64, next = i + WAVES;
-    if (AHEAD && next < end) pages_of(next);
+  for (; i < end; i += stride) {
+    const int j0 = span.chunk(i) * 64, next = i + stride;
+    if (next < end) entries_of(next);
     float4v sc[RT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -128,8 +128,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
         sc[rt][t] = x;
       }
     }
-    if (AHEAD && next < end) load_k(next);
-    if (!AHEAD) load_v(i);
+    if (next < end) load_k(next);
     // keys that some row does not see: hidden from it; those that no row sees may hold anything, so their values are cleared
     const bool all_there = __ballot(!v_there) == 0;
     if (!all_there || j0 + 63 > span.place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= span.place_max - a.window)) {
@@ -209,11 +208,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
         o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1], p[rt][1], o[rt][dt], 0, 0, 0);
       }
     }
-    if (AHEAD && next < end) load_v(next);
-    if (!AHEAD && next < end) {
-      pages_of(next);
-      load_k(next);
-    }
+    if (next < end) load_v(next);
   }
 
   // the waves' results, joined through LDS, sixteen rows at a time
@@ -249,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
       }
       const int row = row0 + rt * 16 + r;
       if (whole) {
-        const int t = row / a.group, head = kv_head * a.group + row - t * a.group;
+        const int t = token_of(a, row), head = kv_head * a.group + row - t * a.group;
         x *= inverse_of(total);
         typedef _Float16 half4b __attribute__((ext_vector_type(4), aligned(2)));
         *reinterpret_cast<half4b *>(a.out + (s.row0 + t) * a.ldo + (long long)head * D + d) = half4b{(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w};
@@ -263,61 +258,93 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
   }
 }
 
-// Joins the parts of a sequence's keys: one wave to a row.
-__global__ __launch_bounds__(256) void attention_join_kernel(const KvParams c, const AttentionParams a, const Split split, int tile_rows) {
-  const int lane = (int)threadIdx.x & 63, rows_most = c.max_new * a.group;
-  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = (int)(at % rows_most), kv_head = (int)(at / rows_most % c.kv_heads), b = (int)(at / rows_most / c.kv_heads);
-  if (b >= c.n_seqs) return;
+// Joins the parts of a sequence's keys: a workgroup to a row, whose threads take four elements of a share of the parts each.
+constexpr int JOIN_THREADS = 256;
+
+template <int D>
+__global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvParams c, const AttentionParams a, const Split split, int tile_rows) {
+  constexpr int LANES = D / 4, SHARES = JOIN_THREADS / LANES;
+  __shared__ __attribute__((aligned(16))) float shares[SHARES][D];
+  __shared__ float factors[64];
+  const int rows_most = c.max_new * a.group, lane = (int)threadIdx.x & 63;
+  const int row = (int)blockIdx.x, kv_head = (int)blockIdx.y, b = (int)blockIdx.z;
+  const long long from = ((long long)b * c.kv_heads + kv_head) * split.parts * rows_most + row;
+  // lane w < parts of every wave takes part w's maximum and sum (64 parts at most); loaded, as the outputs are, before it is known how many there are
+  const float2v mine = lane < split.parts ? *reinterpret_cast<const float2v *>(split.ml + (from + (long long)lane * rows_most) * 2) : float2v{0.f, 0.f};
+  const int share = (int)threadIdx.x / LANES, d = (int)(threadIdx.x % LANES) * 4;
+  float4v y[4];
+  auto load = [&](int w0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int w = w0 + u * SHARES;
+      y[u] = w < split.parts ? *reinterpret_cast<const float4v *>(split.o + (from + (long long)w * rows_most) * D + d) : float4v{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  load(share);
   const Sequence s = sequence(c, b);
   if (row >= s.rows * a.group) return;
-  const int parts = parts_of(split, span_of(a, s, row / tile_rows * tile_rows, tile_rows).chunks);
+  const int parts = parts_of(split, span_of(a, s, row & -tile_rows, tile_rows).chunks);
   if (parts == 1) return;                                        // written already
-  const long long from = ((long long)b * c.kv_heads + kv_head) * split.parts * rows_most + row;
-  const int width = c.head_dim / 64;
-  // lane w < parts holds part w's maximum and sum (64 parts at most)
-  const float2v mine = lane < parts ? *reinterpret_cast<const float2v *>(split.ml + (from + (long long)lane * rows_most) * 2) : float2v{-__builtin_inff(), 0.f};
-  float top = mine.x;
+  const float m = lane < parts ? mine.x : -__builtin_inff();
+  float top = m;
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-  const float f = __builtin_amdgcn_exp2f(mine.x - base_of(top)), total = wave_sum(mine.y * f);
-  float x[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int w = 0; w < parts; ++w) {
-    const float fw = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), w));
-    const float *o = split.o + (from + (long long)w * rows_most) * c.head_dim;
-    for (int i = 0; i < width; ++i) x[i] = __fmaf_rn(o[lane + 64 * i], fw, x[i]);
+  const float f = __builtin_amdgcn_exp2f(m - base_of(top)), total = wave_sum(lane < parts ? mine.y * f : 0.f);
+  if (threadIdx.x < 64) factors[lane] = f;
+  __syncthreads();
+  float4v x = {0.f, 0.f, 0.f, 0.f};
+  for (int w0 = share; w0 < parts; w0 += 4 * SHARES) {
+    if (w0 != share) load(w0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int w = w0 + u * SHARES;
+      if (w >= parts) break;                                     // (what is there was not written by this call)
+      const float fw = factors[w];
+      x.x = __fmaf_rn(y[u].x, fw, x.x); x.y = __fmaf_rn(y[u].y, fw, x.y); x.z = __fmaf_rn(y[u].z, fw, x.z); x.w = __fmaf_rn(y[u].w, fw, x.w);
+    }
   }
-  const int t = row / a.group, head = kv_head * a.group + row - t * a.group;
-  const float inverse = inverse_of(total);
-  for (int i = 0; i < width; ++i) a.out[(s.row0 + t) * a.ldo + (long long)head * c.head_dim + lane + 64 * i] = __float2half_rn(x[i] * inverse);
-  if (a.lse && lane == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
+  *reinterpret_cast<float4v *>(&shares[share][d]) = x;
+  __syncthreads();
+  const int t = token_of(a, row), head = kv_head * a.group + row - t * a.group;
+  if ((int)threadIdx.x < D) {
+    float y = 0.f;
+#pragma unroll
+    for (int w = 0; w < SHARES; ++w) y += shares[w][threadIdx.x];
+    a.out[(s.row0 + t) * a.ldo + (long long)head * D + threadIdx.x] = __float2half_rn(y * inverse_of(total));
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
 }
 
 template <bool E4M3, int D, int RT>
 int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
   const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT);
-  const long long blocks = (long long)s.parts * c.kv_heads * tiles * c.n_seqs;
-  if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
+  const long long blocks = (long long)tiles * c.n_seqs;
+  if (blocks > 0x7fffffff / 512 || c.kv_heads > 65535) return VQ_ERR_SHAPE;
   const int lds = (2 * 16 + 16 * (D + 4)) * WAVES * 4;
   VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT>));
-  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT>), dim3((unsigned)blocks), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
+  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT>), dim3((unsigned)blocks, c.kv_heads, s.parts), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 
 }  // namespace
 
+// Two tiles share the conversions and loads of a chunk, where the registers are there: not beside 64 of a 16-bit chunk's keys and as many of its values.
+int attention_decode_rows(const KvParams &c, const AttentionParams &a) {
+  return (long long)c.max_new * a.group > 16 && (c.e4m3 || c.head_dim == 64) ? 32 : 16;
+}
+
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  const bool two = c.max_new * (long long)a.group > 16;
+  const bool two = attention_decode_rows(c, a) == 32;
   if (c.head_dim == 64) return c.e4m3 ? (two ? launch<true, 64, 2>(c, a, s, stream) : launch<true, 64, 1>(c, a, s, stream))
                                       : (two ? launch<false, 64, 2>(c, a, s, stream) : launch<false, 64, 1>(c, a, s, stream));
-  return c.e4m3 ? (two ? launch<true, 128, 2>(c, a, s, stream) : launch<true, 128, 1>(c, a, s, stream))
-                : (two ? launch<false, 128, 2>(c, a, s, stream) : launch<false, 128, 1>(c, a, s, stream));
+  return c.e4m3 ? (two ? launch<true, 128, 2>(c, a, s, stream) : launch<true, 128, 1>(c, a, s, stream)) : launch<false, 128, 1>(c, a, s, stream);
 }
 
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream) {
-  const long long blocks = ((long long)c.n_seqs * c.kv_heads * c.max_new * a.group + 3) / 4;
-  if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
-  hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, c, a, s, tile_rows);
+  const dim3 blocks(c.max_new * a.group, c.kv_heads, c.n_seqs);
+  if (c.kv_heads > 65535 || c.n_seqs > 65535) return VQ_ERR_SHAPE;
+  if (c.head_dim == 64) hipLaunchKernelGGL((attention_join_kernel<64>), blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
+  else hipLaunchKernelGGL((attention_join_kernel<128>), blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 

@@ -34,6 +34,7 @@ struct AttentionParams {
   float *lse;
   float scale;                   // of the scores, times log2(e)
   int q_heads, group, window, sinks;
+  unsigned by_group;             // 2^32 / group, rounded up: r / group is the upper half of r * by_group for all rows r (group > 1)
 };
 size_t attention_workspace_bytes(const KvParams &c, const AttentionParams &a);
 int launch_attention(const KvParams &c, const AttentionParams &a, void *workspace, size_t workspace_bytes, hipStream_t s);
