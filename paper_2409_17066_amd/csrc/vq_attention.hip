@@ -95,20 +95,23 @@ __global__ __launch_bounds__(64) void attention_wave_kernel(const KvParams c, co
 
 namespace {
 
-// How a call is taken: `tile_rows` rows of a key head to a workgroup (0: the wave kernel), the keys in up to `parts` parts.
+// How a call is taken: `tile_rows` rows of a key head to a workgroup (0: the wave kernel), by the prompt or the decode kernel, the keys in up to `parts` parts.
 struct Plan {
   int tile_rows, parts;
+  bool prompt;
   size_t o_bytes, ml_bytes;
 };
 
 Plan plan_of(const KvParams &c, const AttentionParams &a) {
-  Plan p{0, 1, 0, 0};
+  Plan p{0, 1, false, 0, 0};
   if (c.head_dim != 64 && c.head_dim != 128) return p;
   const long long rows = (long long)c.max_new * a.group;
-  p.tile_rows = attention_decode_rows(c, a);
+  p.prompt = rows > 64;
+  p.tile_rows = p.prompt ? attention_prompt_rows() : attention_decode_rows(c, a);
   const long long seen = a.window > 0 ? std::min<long long>(c.max_length, (long long)a.window + a.sinks + p.tile_rows / a.group + 64) : c.max_length;
   const long long chunks = (seen + 63) / 64, groups = (long long)c.n_seqs * c.kv_heads * ((rows + p.tile_rows - 1) / p.tile_rows);
-  const long long wanted = std::min((long long)cu_count() / groups, chunks / 16);
+  // Parts until there is a workgroup to a compute unit (of the prompt kernel two), of two runs at least: a second launch costs about 4 us.
+  const long long wanted = std::min((p.prompt ? 2LL : 1LL) * cu_count() / groups, chunks / (2 * RUN));
   p.parts = (int)std::max(1LL, std::min(wanted, 64LL));
   if (p.parts > 1) {
     p.o_bytes = (size_t)c.n_seqs * c.kv_heads * p.parts * rows * c.head_dim * 4;
@@ -130,7 +133,7 @@ int launch_attention(const KvParams &c, const AttentionParams &a, void *workspac
     const bool room = p.parts > 1 && workspace_bytes >= p.o_bytes + p.ml_bytes;
     float *o = static_cast<float *>(workspace);
     const Split split{room ? p.parts : 1, o, room ? o + p.o_bytes / 4 : nullptr};
-    const int rc = launch_attention_decode(c, a, split, s);
+    const int rc = p.prompt ? launch_attention_prompt(c, a, split, s) : launch_attention_decode(c, a, split, s);
     return rc != VQ_OK || !room ? rc : launch_attention_join(c, a, split, p.tile_rows, s);
   }
   const long long blocks = (long long)c.n_seqs * c.max_new * a.q_heads;

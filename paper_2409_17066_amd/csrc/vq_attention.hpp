@@ -6,6 +6,7 @@ namespace vq {
 
 // How a sequence's keys are cut into parts: part p takes every `parts`-th run of eight chunks of 64 keys from run p on, so that what a workgroup looks at
 // first does not depend on the sequence's length.
+constexpr int RUN = 8;
 struct Split {
   int parts;
   float *o, *ml;               // partial outputs [seq][kv head][part][row][head_dim], maxima and sums [seq][kv head][part][row][2]
@@ -14,6 +15,8 @@ struct Split {
 // Rows of a key head to a workgroup of launch_attention_decode.
 int attention_decode_rows(const KvParams &c, const AttentionParams &a);
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
+int attention_prompt_rows();
+int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
 
 #ifdef __HIPCC__
@@ -36,7 +39,6 @@ __device__ __forceinline__ Span span_of(const AttentionParams &a, const Sequence
   v.chunks = v.end > 0 ? v.sink_chunks + max(((v.end + 63) >> 6) - v.first, 0) : 0;
   return v;
 }
-constexpr int RUN = 8;
 // Parts that have chunks, one at least.
 __device__ __forceinline__ int parts_of(const Split &s, int chunks) { return max(min(s.parts, (chunks + RUN - 1) / RUN), 1); }
 

@@ -1,0 +1,279 @@
+// Attention of many rows a key head (a prompt, or a chunk of one) over a paged cache: the prompt path.
+//
+// The matrix cores bound it, and the vector ALUs' softmax beside them.  Four waves of a workgroup take 32 rows each, two workgroups share a compute
+// unit.  Chunks of 64 keys pass through LDS as binary16 numbers, in two buffers: the next chunk's words are loaded before a chunk is computed and are converted and
+// stored behind it.  Scores come transposed, S^T = K Q^T (v_mfma_f32_32x32x16_f16): a lane holds sixteen keys a tile of one row, so that a row's maximum is
+// one exchange between two lanes, and the running maximum scales registers of the same lane.  Rows of a key tile are stored in an order that makes a lane's scores those of
+// sixteen consecutive keys, eight of which are what the lane has to give as operand B of O^T = V^T P^T: the probabilities never leave their registers.
+#include "vq_attention.hpp"
+
+namespace vq {
+
+namespace {
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = 32 * WAVES;
+typedef float float16v __attribute__((ext_vector_type(16)));
+struct Sixteen {
+  float f[16];
+};
+
+// Row of LDS for key (of 64): within 32 keys, key 16 h + 4 a + i is row 8 a + 4 h + i.
+__device__ __forceinline__ int row_of_key(int key) { return (key & 32) | ((key & 12) << 1) | ((key & 16) >> 2) | (key & 3); }
+
+template <bool E4M3, int D>
+__global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int zigzag) {
+  constexpr int BYTES = E4M3 ? 1 : 2;
+  constexpr int KU = D * BYTES / 16, VU = 64 * BYTES / 16;        // 16-byte words of a key, and of an element's 64 keys
+  constexpr int REPS = 64 * KU / THREADS, SLOTS = D / 8;          // words a thread brings; 16-byte slots of a key in LDS
+  constexpr int K_BYTES = 64 * D * 2, BUFFER = 2 * K_BYTES;
+  constexpr int STEPS = D / 16, DT = D / 32;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  int *there = reinterpret_cast<int *>(lds + 2 * BUFFER);          // [2][4]: whether each sixteen keys of a buffer have a page
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
+
+  // The workgroups of a sequence's key head go to one XCD (where their number is a multiple of eight), the longest first, or, where all
+  // are resident at once, so that the two of a compute unit have equal work together.
+  const int pairs = c.n_seqs * c.kv_heads, pair = (int)(blockIdx.x % pairs);
+  const int rest = (int)(blockIdx.x / pairs), part = rest % split.parts, rank = rest / split.parts, longer = (tiles + 1) / 2;
+  const int tile = !zigzag || rank < longer ? tiles - 1 - rank : rank - longer;
+  const int b = pair / c.kv_heads, kv_head = pair - b * c.kv_heads;
+  const Sequence s = sequence(c, b);
+  const int rows = s.rows * a.group, row0 = tile * ROWS;
+  if (row0 >= rows) return;
+  const Span span = span_of(a, s, row0, ROWS);
+  // chunks of this part: runs of RUN, every split.parts-th
+  const int begin = part * RUN;
+  if (part > 0 && begin >= span.chunks) return;
+  const int stride = split.parts * RUN;
+  auto chunk_at = [&](int i) { return span.chunk(begin + (i / RUN) * stride + i % RUN); };
+  int count = 0;
+  if (begin < span.chunks) {
+    const int runs = (span.chunks - begin + stride - 1) / stride, last = span.chunks - begin - (runs - 1) * stride;
+    count = (runs - 1) * RUN + min(last, RUN);
+  }
+
+  // this wave's rows
+  const int wave_row = row0 + wave * 32;
+  const bool has_rows = wave_row < rows;
+  const int row = min(wave_row + n, rows - 1), token = token_of(a, row), place = s.first + token;
+  const int place_min = s.first + token_of(a, min(wave_row, rows - 1)), place_max = s.first + token_of(a, min(wave_row + 31, rows - 1));
+  half8v q[STEPS];
+  {
+    const __half *x = a.q + (s.row0 + token) * a.ldq + ((long long)kv_head * a.group + row - token * a.group) * D + h * 8;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) q[i] = __builtin_bit_cast(half8v, (uint4v)*reinterpret_cast<const uint4b *>(x + i * 16));
+  }
+  float m = -__builtin_inff(), l = 0.f;
+  float16v o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) o[dt] = float16v{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+  const int shift = c.page_shift, mask = (1 << shift) - 1;
+  const int k_key = tid / KU, k_piece = tid % KU, v_d = tid / VU, v_piece = tid % VU, v_key = v_piece * (16 / BYTES);
+  constexpr int K_STEP = THREADS / KU, V_STEP = THREADS / VU;       // keys and elements from one word of a thread to its next
+  uint4v kw[REPS], vw[REPS];
+  float ks[REPS], vs = 1.f;
+  int k_entry[REPS], v_entry;
+  bool v_there = false;
+  auto entry = [&](int of) { return of >> shift < c.table_pages ? c.page_table[b * c.table_stride + (of >> shift)] : -1; };
+  auto entries = [&](int i) {
+    const int j0 = chunk_at(i) * 64;
+#pragma unroll
+    for (int r = 0; r < REPS; ++r) k_entry[r] = entry(j0 + k_key + r * K_STEP);
+    v_entry = entry(j0 + v_key);
+  };
+  // page of a place some row looks at, else page 0, whose contents are not used (nor its scale: it may be anything)
+  auto page_at = [&](int of, int entry, bool &is) {
+    of &= ~15;
+    is = (unsigned)entry < (unsigned)c.n_pages && of < span.end && (of + 15 >= span.low || of < a.sinks);
+    return is ? entry : 0;
+  };
+  auto load = [&](int i) {
+    const int j0 = chunk_at(i) * 64;
+#pragma unroll
+    for (int r = 0; r < REPS; ++r) {
+      const int j = j0 + k_key + r * K_STEP;
+      bool is;
+      const int page = page_at(j, k_entry[r], is);
+      kw[r] = *reinterpret_cast<const uint4v *>(c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask)) * (D * BYTES) + k_piece * 16);
+      ks[r] = E4M3 && is ? c.k_scales[(long long)page * c.kv_heads + kv_head] : 1.f;
+    }
+    const int j = j0 + v_key, page = page_at(j, v_entry, v_there);
+    const unsigned char *from = c.v_pages + page * c.v_page_bytes + ((((long long)kv_head * D + v_d) << shift) + (j & mask)) * BYTES;
+#pragma unroll
+    for (int r = 0; r < REPS; ++r) vw[r] = *reinterpret_cast<const uint4v *>(from + ((long long)(r * V_STEP * BYTES) << shift));
+    vs = E4M3 && v_there ? c.v_scales[(long long)page * c.kv_heads + kv_head] : 1.f;
+  };
+  auto slot_k = [&](int key, int slot) {
+    const int r = row_of_key(key);
+    return (r * SLOTS + (slot ^ (SLOTS == 16 ? r & 15 : (r >> 1) & 7))) * 16;
+  };
+  auto slot_v = [&](int d, int slot) { return K_BYTES + (d * 8 + (slot ^ ((d >> 1) & 7))) * 16; };
+  auto store = [&](int i) {
+    unsigned char *buffer = lds + (i & 1) * BUFFER;
+    const int j0 = chunk_at(i) * 64;
+    if (j0 + 64 > span.end || j0 < span.low || !v_there) {          // values that no row looks at may be anything: cleared
+      unsigned keep[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        keep[w] = 0;
+#pragma unroll
+        for (int r = 0; r < 4 / BYTES; ++r) {
+          const int j = j0 + v_key + w * (4 / BYTES) + r;
+          if (v_there && j < span.end && (j >= span.low || j < a.sinks)) keep[w] |= (E4M3 ? 0xffu : 0xffffu) << (8 * BYTES * r);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < REPS; ++r) vw[r] &= uint4v{keep[0], keep[1], keep[2], keep[3]};
+    }
+#pragma unroll
+    for (int r = 0; r < REPS; ++r) {
+      const int key = k_key + r * K_STEP, d = v_d + r * V_STEP;
+      if constexpr (E4M3) {
+        *reinterpret_cast<half8v *>(buffer + slot_k(key, 2 * k_piece)) = halves_of_e4m3(kw[r].x, kw[r].y, ks[r]);
+        *reinterpret_cast<half8v *>(buffer + slot_k(key, 2 * k_piece + 1)) = halves_of_e4m3(kw[r].z, kw[r].w, ks[r]);
+        *reinterpret_cast<half8v *>(buffer + slot_v(d, 2 * v_piece)) = halves_of_e4m3(vw[r].x, vw[r].y, vs);
+        *reinterpret_cast<half8v *>(buffer + slot_v(d, 2 * v_piece + 1)) = halves_of_e4m3(vw[r].z, vw[r].w, vs);
+      } else {
+        *reinterpret_cast<uint4v *>(buffer + slot_k(key, k_piece)) = kw[r];
+        *reinterpret_cast<uint4v *>(buffer + slot_v(d, v_piece)) = vw[r];
+      }
+    }
+    if (tid < VU && (E4M3 || !(tid & 1))) there[(i & 1) * 4 + (E4M3 ? tid : tid >> 1)] = v_there;
+  };
+
+  if (count > 0) {
+    entries(0);
+    load(0);
+    if (count > 1) entries(1);
+    store(0);
+  }
+  __syncthreads();
+  for (int i = 0; i < count; ++i) {
+    if (i + 1 < count) load(i + 1);
+    if (i + 2 < count) entries(i + 2);
+    const int j0 = chunk_at(i) * 64;
+    const unsigned char *buffer = lds + (i & 1) * BUFFER;
+    const bool looks = has_rows && j0 <= place_max && (a.window <= 0 || j0 + 63 > place_min - a.window || j0 < a.sinks);
+    if (looks) {
+      Sixteen sc[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float16v x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+          const int r = 32 * t + n, slot = (2 * st + h) ^ (SLOTS == 16 ? n & 15 : (n >> 1) & 7);
+          const half8v f = *reinterpret_cast<const half8v *>(buffer + (r * SLOTS + slot) * 16);
+          x = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[st], x, 0, 0, 0);
+        }
+        sc[t] = __builtin_bit_cast(Sixteen, x);
+      }
+      const int4 is = *reinterpret_cast<const int4 *>(there + (i & 1) * 4);
+      const bool all = is.x && is.y && is.z && is.w;
+      if (!all || j0 + 63 > place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= place_max - a.window)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bool page = (t ? (h ? is.w : is.z) : (h ? is.y : is.x)) != 0;
+          const int base = j0 + 32 * t + 16 * h;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = base + r;
+            const bool sees = page && j <= place && j < s.end && (a.window <= 0 || j > place - a.window || j < a.sinks);
+            sc[t].f[r] = sees ? sc[t].f[r] : -__builtin_inff();
+          }
+        }
+      }
+      float top = fmaxf(sc[0].f[0], sc[1].f[0]);
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, sc[0].f[r]), sc[1].f[r]);
+      float low, high;
+      across_halves(top, low, high);
+      const float now = fmaxf(low, high) * a.scale;
+      // The base of the exponents follows the maximum only when it has grown by 2^8: binary16 holds what lies in between.
+      if (__ballot(now > m + 8.f)) {
+        const float next = fmaxf(m, now), again = __builtin_amdgcn_exp2f(m - base_of(next));
+        l *= again;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] *= again;
+        m = next;
+      }
+      const float base = base_of(m);
+      half8v p[2][2];
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float e[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) e[r] = __builtin_amdgcn_exp2f(__fmaf_rn(sc[t].f[8 * u + r], a.scale, -base));
+          sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+          p[t][u] = half8v{(_Float16)e[0], (_Float16)e[1], (_Float16)e[2], (_Float16)e[3], (_Float16)e[4], (_Float16)e[5], (_Float16)e[6], (_Float16)e[7]};
+        }
+      l += sum;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const int slot = (4 * t + 2 * h + u) ^ ((n >> 1) & 7);
+            const half8v f = *reinterpret_cast<const half8v *>(buffer + K_BYTES + ((32 * dt + n) * 8 + slot) * 16);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[t][u], o[dt], 0, 0, 0);
+          }
+    }
+    if (i + 1 < count) store(i + 1);
+    __syncthreads();
+  }
+
+  float low, high;
+  across_halves(l, low, high);
+  const float total = low + high;
+  if (wave_row + n >= rows) return;
+  const bool whole = parts_of(split, span.chunks) == 1;
+  const float inverse = inverse_of(total);
+  const int head = kv_head * a.group + row - token * a.group;
+  const long long to = (((long long)b * c.kv_heads + kv_head) * split.parts + part) * ((long long)c.max_new * a.group) + row;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    const Sixteen x = __builtin_bit_cast(Sixteen, o[dt]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int d = 32 * dt + 8 * w + 4 * h;
+      const float y0 = x.f[4 * w], y1 = x.f[4 * w + 1], y2 = x.f[4 * w + 2], y3 = x.f[4 * w + 3];
+      if (whole) {
+        typedef _Float16 half4b __attribute__((ext_vector_type(4), aligned(2)));
+        *reinterpret_cast<half4b *>(a.out + (s.row0 + token) * a.ldo + (long long)head * D + d) =
+            half4b{(_Float16)(y0 * inverse), (_Float16)(y1 * inverse), (_Float16)(y2 * inverse), (_Float16)(y3 * inverse)};
+      } else {
+        *reinterpret_cast<float4v *>(split.o + to * D + d) = float4v{y0, y1, y2, y3};
+      }
+    }
+  }
+  if (h == 0) {
+    if (!whole) *reinterpret_cast<float2v *>(split.ml + to * 2) = float2v{m, total};
+    else if (a.lse) a.lse[(long long)(s.row0 + token) * a.q_heads + head] = lse_of(m, total);
+  }
+}
+
+template <bool E4M3, int D>
+int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  const int tiles = (c.max_new * a.group + ROWS - 1) / ROWS;
+  const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
+  if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
+  VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D>));
+  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 32, stream, c, a, s, tiles,
+                     blocks <= 2 * cu_count());
+  return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
+}
+
+}  // namespace
+
+int attention_prompt_rows() { return ROWS; }
+
+int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  if (c.head_dim == 64) return c.e4m3 ? launch<true, 64>(c, a, s, stream) : launch<false, 64>(c, a, s, stream);
+  return c.e4m3 ? launch<true, 128>(c, a, s, stream) : launch<false, 128>(c, a, s, stream);
+}
+
+}  // namespace vq
