@@ -74,6 +74,18 @@ __device__ __forceinline__ half8v halves_of_e4m3(unsigned a, unsigned b, float s
   return half8v{w.x, w.y, x.x, x.y, y.x, y.y, z.x, z.y};
 }
 
+// Which of the places [base, base + 16) a token at `place` sees, as bits.
+__device__ __forceinline__ unsigned seen_of(const AttentionParams &a, const Sequence &s, int place, int base) {
+  auto below = [&](int limit) { return (1u << min(max(limit - base, 0), 16)) - 1u; };
+  const unsigned most = below(min(place + 1, s.end));
+  return a.window > 0 ? most & (~below(place - a.window + 1) | below(a.sinks)) : most;
+}
+// x where bit r of `seen` is set, else minus infinity.
+__device__ __forceinline__ float where_seen(unsigned seen, int r, float x) {
+  const unsigned all = (unsigned)((int)(seen << (31 - r)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & all) | (0xff800000u & ~all));
+}
+
 // A finite stand-in for the maximum of a row that has seen nothing yet.
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
 // One over a softmax's sum; zero for a row that sees nothing; what is not a number stays none.

@@ -133,18 +133,14 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
     const bool all_there = __ballot(!v_there) == 0;
     if (!all_there || j0 + 63 > span.place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= span.place_max - a.window)) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < RT; ++rt) {
+        const unsigned seen = v_there ? seen_of(a, s, place[rt], j0 + 16 * g) : 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          float x[4] = {sc[rt][t].x, sc[rt][t].y, sc[rt][t].z, sc[rt][t].w};
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int j = j0 + 16 * g + 4 * t + r;
-            const bool sees = v_there && j <= place[rt] && j < s.end && (a.window <= 0 || j > place[rt] - a.window || j < a.sinks);
-            x[r] = sees ? x[r] : -__builtin_inff();
-          }
-          sc[rt][t] = float4v{x[0], x[1], x[2], x[3]};
+          const float4v x = sc[rt][t];
+          sc[rt][t] = float4v{where_seen(seen, 4 * t, x.x), where_seen(seen, 4 * t + 1, x.y), where_seen(seen, 4 * t + 2, x.z), where_seen(seen, 4 * t + 3, x.w)};
         }
+      }
       unsigned keep[4 * VL];
 #pragma unroll
       for (int w = 0; w < 4 * VL; ++w) {
@@ -165,15 +161,16 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
     for (int rt = 0; rt < RT; ++rt) {
       float top = fmaxf(fmaxf(fmaxf(sc[rt][0].x, sc[rt][0].y), fmaxf(sc[rt][0].z, sc[rt][0].w)), fmaxf(fmaxf(sc[rt][1].x, sc[rt][1].y), fmaxf(sc[rt][1].z, sc[rt][1].w)));
       top = fmaxf(top, fmaxf(fmaxf(fmaxf(sc[rt][2].x, sc[rt][2].y), fmaxf(sc[rt][2].z, sc[rt][2].w)), fmaxf(fmaxf(sc[rt][3].x, sc[rt][3].y), fmaxf(sc[rt][3].z, sc[rt][3].w))));
-      const float now = fmaxf(m[rt], rows_max(top) * a.scale);
-      const float base = base_of(now);
-      if (__ballot(now > m[rt])) {
-        const float again = __builtin_amdgcn_exp2f(m[rt] - base);
+      // The base of the exponents follows the maximum only when it has grown by 2^8: binary16 holds what lies in between.
+      const float now = rows_max(top) * a.scale;
+      if (__ballot(now > m[rt] + 8.f)) {
+        const float next = fmaxf(m[rt], now), again = __builtin_amdgcn_exp2f(m[rt] - base_of(next));
         l[rt] *= again;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= again;
-        m[rt] = now;
+        m[rt] = next;
       }
+      const float base = base_of(m[rt]);
       float sum = 0.f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {

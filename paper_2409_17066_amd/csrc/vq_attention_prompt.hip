@@ -6,6 +6,7 @@
 // one exchange between two lanes, and the running maximum scales registers of the same lane.  Rows of a key tile are stored in an order that makes a lane's scores those of
 // sixteen consecutive keys, eight of which are what the lane has to give as operand B of O^T = V^T P^T: the probabilities never leave their registers.
 #include "vq_attention.hpp"
+#include <type_traits>
 
 namespace vq {
 
@@ -20,6 +21,18 @@ struct Sixteen {
 // Row of LDS for key (of 64): within 32 keys, key 16 h + 4 a + i is row 8 a + 4 h + i.
 __device__ __forceinline__ int row_of_key(int key) { return (key & 32) | ((key & 12) << 1) | ((key & 16) >> 2) | (key & 3); }
 
+// The sequence that has `n` longer ones (of equal ones the first comes first; as they are numbered, where there are more than a wave has lanes).
+__device__ __forceinline__ int nth_longest(const KvParams &c, int n, int lane) {
+  if (c.n_seqs == 1 || c.n_seqs > 64) return n;
+  const int mine = lane < c.n_seqs ? max(c.lengths[lane], 0) : -1;
+  int before = 0;
+  for (int j = 0; j < c.n_seqs; ++j) {
+    const int other = __builtin_amdgcn_readlane(mine, j);
+    before += other > mine || (other == mine && j < lane);
+  }
+  return (int)__builtin_ctzll(__ballot(lane < c.n_seqs && before == n));
+}
+
 template <bool E4M3, int D>
 __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int zigzag) {
   constexpr int BYTES = E4M3 ? 1 : 2;
@@ -28,15 +41,23 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   constexpr int K_BYTES = 64 * D * 2, BUFFER = 2 * K_BYTES;
   constexpr int STEPS = D / 16, DT = D / 32;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  int *there = reinterpret_cast<int *>(lds + 2 * BUFFER);          // [2][4]: whether each sixteen keys of a buffer have a page
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
+  unsigned char *there = lds + 2 * BUFFER;                         // [2][4]: whether each sixteen keys of a buffer have a page
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
 
-  // The workgroups of a sequence's key head go to one XCD (where their number is a multiple of eight), the longest first, or, where all
-  // are resident at once, so that the two of a compute unit have equal work together.
-  const int pairs = c.n_seqs * c.kv_heads, pair = (int)(blockIdx.x % pairs);
-  const int rest = (int)(blockIdx.x / pairs), part = rest % split.parts, rank = rest / split.parts, longer = (tiles + 1) / 2;
-  const int tile = !zigzag || rank < longer ? tiles - 1 - rank : rank - longer;
-  const int b = pair / c.kv_heads, kv_head = pair - b * c.kv_heads;
+  // Long sequences first and of each the rows that see most, so that short work fills the end; where all workgroups are resident at once, so that
+  // the two of a compute unit have equal work together.  Those of a key head go to one XCD where the heads are a multiple of eight.
+  const int kv_head = (int)(blockIdx.x % c.kv_heads), rest = (int)(blockIdx.x / c.kv_heads);
+  int b, part, rank;
+  if (zigzag) {
+    b = rest % c.n_seqs;
+    part = rest / c.n_seqs % split.parts;
+    rank = rest / c.n_seqs / split.parts;
+  } else {
+    part = rest % split.parts;
+    rank = rest / split.parts % tiles;
+    b = nth_longest(c, rest / split.parts / tiles, lane);
+  }
+  const int longer = (tiles + 1) / 2, tile = !zigzag || rank < longer ? tiles - 1 - rank : rank - longer;
   const Sequence s = sequence(c, b);
   const int rows = s.rows * a.group, row0 = tile * ROWS;
   if (row0 >= rows) return;
@@ -68,49 +89,69 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = float16v{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
-  const int shift = c.page_shift, mask = (1 << shift) - 1;
-  const int k_key = tid / KU, k_piece = tid % KU, v_d = tid / VU, v_piece = tid % VU, v_key = v_piece * (16 / BYTES);
+  // What a thread brings of a chunk: REPS words of keys and of values.  All lanes of a wave bring words of one page, so that its number, address and scale
+  // are scalars: of the keys eight tokens (four, sixteen) of a wave are adjacent, of the values a wave takes sixteen tokens, or, where a page
+  // holds a whole chunk, the workgroup all of them, so that adjacent lanes read adjacent words.
+  const int shift = c.page_shift;
+  const bool wide = shift >= 6;
   constexpr int K_STEP = THREADS / KU, V_STEP = THREADS / VU;       // keys and elements from one word of a thread to its next
+  const int k_key = tid / KU, k_piece = tid % KU, wave_key = wave * (64 / KU);
+  const int v_piece = wide ? tid % VU : wave * BYTES + lane % BYTES, v_d = wide ? tid / VU : lane / BYTES, v_key = v_piece * (16 / BYTES);
+  const unsigned k_offset = (unsigned)((k_key - wave_key) * (D * BYTES) + k_piece * 16);
+  const unsigned v_offset = (unsigned)((v_d << shift) * BYTES + (wide ? v_piece * 16 : lane % BYTES * 16)), v_step = (unsigned)(V_STEP * BYTES) << shift;
   uint4v kw[REPS], vw[REPS];
   float ks[REPS], vs = 1.f;
-  int k_entry[REPS], v_entry;
+  int k_entry[REPS], v_entry = -1;
   bool v_there = false;
-  auto entry = [&](int of) { return of >> shift < c.table_pages ? c.page_table[b * c.table_stride + (of >> shift)] : -1; };
+  typedef const __attribute__((address_space(4))) int *ScalarInts;
+  typedef const __attribute__((address_space(4))) float *ScalarFloats;
+  const ScalarInts table = (ScalarInts)(c.page_table + b * c.table_stride);
+  auto entry = [&](int of) { return of >> shift < c.table_pages ? table[of >> shift] : -1; };
   auto entries = [&](int i) {
     const int j0 = chunk_at(i) * 64;
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) k_entry[r] = entry(j0 + k_key + r * K_STEP);
-    v_entry = entry(j0 + v_key);
+    for (int r = 0; r < REPS; ++r) k_entry[r] = entry(j0 + wave_key + r * K_STEP);
+    v_entry = entry(j0 + (wide ? 0 : wave * 16));
   };
-  // page of a place some row looks at, else page 0, whose contents are not used (nor its scale: it may be anything)
+  // page of places [of, of + 16), where some row looks at one of its tokens of this chunk, else page 0, whose contents are not used (nor its scale: it may be anything)
   auto page_at = [&](int of, int entry, bool &is) {
-    of &= ~15;
-    is = (unsigned)entry < (unsigned)c.n_pages && of < span.end && (of + 15 >= span.low || of < a.sinks);
+    is = (unsigned)entry < (unsigned)c.n_pages && (wide || (of < span.end && (of + 15 >= span.low || of < a.sinks)));
     return is ? entry : 0;
   };
+  auto scale_of = [&](const float *scales, int page) { return ((ScalarFloats)scales)[(long long)page * c.kv_heads + kv_head]; };
   auto load = [&](int i) {
-    const int j0 = chunk_at(i) * 64;
+    const int j0 = chunk_at(i) * 64, mask = (1 << shift) - 1;
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
-      const int j = j0 + k_key + r * K_STEP;
+      const int j = j0 + wave_key + r * K_STEP;
       bool is;
-      const int page = page_at(j, k_entry[r], is);
-      kw[r] = *reinterpret_cast<const uint4v *>(c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask)) * (D * BYTES) + k_piece * 16);
-      ks[r] = E4M3 && is ? c.k_scales[(long long)page * c.kv_heads + kv_head] : 1.f;
+      const int page = page_at(j & ~15, k_entry[r], is);
+      const unsigned char *from = c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask)) * (D * BYTES);
+      kw[r] = *reinterpret_cast<const uint4v *>(from + k_offset);
+      if (E4M3) {
+        const float x = scale_of(c.k_scales, page);
+        ks[r] = is ? x : 1.f;
+      }
     }
-    const int j = j0 + v_key, page = page_at(j, v_entry, v_there);
-    const unsigned char *from = c.v_pages + page * c.v_page_bytes + ((((long long)kv_head * D + v_d) << shift) + (j & mask)) * BYTES;
+    const int j = j0 + (wide ? 0 : wave * 16), page = page_at(j, v_entry, v_there);
+    const unsigned char *from = c.v_pages + page * c.v_page_bytes + ((((long long)kv_head * D) << shift) + (j & mask)) * BYTES;
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) vw[r] = *reinterpret_cast<const uint4v *>(from + ((long long)(r * V_STEP * BYTES) << shift));
-    vs = E4M3 && v_there ? c.v_scales[(long long)page * c.kv_heads + kv_head] : 1.f;
+    for (int r = 0; r < REPS; ++r) vw[r] = *reinterpret_cast<const uint4v *>(from + r * v_step + v_offset);
+    if (E4M3) {
+      const float x = scale_of(c.v_scales, page);
+      vs = v_there ? x : 1.f;
+    }
   };
+  using Zero = std::integral_constant<int, 0>;
+  using One = std::integral_constant<int, 1>;
   auto slot_k = [&](int key, int slot) {
     const int r = row_of_key(key);
     return (r * SLOTS + (slot ^ (SLOTS == 16 ? r & 15 : (r >> 1) & 7))) * 16;
   };
   auto slot_v = [&](int d, int slot) { return K_BYTES + (d * 8 + (slot ^ ((d >> 1) & 7))) * 16; };
-  auto store = [&](int i) {
-    unsigned char *buffer = lds + (i & 1) * BUFFER;
+  auto store = [&](int i, auto into) {
+    constexpr int INTO = decltype(into)::value;
+    unsigned char *buffer = lds + INTO * BUFFER;
     const int j0 = chunk_at(i) * 64;
     if (j0 + 64 > span.end || j0 < span.low || !v_there) {          // values that no row looks at may be anything: cleared
       unsigned keep[4];
@@ -139,21 +180,25 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
         *reinterpret_cast<uint4v *>(buffer + slot_v(d, v_piece)) = vw[r];
       }
     }
-    if (tid < VU && (E4M3 || !(tid & 1))) there[(i & 1) * 4 + (E4M3 ? tid : tid >> 1)] = v_there;
+    if (lane == 0) there[INTO * 4 + wave] = v_there;
   };
 
   if (count > 0) {
     entries(0);
     load(0);
     if (count > 1) entries(1);
-    store(0);
+    store(0, Zero{});
   }
+  // (the queries have arrived here: a wait for them inside the loop would wait for the next chunk's loads too)
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) asm volatile("" : "+v"(q[i]));
   __syncthreads();
-  for (int i = 0; i < count; ++i) {
+  auto step = [&](int i, auto of) {                                // (the buffers take turns; a constant one makes their addresses immediates)
+    constexpr int OF = decltype(of)::value;
     if (i + 1 < count) load(i + 1);
     if (i + 2 < count) entries(i + 2);
     const int j0 = chunk_at(i) * 64;
-    const unsigned char *buffer = lds + (i & 1) * BUFFER;
+    const unsigned char *buffer = lds + OF * BUFFER;
     const bool looks = has_rows && j0 <= place_max && (a.window <= 0 || j0 + 63 > place_min - a.window || j0 < a.sinks);
     if (looks) {
       Sixteen sc[2];
@@ -168,19 +213,13 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
         }
         sc[t] = __builtin_bit_cast(Sixteen, x);
       }
-      const int4 is = *reinterpret_cast<const int4 *>(there + (i & 1) * 4);
-      const bool all = is.x && is.y && is.z && is.w;
-      if (!all || j0 + 63 > place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= place_max - a.window)) {
+      const unsigned is = (unsigned)__builtin_amdgcn_readfirstlane(*reinterpret_cast<const int *>(there + OF * 4));
+      if (is != 0x01010101u || j0 + 63 > place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= place_max - a.window)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const bool page = (t ? (h ? is.w : is.z) : (h ? is.y : is.x)) != 0;
-          const int base = j0 + 32 * t + 16 * h;
+          const unsigned seen = is >> (16 * t + 8 * h) & 1 ? seen_of(a, s, place, j0 + 32 * t + 16 * h) : 0;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = base + r;
-            const bool sees = page && j <= place && j < s.end && (a.window <= 0 || j > place - a.window || j < a.sinks);
-            sc[t].f[r] = sees ? sc[t].f[r] : -__builtin_inff();
-          }
+          for (int r = 0; r < 16; ++r) sc[t].f[r] = where_seen(seen, r, sc[t].f[r]);
         }
       }
       float top = fmaxf(sc[0].f[0], sc[1].f[0]);
@@ -222,8 +261,12 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
             o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[t][u], o[dt], 0, 0, 0);
           }
     }
-    if (i + 1 < count) store(i + 1);
+    if (i + 1 < count) store(i + 1, std::integral_constant<int, 1 - OF>{});
     __syncthreads();
+  };
+  for (int i = 0; i < count; i += 2) {
+    step(i, Zero{});
+    if (i + 1 < count) step(i + 1, One{});
   }
 
   float low, high;
@@ -262,7 +305,7 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
   const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
   if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
   VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D>));
-  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 32, stream, c, a, s, tiles,
+  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16, stream, c, a, s, tiles,
                      blocks <= 2 * cu_count());
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
