@@ -39,7 +39,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   constexpr int KU = D * BYTES / 16, VU = 64 * BYTES / 16;        // 16-byte words of a key, and of an element's 64 keys
   constexpr int REPS = 64 * KU / THREADS, SLOTS = D / 8;          // words a thread brings; 16-byte slots of a key in LDS
   constexpr int K_BYTES = 64 * D * 2, BUFFER = 2 * K_BYTES;
-  constexpr int STEPS = D / 16, DT = D / 32;
+  constexpr int STEPS = D / 16, DT = D / 32, AHEAD = 6;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *there = lds + 2 * BUFFER;                         // [2][4]: whether each sixteen keys of a buffer have a page
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
@@ -192,28 +192,53 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   // (the queries have arrived here: a wait for them inside the loop would wait for the next chunk's loads too)
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) asm volatile("" : "+v"(q[i]));
+  // Where this lane's operands lie in the first buffer; what else an address consists of is a constant.
+  auto lds_halves = [](unsigned at) { return *(const __attribute__((address_space(3))) half8v *)(size_t)at; };
+  const unsigned lds_at = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+  unsigned k_from[STEPS], v_from[4];
+#pragma unroll
+  for (int st = 0; st < STEPS; ++st) {
+    k_from[st] = lds_at + (n * SLOTS + ((2 * st + h) ^ (SLOTS == 16 ? n & 15 : (n >> 1) & 7))) * 16;
+    asm volatile("" : "+v"(k_from[st]));
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    v_from[u] = lds_at + K_BYTES + (n * 8 + ((4 * (u >> 1) + 2 * h + (u & 1)) ^ ((n >> 1) & 7))) * 16;
+    asm volatile("" : "+v"(v_from[u]));
+  }
   __syncthreads();
   auto step = [&](int i, auto of) {                                // (the buffers take turns; a constant one makes their addresses immediates)
     constexpr int OF = decltype(of)::value;
     if (i + 1 < count) load(i + 1);
     if (i + 2 < count) entries(i + 2);
     const int j0 = chunk_at(i) * 64;
-    const unsigned char *buffer = lds + OF * BUFFER;
     const bool looks = has_rows && j0 <= place_max && (a.window <= 0 || j0 + 63 > place_min - a.window || j0 < a.sinks);
     if (looks) {
       Sixteen sc[2];
+      const int pages = *(const __attribute__((address_space(3))) int *)(size_t)(lds_at + 2 * BUFFER + OF * 4);
+      __builtin_amdgcn_sched_barrier(0);                           // (in front of the operands: it is waited for alone)
+      // operands are read from LDS several products ahead
+      half8v f[2 * STEPS];
+#pragma unroll
+      for (int u = 0; u < 2 * STEPS; ++u) f[u] = lds_halves(k_from[u % STEPS] + OF * BUFFER + u / STEPS * 32 * SLOTS * 16);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         float16v x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          const int r = 32 * t + n, slot = (2 * st + h) ^ (SLOTS == 16 ? n & 15 : (n >> 1) & 7);
-          const half8v f = *reinterpret_cast<const half8v *>(buffer + (r * SLOTS + slot) * 16);
-          x = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[st], x, 0, 0, 0);
-        }
+        for (int st = 0; st < STEPS; ++st) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[t * STEPS + st], q[st], x, 0, 0, 0);
         sc[t] = __builtin_bit_cast(Sixteen, x);
       }
-      const unsigned is = (unsigned)__builtin_amdgcn_readfirstlane(*reinterpret_cast<const int *>(there + OF * 4));
+      half8v vf[4 * DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) vf[dt] = lds_halves(v_from[0] + OF * BUFFER + dt * 32 * 8 * 16);
+      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+      for (int u = 0; u < 2 * STEPS + DT - AHEAD; ++u) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, AHEAD - DT, 0);
+      const unsigned is = (unsigned)__builtin_amdgcn_readfirstlane(pages);
       if (is != 0x01010101u || j0 + 63 > place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= place_max - a.window)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -251,15 +276,15 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
         }
       l += sum;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int u = DT; u < 4 * DT; ++u) vf[u] = lds_halves(v_from[u / DT] + OF * BUFFER + u % DT * 32 * 8 * 16);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 4 * DT; ++u) o[u % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[u], p[u / DT / 2][u / DT % 2], o[u % DT], 0, 0, 0);
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const int slot = (4 * t + 2 * h + u) ^ ((n >> 1) & 7);
-            const half8v f = *reinterpret_cast<const half8v *>(buffer + K_BYTES + ((32 * dt + n) * 8 + slot) * 16);
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[t][u], o[dt], 0, 0, 0);
-          }
+      for (int u = 0; u < 3 * DT; ++u) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, DT, 0);
     }
     if (i + 1 < count) store(i + 1, std::integral_constant<int, 1 - OF>{});
     __syncthreads();
