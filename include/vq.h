@@ -314,7 +314,7 @@ typedef struct vq_kv_desc {
   int32_t table_pages;                     /* entries of a row of page_table                               */
   int32_t reserved;                        /* 0                                                            */
   void *k_pages, *v_pages;                 /* 16-byte aligned                                              */
-  int64_t k_page_stride, v_page_stride;    /* elements from page to page; a page's bytes are a multiple of 16 */
+  int64_t k_page_stride, v_page_stride;    /* elements from page to page: a multiple of 16 bytes below 4 GiB */
   float *k_scales, *v_scales;              /* [n_pages][kv_heads]; VQ_KV_E4M3 only                         */
   const int32_t *page_table; int64_t table_stride;   /* [n_seqs][table_stride]                             */
   const int32_t *lengths;                  /* [n_seqs]                                                     */

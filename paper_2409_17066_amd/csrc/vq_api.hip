@@ -382,7 +382,7 @@ int make_kv_params(const vq_kv_desc *d, KvParams *p) {
   if (d->table_pages < 0 || d->max_length > (long long)d->table_pages * d->page_tokens || d->table_stride < d->table_pages) return VQ_ERR_SHAPE;
   if (!d->starts && (d->n_tokens % d->n_seqs != 0 || d->max_new < d->n_tokens / d->n_seqs)) return VQ_ERR_SHAPE;
   if (!d->k_pages || !d->v_pages || !d->lengths || (!d->page_table && d->table_pages) || (e4m3 && (!d->k_scales || !d->v_scales))) return VQ_ERR_NULL;
-  const long long page = (long long)d->kv_heads * d->page_tokens * d->head_dim, element = e4m3 ? 1 : 2, most = 0x7fffffffffffffffll / 4;
+  const long long page = (long long)d->kv_heads * d->page_tokens * d->head_dim, element = e4m3 ? 1 : 2, most = (1ll << 32) / element - 1;
   if (d->k_page_stride < page || d->v_page_stride < page || d->k_page_stride > most || d->v_page_stride > most) return VQ_ERR_SHAPE;
   if (!aligned(d->k_pages, 16) || !aligned(d->v_pages, 16) || d->k_page_stride * element % 16 || d->v_page_stride * element % 16) return VQ_ERR_ALIGNMENT;
   if (!aligned(d->lengths, 4) || !aligned(d->page_table, 4) || !aligned(d->starts, 4) || (e4m3 && (!aligned(d->k_scales, 4) || !aligned(d->v_scales, 4))))

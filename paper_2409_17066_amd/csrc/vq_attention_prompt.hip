@@ -63,15 +63,10 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   if (row0 >= rows) return;
   const Span span = span_of(a, s, row0, ROWS);
   // chunks of this part: runs of RUN, every split.parts-th
-  const int begin = part * RUN;
-  if (part > 0 && begin >= span.chunks) return;
-  const int stride = split.parts * RUN;
-  auto chunk_at = [&](int i) { return span.chunk(begin + (i / RUN) * stride + i % RUN); };
-  int count = 0;
-  if (begin < span.chunks) {
-    const int runs = (span.chunks - begin + stride - 1) / stride, last = span.chunks - begin - (runs - 1) * stride;
-    count = (runs - 1) * RUN + min(last, RUN);
-  }
+  if (part > 0 && part * RUN >= span.chunks) return;
+  const int jump = (split.parts - 1) * RUN;
+  auto following = [&](int chunk) { return chunk + 1 + ((chunk + 1) % RUN == 0 ? jump : 0); };
+  auto first_of = [&](int chunk) { return (chunk < span.sink_chunks ? chunk : chunk + span.first - span.sink_chunks) * 64; };
 
   // this wave's rows
   const int wave_row = row0 + wave * 32;
@@ -106,41 +101,39 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   typedef const __attribute__((address_space(4))) int *ScalarInts;
   typedef const __attribute__((address_space(4))) float *ScalarFloats;
   const ScalarInts table = (ScalarInts)(c.page_table + b * c.table_stride);
-  auto entry = [&](int of) { return of >> shift < c.table_pages ? table[of >> shift] : -1; };
-  auto entries = [&](int i) {
-    const int j0 = chunk_at(i) * 64;
+  const int last_entry = c.table_pages - 1, mask = (1 << shift) - 1;
+  int k_place[REPS];                                                // of this wave's keys in a chunk
+  unsigned k_in_page[REPS];
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) k_entry[r] = entry(j0 + wave_key + r * K_STEP);
-    v_entry = entry(j0 + (wide ? 0 : wave * 16));
+  for (int r = 0; r < REPS; ++r) {
+    k_place[r] = wave_key + r * K_STEP;
+    k_in_page[r] = (unsigned)(k_place[r] & mask) * (D * BYTES);
+  }
+  const int v_place = wide ? 0 : wave * 16;
+  const unsigned v_in_page = (unsigned)(v_place & mask) * BYTES;
+  const unsigned char *k_head = c.k_pages + ((long long)kv_head << shift) * (D * BYTES), *v_head = c.v_pages + (((long long)kv_head * D) << shift) * BYTES;
+  const ScalarFloats k_scales = (ScalarFloats)c.k_scales + kv_head, v_scales = (ScalarFloats)c.v_scales + kv_head;
+  // Entries of the page table; past its end, where no key is, the last one's.
+  auto entries = [&](int j0) {
+#pragma unroll
+    for (int r = 0; r < REPS; ++r) k_entry[r] = table[min((j0 + k_place[r]) >> shift, last_entry)];
+    v_entry = table[min((j0 + v_place) >> shift, last_entry)];
   };
-  // page of places [of, of + 16), where some row looks at one of its tokens of this chunk, else page 0, whose contents are not used (nor its scale: it may be anything)
-  auto page_at = [&](int of, int entry, bool &is) {
-    is = (unsigned)entry < (unsigned)c.n_pages && (wide || (of < span.end && (of + 15 >= span.low || of < a.sinks)));
-    return is ? entry : 0;
-  };
-  auto scale_of = [&](const float *scales, int page) { return ((ScalarFloats)scales)[(long long)page * c.kv_heads + kv_head]; };
-  auto load = [&](int i) {
-    const int j0 = chunk_at(i) * 64, mask = (1 << shift) - 1;
+  // (instead of a page that is not there page 0 is read, and what comes of it is not used)
+  auto load = [&](int j0) {
+    const unsigned in_page = (unsigned)(j0 & mask);
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
-      const int j = j0 + wave_key + r * K_STEP;
-      bool is;
-      const int page = page_at(j & ~15, k_entry[r], is);
-      const unsigned char *from = c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask)) * (D * BYTES);
-      kw[r] = *reinterpret_cast<const uint4v *>(from + k_offset);
-      if (E4M3) {
-        const float x = scale_of(c.k_scales, page);
-        ks[r] = is ? x : 1.f;
-      }
+      const unsigned page = (unsigned)k_entry[r] < (unsigned)c.n_pages ? (unsigned)k_entry[r] : 0u;
+      kw[r] = *reinterpret_cast<const uint4v *>(k_head + (unsigned long long)page * (unsigned)c.k_page_bytes + (in_page * (D * BYTES) + k_in_page[r]) + k_offset);
+      if (E4M3) ks[r] = k_scales[(unsigned long long)page * (unsigned)c.kv_heads];
     }
-    const int j = j0 + (wide ? 0 : wave * 16), page = page_at(j, v_entry, v_there);
-    const unsigned char *from = c.v_pages + page * c.v_page_bytes + ((((long long)kv_head * D) << shift) + (j & mask)) * BYTES;
+    v_there = (unsigned)v_entry < (unsigned)c.n_pages;
+    const unsigned page = v_there ? (unsigned)v_entry : 0u;
+    const unsigned char *from = v_head + (unsigned long long)page * (unsigned)c.v_page_bytes + (in_page * BYTES + v_in_page);
 #pragma unroll
     for (int r = 0; r < REPS; ++r) vw[r] = *reinterpret_cast<const uint4v *>(from + r * v_step + v_offset);
-    if (E4M3) {
-      const float x = scale_of(c.v_scales, page);
-      vs = v_there ? x : 1.f;
-    }
+    if (E4M3) vs = v_scales[(unsigned long long)page * (unsigned)c.kv_heads];
   };
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
@@ -149,10 +142,9 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
     return (r * SLOTS + (slot ^ (SLOTS == 16 ? r & 15 : (r >> 1) & 7))) * 16;
   };
   auto slot_v = [&](int d, int slot) { return K_BYTES + (d * 8 + (slot ^ ((d >> 1) & 7))) * 16; };
-  auto store = [&](int i, auto into) {
+  auto store = [&](int j0, auto into) {
     constexpr int INTO = decltype(into)::value;
     unsigned char *buffer = lds + INTO * BUFFER;
-    const int j0 = chunk_at(i) * 64;
     if (j0 + 64 > span.end || j0 < span.low || !v_there) {          // values that no row looks at may be anything: cleared
       unsigned keep[4];
 #pragma unroll
@@ -166,6 +158,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       }
 #pragma unroll
       for (int r = 0; r < REPS; ++r) vw[r] &= uint4v{keep[0], keep[1], keep[2], keep[3]};
+      if (!(keep[0] | keep[1] | keep[2] | keep[3])) vs = 1.f;         // (the scale may be anything too)
     }
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
@@ -183,11 +176,16 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
     if (lane == 0) there[INTO * 4 + wave] = v_there;
   };
 
-  if (count > 0) {
-    entries(0);
-    load(0);
-    if (count > 1) entries(1);
-    store(0, Zero{});
+  // first places of the chunks that are computed, stored to LDS and looked up in the page table next
+  int chunk = part * RUN, j_now = first_of(chunk), j_next = 0, j_after = 0;
+  const bool any = chunk < span.chunks;
+  if (any) {
+    entries(j_now);
+    load(j_now);
+    chunk = following(chunk);
+    j_next = first_of(chunk);
+    entries(j_next);
+    store(j_now, Zero{});
   }
   // (the queries have arrived here: a wait for them inside the loop would wait for the next chunk's loads too)
 #pragma unroll
@@ -207,11 +205,17 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
     asm volatile("" : "+v"(v_from[u]));
   }
   __syncthreads();
-  auto step = [&](int i, auto of) {                                // (the buffers take turns; a constant one makes their addresses immediates)
+  // One chunk; whether there is another.  (The buffers take turns; a constant one makes their addresses immediates.)
+  auto step = [&](auto of) {
     constexpr int OF = decltype(of)::value;
-    if (i + 1 < count) load(i + 1);
-    if (i + 2 < count) entries(i + 2);
-    const int j0 = chunk_at(i) * 64;
+    const bool more = chunk < span.chunks;
+    if (more) {
+      load(j_next);
+      chunk = following(chunk);
+      j_after = first_of(chunk);
+      entries(j_after);
+    }
+    const int j0 = j_now;
     const bool looks = has_rows && j0 <= place_max && (a.window <= 0 || j0 + 63 > place_min - a.window || j0 < a.sinks);
     if (looks) {
       Sixteen sc[2];
@@ -286,13 +290,14 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       }
       __builtin_amdgcn_sched_group_barrier(0x8, DT, 0);
     }
-    if (i + 1 < count) store(i + 1, std::integral_constant<int, 1 - OF>{});
+    if (more) store(j_next, std::integral_constant<int, 1 - OF>{});
+    j_now = j_next;
+    j_next = j_after;
     __syncthreads();
+    return more;
   };
-  for (int i = 0; i < count; i += 2) {
-    step(i, Zero{});
-    if (i + 1 < count) step(i + 1, One{});
-  }
+  if (any)
+    while (step(Zero{}) && step(One{})) {}
 
   float low, high;
   across_halves(l, low, high);
