@@ -98,9 +98,13 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   float ks[REPS], vs = 1.f;
   int k_entry[REPS], v_entry = -1;
   bool v_there = false;
-  typedef const __attribute__((address_space(4))) int *ScalarInts;
-  typedef const __attribute__((address_space(4))) float *ScalarFloats;
-  const ScalarInts table = (ScalarInts)(c.page_table + b * c.table_stride);
+  // (Numbers and scales come by vector loads of one address: scalar loads would share a counter with the reads of LDS and come in any order, so that
+  // every wait for LDS behind them would wait for them as well.)
+  unsigned nothing;
+  asm volatile("v_mov_b32 %0, 0" : "=v"(nothing));
+  auto one_int = [&](const int *from) { return *(from + nothing); };
+  auto one_float = [&](const float *from) { return *(from + nothing); };
+  const int *table = c.page_table + b * c.table_stride;
   const int last_entry = c.table_pages - 1, mask = (1 << shift) - 1;
   int k_place[REPS];                                                // of this wave's keys in a chunk
   unsigned k_in_page[REPS];
@@ -112,28 +116,29 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   const int v_place = wide ? 0 : wave * 16;
   const unsigned v_in_page = (unsigned)(v_place & mask) * BYTES;
   const unsigned char *k_head = c.k_pages + ((long long)kv_head << shift) * (D * BYTES), *v_head = c.v_pages + (((long long)kv_head * D) << shift) * BYTES;
-  const ScalarFloats k_scales = (ScalarFloats)c.k_scales + kv_head, v_scales = (ScalarFloats)c.v_scales + kv_head;
+  const float *k_scales = c.k_scales + kv_head, *v_scales = c.v_scales + kv_head;
   // Entries of the page table; past its end, where no key is, the last one's.
   auto entries = [&](int j0) {
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) k_entry[r] = table[min((j0 + k_place[r]) >> shift, last_entry)];
-    v_entry = table[min((j0 + v_place) >> shift, last_entry)];
+    for (int r = 0; r < REPS; ++r) k_entry[r] = one_int(table + min((j0 + k_place[r]) >> shift, last_entry));
+    v_entry = one_int(table + min((j0 + v_place) >> shift, last_entry));
   };
   // (instead of a page that is not there page 0 is read, and what comes of it is not used)
   auto load = [&](int j0) {
     const unsigned in_page = (unsigned)(j0 & mask);
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
-      const unsigned page = (unsigned)k_entry[r] < (unsigned)c.n_pages ? (unsigned)k_entry[r] : 0u;
+      const unsigned entry = (unsigned)__builtin_amdgcn_readfirstlane(k_entry[r]), page = entry < (unsigned)c.n_pages ? entry : 0u;
       kw[r] = *reinterpret_cast<const uint4v *>(k_head + (unsigned long long)page * (unsigned)c.k_page_bytes + (in_page * (D * BYTES) + k_in_page[r]) + k_offset);
-      if (E4M3) ks[r] = k_scales[(unsigned long long)page * (unsigned)c.kv_heads];
+      if (E4M3) ks[r] = one_float(k_scales + (unsigned long long)page * (unsigned)c.kv_heads);
     }
-    v_there = (unsigned)v_entry < (unsigned)c.n_pages;
-    const unsigned page = v_there ? (unsigned)v_entry : 0u;
+    const unsigned entry = (unsigned)__builtin_amdgcn_readfirstlane(v_entry);
+    v_there = entry < (unsigned)c.n_pages;
+    const unsigned page = v_there ? entry : 0u;
     const unsigned char *from = v_head + (unsigned long long)page * (unsigned)c.v_page_bytes + (in_page * BYTES + v_in_page);
 #pragma unroll
     for (int r = 0; r < REPS; ++r) vw[r] = *reinterpret_cast<const uint4v *>(from + r * v_step + v_offset);
-    if (E4M3) vs = v_scales[(unsigned long long)page * (unsigned)c.kv_heads];
+    if (E4M3) vs = one_float(v_scales + (unsigned long long)page * (unsigned)c.kv_heads);
   };
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
