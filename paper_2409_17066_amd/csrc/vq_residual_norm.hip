@@ -24,11 +24,14 @@ struct Eight {
 
 typedef float float4b __attribute__((ext_vector_type(4), aligned(4)));
 
-// Elements [i, i + 8) of a row, zeros past its end.
+// Elements [i, i + 8) of a row, zeros past its end.  ONCE: read past the caches, where what is read once would push out what the call writes
+// for the next one (2048 x 8192, both norms, stream in 32 bits: 51.6 us with ordinary loads, 39.2 so).
+template <bool ONCE>
 __device__ __forceinline__ Eight load8(const __half *row, int i, int width) {
   Eight r;
   if (i + 8 <= width) {
-    const uint4v u = *reinterpret_cast<const uint4b *>(row + i);
+    const uint4b *at = reinterpret_cast<const uint4b *>(row + i);
+    const uint4v u = ONCE ? __builtin_nontemporal_load(at) : *at;
     const unsigned w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -42,10 +45,12 @@ __device__ __forceinline__ Eight load8(const __half *row, int i, int width) {
   }
   return r;
 }
+template <bool ONCE>
 __device__ __forceinline__ Eight load8(const float *row, int i, int width) {
   Eight r;
   if (i + 8 <= width) {
-    const float4v a = *reinterpret_cast<const float4b *>(row + i), b = *reinterpret_cast<const float4b *>(row + i + 4);
+    const float4b *at = reinterpret_cast<const float4b *>(row + i);
+    const float4v a = ONCE ? __builtin_nontemporal_load(at) : *at, b = ONCE ? __builtin_nontemporal_load(at + 1) : at[1];
     r.e[0] = a.x; r.e[1] = a.y; r.e[2] = a.z; r.e[3] = a.w;
     r.e[4] = b.x; r.e[5] = b.y; r.e[6] = b.z; r.e[7] = b.w;
   } else {
@@ -98,14 +103,14 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
   const Stream *x = static_cast<const Stream *>(p.x) + row * p.ldx;
   Eight y[NV];
 #pragma unroll
-  for (int v = 0; v < NV; ++v) y[v] = load8(x, i0 + v * stride, width);
+  for (int v = 0; v < NV; ++v) y[v] = load8<true>(x, i0 + v * stride, width);
   if (p.h) {
     const __half *h = p.h + row * p.ldh;
     Eight f[NV];
     float ss = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      f[v] = load8(h, i0 + v * stride, width);
+      f[v] = load8<true>(h, i0 + v * stride, width);
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss = __fmaf_rn(f[v].e[j], f[v].e[j], ss);
     }
@@ -114,7 +119,7 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
       r = 1.f / __fsqrt_rn(block_sum(ss, sums[0]) / (float)width + p.eps);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const Eight w = load8(p.w_post, i0 + v * stride, width);
+        const Eight w = load8<false>(p.w_post, i0 + v * stride, width);
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[v].e[j] *= w.e[j];
       }
@@ -123,7 +128,7 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       if (p.gate) {
-        const Eight g = load8(p.gate + row * p.ldgate, i0 + v * stride, width);
+        const Eight g = load8<false>(p.gate + row * p.ldgate, i0 + v * stride, width);
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[v].e[j] *= g.e[j];
       }
@@ -146,7 +151,7 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
   __half *to = p.z + row * p.ldz;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const Eight w = load8(p.w_pre, i0 + v * stride, width);
+    const Eight w = load8<false>(p.w_pre, i0 + v * stride, width);
 #pragma unroll
     for (int j = 0; j < 8; ++j) y[v].e[j] = y[v].e[j] * r * w.e[j];
     store8(to, i0 + v * stride, width, y[v]);
