@@ -100,11 +100,12 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   bool v_there = false;
   // (Numbers and scales come by vector loads of one address: scalar loads would share a counter with the reads of LDS and come in any order, so that
   // every wait for LDS behind them would wait for them as well.)
-  unsigned nothing;
-  asm volatile("v_mov_b32 %0, 0" : "=v"(nothing));
-  auto one_int = [&](const int *from) { return *(from + nothing); };
-  auto one_float = [&](const float *from) { return *(from + nothing); };
-  const int *table = c.page_table + b * c.table_stride;
+  auto buffer = [](const void *at) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(at), 0, 0xffffffffu, 0x00020000); };
+  auto word_at = [](__amdgpu_buffer_rsrc_t from, unsigned lane_offset, unsigned offset) {
+    return __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset, offset, 0));
+  };
+  auto number_at = [](__amdgpu_buffer_rsrc_t from, unsigned offset) { return __builtin_amdgcn_raw_buffer_load_b32(from, 0, offset, 0); };
+  const __amdgpu_buffer_rsrc_t table = buffer(c.page_table + b * c.table_stride), k_scales = buffer(c.k_scales + kv_head), v_scales = buffer(c.v_scales + kv_head);
   const int last_entry = c.table_pages - 1, mask = (1 << shift) - 1;
   int k_place[REPS];                                                // of this wave's keys in a chunk
   unsigned k_in_page[REPS];
@@ -116,12 +117,11 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   const int v_place = wide ? 0 : wave * 16;
   const unsigned v_in_page = (unsigned)(v_place & mask) * BYTES;
   const unsigned char *k_head = c.k_pages + ((long long)kv_head << shift) * (D * BYTES), *v_head = c.v_pages + (((long long)kv_head * D) << shift) * BYTES;
-  const float *k_scales = c.k_scales + kv_head, *v_scales = c.v_scales + kv_head;
   // Entries of the page table; past its end, where no key is, the last one's.
   auto entries = [&](int j0) {
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) k_entry[r] = one_int(table + min((j0 + k_place[r]) >> shift, last_entry));
-    v_entry = one_int(table + min((j0 + v_place) >> shift, last_entry));
+    for (int r = 0; r < REPS; ++r) k_entry[r] = (int)number_at(table, (unsigned)min((j0 + k_place[r]) >> shift, last_entry) * 4u);
+    v_entry = (int)number_at(table, (unsigned)min((j0 + v_place) >> shift, last_entry) * 4u);
   };
   // (instead of a page that is not there page 0 is read, and what comes of it is not used)
   auto load = [&](int j0) {
@@ -129,27 +129,28 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
       const unsigned entry = (unsigned)__builtin_amdgcn_readfirstlane(k_entry[r]), page = entry < (unsigned)c.n_pages ? entry : 0u;
-      kw[r] = *reinterpret_cast<const uint4v *>(k_head + (unsigned long long)page * (unsigned)c.k_page_bytes + (in_page * (D * BYTES) + k_in_page[r]) + k_offset);
-      if (E4M3) ks[r] = one_float(k_scales + (unsigned long long)page * (unsigned)c.kv_heads);
+      kw[r] = word_at(buffer(k_head + (unsigned long long)page * (unsigned)c.k_page_bytes), k_offset, in_page * (D * BYTES) + k_in_page[r]);
+      if (E4M3) ks[r] = __uint_as_float(number_at(k_scales, page * (unsigned)c.kv_heads * 4u));
     }
     const unsigned entry = (unsigned)__builtin_amdgcn_readfirstlane(v_entry);
     v_there = entry < (unsigned)c.n_pages;
     const unsigned page = v_there ? entry : 0u;
-    const unsigned char *from = v_head + (unsigned long long)page * (unsigned)c.v_page_bytes + (in_page * BYTES + v_in_page);
+    const __amdgpu_buffer_rsrc_t from = buffer(v_head + (unsigned long long)page * (unsigned)c.v_page_bytes);
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) vw[r] = *reinterpret_cast<const uint4v *>(from + r * v_step + v_offset);
-    if (E4M3) vs = one_float(v_scales + (unsigned long long)page * (unsigned)c.kv_heads);
+    for (int r = 0; r < REPS; ++r) vw[r] = word_at(from, v_offset, in_page * BYTES + v_in_page + r * v_step);
+    if (E4M3) vs = __uint_as_float(number_at(v_scales, page * (unsigned)c.kv_heads * 4u));
   };
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
-  auto slot_k = [&](int key, int slot) {
-    const int r = row_of_key(key);
-    return (r * SLOTS + (slot ^ (SLOTS == 16 ? r & 15 : (r >> 1) & 7))) * 16;
-  };
-  auto slot_v = [&](int d, int slot) { return K_BYTES + (d * 8 + (slot ^ ((d >> 1) & 7))) * 16; };
+  // Where this thread's words go: slots of sixteen bytes whose number is mixed with the row's, for reads without conflicts.  Its other words lie constant
+  // distances further on, and the second half of one that is converted is the neighbour.
+  const unsigned lds_at = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+  const int k_row = row_of_key(k_key);
+  unsigned k_to = lds_at + (k_row * SLOTS + ((E4M3 ? 2 * k_piece : k_piece) ^ (SLOTS == 16 ? k_row & 15 : (k_row >> 1) & 7))) * 16;
+  unsigned v_to = lds_at + K_BYTES + (v_d * 8 + ((E4M3 ? 2 * v_piece : v_piece) ^ ((v_d >> 1) & 7))) * 16;
+  auto put = [](unsigned at, uint4v x) { *(__attribute__((address_space(3))) uint4v *)(size_t)at = x; };
   auto store = [&](int j0, auto into) {
     constexpr int INTO = decltype(into)::value;
-    unsigned char *buffer = lds + INTO * BUFFER;
     if (j0 + 64 > span.end || j0 < span.low || !v_there) {          // values that no row looks at may be anything: cleared
       unsigned keep[4];
 #pragma unroll
@@ -167,15 +168,16 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
     }
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
-      const int key = k_key + r * K_STEP, d = v_d + r * V_STEP;
+      const int row = row_of_key(r * K_STEP);                       // how far key k_key + r * K_STEP is from k_key: row 4 has its slots mixed otherwise
+      const unsigned mixed = (SLOTS == 16 ? row & 15 : 0) * 16u, k_further = INTO * BUFFER + row * SLOTS * 16, v_further = INTO * BUFFER + r * V_STEP * 8 * 16;
       if constexpr (E4M3) {
-        *reinterpret_cast<half8v *>(buffer + slot_k(key, 2 * k_piece)) = halves_of_e4m3(kw[r].x, kw[r].y, ks[r]);
-        *reinterpret_cast<half8v *>(buffer + slot_k(key, 2 * k_piece + 1)) = halves_of_e4m3(kw[r].z, kw[r].w, ks[r]);
-        *reinterpret_cast<half8v *>(buffer + slot_v(d, 2 * v_piece)) = halves_of_e4m3(vw[r].x, vw[r].y, vs);
-        *reinterpret_cast<half8v *>(buffer + slot_v(d, 2 * v_piece + 1)) = halves_of_e4m3(vw[r].z, vw[r].w, vs);
+        put((k_to ^ mixed) + k_further, __builtin_bit_cast(uint4v, halves_of_e4m3(kw[r].x, kw[r].y, ks[r])));
+        put((k_to ^ mixed ^ 16u) + k_further, __builtin_bit_cast(uint4v, halves_of_e4m3(kw[r].z, kw[r].w, ks[r])));
+        put(v_to + v_further, __builtin_bit_cast(uint4v, halves_of_e4m3(vw[r].x, vw[r].y, vs)));
+        put((v_to ^ 16u) + v_further, __builtin_bit_cast(uint4v, halves_of_e4m3(vw[r].z, vw[r].w, vs)));
       } else {
-        *reinterpret_cast<uint4v *>(buffer + slot_k(key, k_piece)) = kw[r];
-        *reinterpret_cast<uint4v *>(buffer + slot_v(d, v_piece)) = vw[r];
+        put((k_to ^ mixed) + k_further, kw[r]);
+        put(v_to + v_further, vw[r]);
       }
     }
     if (lane == 0) there[INTO * 4 + wave] = v_there;
@@ -197,7 +199,6 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   for (int i = 0; i < STEPS; ++i) asm volatile("" : "+v"(q[i]));
   // Where this lane's operands lie in the first buffer; what else an address consists of is a constant.
   auto lds_halves = [](unsigned at) { return *(const __attribute__((address_space(3))) half8v *)(size_t)at; };
-  const unsigned lds_at = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
   unsigned k_from[STEPS], v_from[4];
 #pragma unroll
   for (int st = 0; st < STEPS; ++st) {
