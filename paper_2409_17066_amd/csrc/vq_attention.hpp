@@ -86,6 +86,58 @@ __device__ __forceinline__ float where_seen(unsigned seen, int r, float x) {
   return __uint_as_float((__float_as_uint(x) & all) | (0xff800000u & ~all));
 }
 
+// Values that are not finite, of keys that some rows of a tile see and others do not: zero times them would reach the rows that do not.  They are taken
+// out of the operands (Odd::clean) and come back as a sum that is not finite for the rows that see them: bits of 64 keys for each element and kind.
+template <bool E4M3>
+struct Odd {
+  static constexpr int KINDS = E4M3 ? 1 : 3, KEYS = E4M3 ? 16 : 8;           // NaN, and in 16 bits both infinities; keys of a 16-byte word
+  static __device__ __forceinline__ bool any(uint4v w) {
+    const unsigned exponent = E4M3 ? 0x7f7f7f7fu : 0x7c007c00u, one = E4M3 ? 0x01010101u : 0x04000400u, carry = E4M3 ? 0x80808080u : 0x80008000u;
+    return ((((w.x & exponent) + one) | ((w.y & exponent) + one) | ((w.z & exponent) + one) | ((w.w & exponent) + one)) & carry) != 0;
+  }
+  // Bits of the word's keys by kind; the word without them.
+  static __device__ __forceinline__ uint4v clean(uint4v w, unsigned (&bits)[KINDS]) {
+    unsigned x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < KINDS; ++k) bits[k] = 0;
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+      const int per = KEYS / 4, shift = i % per * (32 / per);
+      const unsigned v = x[i / per] >> shift & (E4M3 ? 0xffu : 0xffffu);
+      const bool odd = E4M3 ? (v & 0x7f) == 0x7f : (v & 0x7c00) == 0x7c00;
+      const int kind = E4M3 || (v & 0x3ff) ? 0 : v & 0x8000 ? 2 : 1;
+#pragma unroll
+      for (int k = 0; k < KINDS; ++k) bits[k] |= odd && kind == k ? 1u << i : 0u;
+      if (odd) x[i / per] &= ~((E4M3 ? 0xffu : 0xffffu) << shift);
+    }
+    return uint4v{x[0], x[1], x[2], x[3]};
+  }
+  // The bits lie in LDS from address `bits` on, [KINDS][elements], eight bytes each.  (Addresses of LDS as numbers, made opaque where they are used: the compiler
+  // would keep each in a register through the loops around, for what hardly ever happens.)
+  static __device__ __forceinline__ void put(unsigned at, int kind, int elements, unsigned of) {
+    typedef __attribute__((address_space(3))) unsigned short *Shorts;
+    typedef __attribute__((address_space(3))) unsigned char *Bytes;
+    if (E4M3) *(Shorts)(size_t)(at + kind * elements * 8) = (unsigned short)of;
+    else *(Bytes)(size_t)(at + kind * elements * 8) = (unsigned char)of;
+  }
+  // What they add to an element, whose bits of the first kind are at `at`, of a row that sees the keys of `seen`.
+  static __device__ __forceinline__ float sum(unsigned at, int elements, unsigned long long seen) {
+    typedef const __attribute__((address_space(3))) unsigned long long *Longs;
+    const float inf = __builtin_inff();
+    float x = *(Longs)(size_t)at & seen ? __builtin_nanf("") : 0.f;
+    if constexpr (!E4M3) {
+      if (*(Longs)(size_t)(at + elements * 8) & seen) x += inf;
+      if (*(Longs)(size_t)(at + 2 * elements * 8) & seen) x -= inf;
+    }
+    return x;
+  }
+};
+// Which of 64 places from `base` on a token sees.
+__device__ __forceinline__ unsigned long long seen64_of(const AttentionParams &a, const Sequence &s, int place, int base) {
+  return (unsigned long long)(seen_of(a, s, place, base) | seen_of(a, s, place, base + 16) << 16) |
+         (unsigned long long)(seen_of(a, s, place, base + 32) | seen_of(a, s, place, base + 48) << 16) << 32;
+}
+
 // A finite stand-in for the maximum of a row that has seen nothing yet.
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
 // One over a softmax's sum; zero for a row that sees nothing; what is not a number stays none.

@@ -15,10 +15,12 @@ namespace {
 
 constexpr int WAVES = RUN;
 
-// RT: tiles of sixteen rows; D: elements of a head.
-template <bool E4M3, int D, int RT>
+// RT: tiles of sixteen rows; D: elements of a head; MANY: rows may be of several new tokens, which see different keys.
+template <bool E4M3, int D, int RT, bool MANY>
 __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles) {
   constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
+  // The next chunk is loaded ahead where there are registers for it beside those of the rows' differences.
+  constexpr bool AHEAD = !MANY || E4M3 || D == 64;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   const int part = (int)blockIdx.z, kv_head = (int)blockIdx.y, b = tiles > 1 ? (int)blockIdx.x / tiles : (int)blockIdx.x, tile = tiles > 1 ? (int)blockIdx.x % tiles : 0;
@@ -26,6 +28,8 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
   // Entries of the page table for places [of, of + 16).  Without a window the first ones do not depend on the sequence's length, and are asked for beside it.
   auto entry = [&](int of) { return of >> shift < c.table_pages ? c.page_table[b * c.table_stride + (of >> shift)] : -1; };
   int i = part * RUN + wave, k_entry = 0, v_entry = 0;
+  float *ml = lds, *out = lds + 2 * 16 * WAVES, *put_back = out;      // (a wave's first part of put_back is read before its results take the place)
+  bool any_odd = false;
   if (a.window == 0) {
     k_entry = entry(i * 64 + 16 * (n >> 2));
     v_entry = entry(i * 64 + 16 * g);
@@ -108,6 +112,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
     const int j0 = span.chunk(i) * 64, next = i + stride;
     if (next < end) entries_of(next);
     float4v sc[RT][4];
+    bool odd = false;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       half8v f[STEPS];
@@ -128,7 +133,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
         sc[rt][t] = x;
       }
     }
-    if (next < end) load_k(next);
+    if (AHEAD && next < end) load_k(next);
     // keys that some row does not see: hidden from it; those that no row sees may hold anything, so their values are cleared
     const bool all_there = __ballot(!v_there) == 0;
     if (!all_there || j0 + 63 > span.place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= span.place_max - a.window)) {
@@ -155,6 +160,29 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int w = 0; w < VL; ++w) v[dt][w] &= uint4v{keep[4 * w], keep[4 * w + 1], keep[4 * w + 2], keep[4 * w + 3]};
+      if (MANY && span.place_min != span.place_max) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int w = 0; w < VL; ++w) odd |= Odd<E4M3>::any(v[dt][w]);
+        odd = __ballot(odd) != 0;
+        if (odd) {
+          unsigned bits = (unsigned)(size_t)(__attribute__((address_space(3))) float *)(put_back + RT * WAVES * 16 * PITCH) + wave * (Odd<E4M3>::KINDS * D * 8) + n * 8 + g * 2;
+          asm volatile("" : "+v"(bits));
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int w = 0; w < VL; ++w) {
+              unsigned of[Odd<E4M3>::KINDS];
+              v[dt][w] = Odd<E4M3>::clean(v[dt][w], of);
+#pragma unroll
+              for (int kind = 0; kind < Odd<E4M3>::KINDS; ++kind) Odd<E4M3>::put(bits + dt * 16 * 8 + w, kind, D, of[kind]);
+              __builtin_amdgcn_sched_barrier(0);                    // (one after the other: registers)
+            }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+        }
+      }
     }
     half8v p[RT][2];
 #pragma unroll
@@ -205,17 +233,39 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
         o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1], p[rt][1], o[rt][dt], 0, 0, 0);
       }
     }
-    if (next < end) load_v(next);
+    if (MANY && odd) {                                             // (to LDS, and from there to the outputs behind the loop: beside what is loaded there are no registers)
+      const unsigned bits = (unsigned)(size_t)(__attribute__((address_space(3))) float *)(put_back + RT * WAVES * 16 * PITCH) + wave * (Odd<E4M3>::KINDS * D * 8) + g * 4 * 8;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const unsigned long long seen = seen64_of(a, s, place[rt], j0);
+        for (int dt = 0; dt < DT; ++dt) {
+          const unsigned at = bits + dt * 16 * 8;
+          float4v *to = reinterpret_cast<float4v *>(put_back + ((rt * WAVES + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
+          const float4v x = {Odd<E4M3>::sum(at, D, seen), Odd<E4M3>::sum(at + 8, D, seen), Odd<E4M3>::sum(at + 16, D, seen), Odd<E4M3>::sum(at + 24, D, seen)};
+          *to = any_odd ? *to + x : x;
+        }
+      }
+      any_odd = true;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (next < end) {
+      if (!AHEAD) load_k(next);
+      load_v(next);
+    }
   }
 
   // the waves' results, joined through LDS, sixteen rows at a time
-  float *ml = lds, *out = lds + 2 * 16 * WAVES;
   const bool whole = parts_of(split, span.chunks) == 1;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int left = here - rt * 16;
     if (left <= 0) break;
     __syncthreads();
+    if (MANY && any_odd) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[rt][dt] += *reinterpret_cast<const float4v *>(put_back + ((rt * WAVES + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
+    }
     const float sum = rows_sum(l[rt]);
     if (wave < active && lane < 16) {
       ml[2 * (wave * 16 + n)] = m[rt];
@@ -312,29 +362,37 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvPa
   if (a.lse && threadIdx.x == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
 }
 
-template <bool E4M3, int D, int RT>
+template <bool E4M3, int D, int RT, bool MANY>
 int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
   const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT);
   const long long blocks = (long long)tiles * c.n_seqs;
   if (blocks > 0x7fffffff / 512 || c.kv_heads > 65535) return VQ_ERR_SHAPE;
-  const int lds = (2 * 16 + 16 * (D + 4)) * WAVES * 4;
-  VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT>));
-  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT>), dim3((unsigned)blocks, c.kv_heads, s.parts), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
+  const int lds = (2 * 16 + 16 * (D + 4) * (MANY ? RT : 1)) * WAVES * 4 + (MANY ? WAVES * Odd<E4M3>::KINDS * D * 8 : 0);
+  VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT, MANY>));
+  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY>), dim3((unsigned)blocks, c.kv_heads, s.parts), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 
 }  // namespace
 
-// Two tiles share the conversions and loads of a chunk, where the registers are there: not beside 64 of a 16-bit chunk's keys and as many of its values.
+// Two tiles share the conversions and loads of a chunk, where the registers are there: not beside 64 of a 16-bit chunk's keys and as many of its values, nor
+// (heads of 128 elements) beside what rows of several tokens need.
 int attention_decode_rows(const KvParams &c, const AttentionParams &a) {
-  return (long long)c.max_new * a.group > 16 && (c.e4m3 || c.head_dim == 64) ? 32 : 16;
+  return (long long)c.max_new * a.group > 16 && (c.head_dim == 64 || (c.e4m3 && c.max_new == 1)) ? 32 : 16;
+}
+
+template <bool MANY>
+static int launch_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  const bool two = attention_decode_rows(c, a) == 32;
+  if (c.head_dim == 64) return c.e4m3 ? (two ? launch<true, 64, 2, MANY>(c, a, s, stream) : launch<true, 64, 1, MANY>(c, a, s, stream))
+                                      : (two ? launch<false, 64, 2, MANY>(c, a, s, stream) : launch<false, 64, 1, MANY>(c, a, s, stream));
+  if constexpr (!MANY)
+    if (two) return launch<true, 128, 2, MANY>(c, a, s, stream);
+  return c.e4m3 ? launch<true, 128, 1, MANY>(c, a, s, stream) : launch<false, 128, 1, MANY>(c, a, s, stream);
 }
 
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  const bool two = attention_decode_rows(c, a) == 32;
-  if (c.head_dim == 64) return c.e4m3 ? (two ? launch<true, 64, 2>(c, a, s, stream) : launch<true, 64, 1>(c, a, s, stream))
-                                      : (two ? launch<false, 64, 2>(c, a, s, stream) : launch<false, 64, 1>(c, a, s, stream));
-  return c.e4m3 ? (two ? launch<true, 128, 2>(c, a, s, stream) : launch<true, 128, 1>(c, a, s, stream)) : launch<false, 128, 1>(c, a, s, stream);
+  return c.max_new > 1 ? launch_decode<true>(c, a, s, stream) : launch_decode<false>(c, a, s, stream);
 }
 
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream) {

@@ -41,7 +41,8 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   constexpr int K_BYTES = 64 * D * 2, BUFFER = 2 * K_BYTES;
   constexpr int STEPS = D / 16, DT = D / 32, AHEAD = 6;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  unsigned char *there = lds + 2 * BUFFER;                         // [2][4]: whether each sixteen keys of a buffer have a page
+  unsigned char *there = lds + 2 * BUFFER;                         // [2][4]: bit 0, whether each sixteen keys of a buffer have a page; 1: values to be put back
+  auto bits_of = [](int buffer) { return 2 * BUFFER + 16 + buffer * (Odd<E4M3>::KINDS * D * 8); };
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
 
   // Long sequences first and of each the rows that see most, so that short work fills the end; where all workgroups are resident at once, so that
@@ -166,6 +167,21 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       for (int r = 0; r < REPS; ++r) vw[r] &= uint4v{keep[0], keep[1], keep[2], keep[3]};
       if (!(keep[0] | keep[1] | keep[2] | keep[3])) vs = 1.f;         // (the scale may be anything too)
     }
+    bool odd = false;
+    if (span.place_min != span.place_max && (j0 + 63 > span.place_min || (a.window > 0 && j0 <= span.place_max - a.window))) {
+      unsigned bits = lds_at + bits_of(INTO) + v_d * 8 + v_piece * (Odd<E4M3>::KEYS / 8);
+      asm volatile("" : "+v"(bits));
+#pragma unroll
+      for (int r = 0; r < REPS; ++r) {
+        odd |= Odd<E4M3>::any(vw[r]);
+        unsigned of[Odd<E4M3>::KINDS];
+        vw[r] = Odd<E4M3>::clean(vw[r], of);
+#pragma unroll
+        for (int kind = 0; kind < Odd<E4M3>::KINDS; ++kind) Odd<E4M3>::put(bits + r * V_STEP * 8, kind, D, of[kind]);
+        __builtin_amdgcn_sched_barrier(0);                            // (one after the other: registers)
+      }
+      odd = __ballot(odd) != 0;
+    }
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
       const int row = row_of_key(r * K_STEP);                       // how far key k_key + r * K_STEP is from k_key: row 4 has its slots mixed otherwise
@@ -180,7 +196,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
         put(v_to + v_further, vw[r]);
       }
     }
-    if (lane == 0) there[INTO * 4 + wave] = v_there;
+    if (lane == 0) there[INTO * 4 + wave] = (unsigned char)(v_there | odd << 1);
   };
 
   // first places of the chunks that are computed, stored to LDS and looked up in the page table next
@@ -295,6 +311,21 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x8, DT, 0);
+      if (is & 0x02020202u) {
+        const unsigned long long seen = seen64_of(a, s, place, j0);
+        unsigned bits = lds_at + bits_of(OF) + h * 4 * 8;
+        asm volatile("" : "+v"(bits));
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          Sixteen x = __builtin_bit_cast(Sixteen, o[dt]);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            x.f[r] += Odd<E4M3>::sum(bits + (32 * dt + 8 * (r >> 2) + (r & 3)) * 8, D, seen);
+            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+          }
+          o[dt] = __builtin_bit_cast(float16v, x);
+        }
+      }
     }
     if (more) store(j_next, std::integral_constant<int, 1 - OF>{});
     j_now = j_next;
@@ -341,7 +372,7 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
   const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
   if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
   VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D>));
-  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16, stream, c, a, s, tiles,
+  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8, stream, c, a, s, tiles,
                      blocks <= 2 * cu_count());
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }

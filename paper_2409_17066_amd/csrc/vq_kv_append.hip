@@ -1,9 +1,12 @@
 // New keys and values into a paged cache, and the rotation of queries and keys by their positions on the way.
 //
 // One launch.  A team of one, two or four waves takes one page, head and matrix (keys or values) that a sequence's new tokens reach, other waves take a head
-// of some queries.  A lane takes eight elements of four tokens at a time: memory bounds it, and with fewer bytes on their way in each wave the chain from lengths to
+// of some queries.  Memory bounds it, and with fewer bytes on their way in each wave the chain from lengths to
 // page table to elements to scale does.  Every element is read once, rotated in binary32 and written once; in 8 bits the page's scale has to be known
-// before the first code is, so a lane keeps its first four tokens in registers between the two, and reads what large pages hold beyond that again (from L2).
+// before the first code is, so a lane keeps its first tokens in registers between the two, and reads what large pages hold beyond that again (from L2).
+// A lane takes 32 elements at a time: of two tokens eight elements and the eight half a head further on, so that what it rotates are pairs and a token's
+// cosines and sines are read once for both (half the loads through L1 of one half each: prompts of four users, 2624 tokens of 32 + 32 + 32 heads, 40 ->
+// 31 us), or, where the rotation pairs other elements, eight elements of four tokens.
 #include "vq_kv.hpp"
 
 namespace vq {
@@ -19,7 +22,7 @@ struct AppendParams {
   __half *q_out;
   int q_heads, slots, team;                   // pages a sequence can reach; waves of a team
   int kv_blocks, q_tiles;                     // workgroups for keys and values; waves for one head of a sequence's queries
-  int columns, groups, tokens;                // lanes of a token, groups of four tokens of a wave, tokens of a wave at a time
+  int columns, groups, tokens;                // lanes of a token, groups of tokens of a wave, tokens of a wave at a time
   Rotary r;
 };
 
@@ -33,33 +36,48 @@ __device__ __forceinline__ Eight widened(uint4v u) {
   return Eight{{(float)a.x, (float)a.y, (float)b.x, (float)b.y, (float)c.x, (float)c.y, (float)d.x, (float)d.y}};
 }
 
-// Elements [d, d + 8) of one head of one token, rotated.  d is a multiple of 8, rotary.dim is even.  EIGHTS: pairs lie half of rotary.dim apart, and
-// eight elements have their partners in eight others.
-template <bool EIGHTS>
-__device__ __forceinline__ Eight rotated(const __half *x, int d, const Rotary &r, int at, Eight y) {
-  if (d >= r.dim) return y;
+__device__ __forceinline__ Eight eight_of(const float *from) {
+  const float4v a = *reinterpret_cast<const float4b *>(from), b = *reinterpret_cast<const float4b *>(from + 4);
+  return Eight{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+
+// Pairs (a[i], b[i]) of elements j + i and dim / 2 + j + i, rotated.
+__device__ __forceinline__ void rotate_pairs(const Rotary &r, int at, int j, Eight &a, Eight &b) {
+  const Eight c = eight_of(r.cos + at * r.ld + j), s = eight_of(r.sin + at * r.ld + j);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = a.e[i], y = b.e[i];
+    a.e[i] = x * c.e[i] - y * s.e[i];
+    b.e[i] = y * c.e[i] + x * s.e[i];
+  }
+}
+
+// Elements [d, d + 8) of one head of one token, rotated, whatever the pairs are.  d is a multiple of 8, rotary.dim is even.
+__device__ __forceinline__ void rotate_eight(const Rotary &r, int at, const __half *x, int d, Eight &y) {
+  if (d >= r.dim) return;
   const long long row = (long long)at * r.ld;
   float (&e)[8] = y.e;
   const int half = r.dim / 2;
-  if constexpr (EIGHTS) {
-    const bool second = d >= half;
-    const int j = second ? d - half : d;
-    const Eight p = widened(*reinterpret_cast<const uint4b *>(x + (second ? j : d + half)));
-    const float4v c0 = *reinterpret_cast<const float4b *>(r.cos + row + j), c1 = *reinterpret_cast<const float4b *>(r.cos + row + j + 4);
-    const float4v s0 = *reinterpret_cast<const float4b *>(r.sin + row + j), s1 = *reinterpret_cast<const float4b *>(r.sin + row + j + 4);
-    const float c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+  if (r.interleaved) {
+    float c[4], s[4];
+    if (d + 8 <= r.dim) {
+      const float4v cv = *reinterpret_cast<const float4b *>(r.cos + row + d / 2), sv = *reinterpret_cast<const float4b *>(r.sin + row + d / 2);
+      c[0] = cv.x; c[1] = cv.y; c[2] = cv.z; c[3] = cv.w;
+      s[0] = sv.x; s[1] = sv.y; s[2] = sv.z; s[3] = sv.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float far = p.e[i] * s[i];
-      e[i] = second ? e[i] * c[i] + far : e[i] * c[i] - far;
+      for (int i = 0; i < 4; ++i) {
+        const bool turns = d + 2 * i < r.dim;
+        c[i] = turns ? r.cos[row + d / 2 + i] : 1.f;
+        s[i] = turns ? r.sin[row + d / 2 + i] : 0.f;
+      }
     }
-  } else if (r.interleaved) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (d + 2 * i >= r.dim) break;
-      const float c = r.cos[row + d / 2 + i], s = r.sin[row + d / 2 + i], a = e[2 * i], b = e[2 * i + 1];
-      e[2 * i] = a * c - b * s;
-      e[2 * i + 1] = b * c + a * s;
+      const float a = e[2 * i], b = e[2 * i + 1];
+      e[2 * i] = a * c[i] - b * s[i];
+      e[2 * i + 1] = b * c[i] + a * s[i];
     }
   } else {
 #pragma unroll
@@ -71,7 +89,6 @@ __device__ __forceinline__ Eight rotated(const __half *x, int d, const Rotary &r
       e[i] = second ? e[i] * c + far : e[i] * c - far;
     }
   }
-  return y;
 }
 
 __device__ __forceinline__ float largest(const Eight &x, float so_far) {
@@ -110,54 +127,66 @@ __device__ __forceinline__ uint4v halves8(const Eight &x) {
   return uint4v{packed(x.e[0], x.e[1]), packed(x.e[2], x.e[3]), packed(x.e[4], x.e[5]), packed(x.e[6], x.e[7])};
 }
 
-// What the lanes of a wave take: column `d` of tokens 4 group ... 4 group + 3 of every `tokens` tokens (lanes left over: none).
+// What a lane takes of every `tokens` tokens: TOKENS of them from TOKENS * group on, PARTS times eight elements (lanes left over: none).
+template <bool PAIRED>
+struct Share {
+  static constexpr int TOKENS = PAIRED ? 2 : 4, PARTS = PAIRED ? 2 : 1;
+  Eight y[TOKENS][PARTS];
+};
 struct Place {
-  int d, group;
+  int d[2], group;                                                  // elements of the parts
   bool lane;
 };
+template <bool PAIRED>
 __device__ __forceinline__ Place place_of(const AppendParams &p) {
-  const int lane = (int)threadIdx.x & 63, group = lane / p.columns;
-  return Place{(lane - group * p.columns) * 8, group, group < p.groups};
+  const int lane = (int)threadIdx.x & 63, group = lane / p.columns, d = (lane - group * p.columns) * 8;
+  return Place{{d, d + p.c.head_dim / 2}, group, group < p.groups};
 }
 
-// Four tokens' elements: rows row0 + t ... of x, where t < end (and t >= begin), rotated if `turn`.
-template <bool EIGHTS>
-__device__ __forceinline__ void take(const Rotary &r, const __half *x, long long ld, int row0, int place0, int d, int t, int begin, int end, bool turn,
-                                     Eight (&y)[4]) {
+// A lane's tokens: rows row0 + t ... of x, where begin <= t < end, rotated if `turn`.
+template <bool PAIRED>
+__device__ __forceinline__ void take(const Rotary &r, const __half *x, long long ld, int row0, int place0, const Place &at, int t, int begin, int end, bool turn,
+                                     Share<PAIRED> &s) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (EIGHTS && k == 2) __builtin_amdgcn_sched_barrier(0);          // (two tokens' operands at a time: registers)
-    y[k] = Eight{};
+  for (int k = 0; k < Share<PAIRED>::TOKENS; ++k) {
+#pragma unroll
+    for (int i = 0; i < Share<PAIRED>::PARTS; ++i) s.y[k][i] = Eight{};
     if (t + k < begin || t + k >= end) continue;
     const __half *from = x + (row0 + t + k) * ld;
-    y[k] = widened(*reinterpret_cast<const uint4b *>(from + d));
-    if (turn) y[k] = rotated<EIGHTS>(from, d, r, min(max(r.position ? r.position[row0 + t + k] : place0 + t + k, 0), r.positions - 1), y[k]);
+#pragma unroll
+    for (int i = 0; i < Share<PAIRED>::PARTS; ++i) s.y[k][i] = widened(*reinterpret_cast<const uint4b *>(from + at.d[i]));
+    if (!turn) continue;
+    const int row = min(max(r.position ? r.position[row0 + t + k] : place0 + t + k, 0), r.positions - 1);
+    if constexpr (PAIRED) rotate_pairs(r, row, at.d[0], s.y[k][0], s.y[k][1]);
+    else rotate_eight(r, row, from, at.d[0], s.y[k][0]);
   }
 }
 
-template <bool EIGHTS>
+template <bool PAIRED>
 __device__ __forceinline__ void append_queries(const AppendParams &p, int wave) {
   const int head = wave % p.q_heads, tile = wave / p.q_heads % p.q_tiles, b = wave / p.q_heads / p.q_tiles;
   if (b >= p.c.n_seqs) return;
   const Sequence s = sequence(p.c, b);
-  const Place at = place_of(p);
-  const int t = tile * p.tokens + at.group * 4;
+  const Place at = place_of<PAIRED>(p);
+  Share<PAIRED> q;
+  const int t = tile * p.tokens + at.group * q.TOKENS;
   if (!at.lane || t >= s.rows) return;
-  Eight y[4];
   const long long from = (long long)head * p.c.head_dim;
-  take<EIGHTS>(p.r, p.q + from, p.ldq, s.row0, s.first, at.d, t, 0, s.rows, p.r.cos != nullptr, y);
+  take<PAIRED>(p.r, p.q + from, p.ldq, s.row0, s.first, at, t, 0, s.rows, p.r.cos != nullptr, q);
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (t + k < s.rows) *reinterpret_cast<uint4b *>(p.q_out + (s.row0 + t + k) * p.ldq_out + from + at.d) = halves8(y[k]);
+  for (int k = 0; k < q.TOKENS; ++k)
+#pragma unroll
+    for (int i = 0; i < q.PARTS; ++i)
+      if (t + k < s.rows) *reinterpret_cast<uint4b *>(p.q_out + (s.row0 + t + k) * p.ldq_out + from + at.d[i]) = halves8(q.y[k][i]);
 }
 
-template <bool E4M3, bool EIGHTS>
-__global__ __launch_bounds__(64 * WAVES, EIGHTS ? 4 : 2) void kv_append_kernel(const AppendParams p) {
+template <bool E4M3, bool PAIRED>
+__global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_kernel(const AppendParams p) {
   __shared__ float wave_max[WAVES];
   __shared__ __attribute__((aligned(16))) unsigned char tiles[WAVES][WAVE_LDS];
   const KvParams &c = p.c;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  if ((int)blockIdx.x >= p.kv_blocks) return append_queries<EIGHTS>(p, ((int)blockIdx.x - p.kv_blocks) * WAVES + wave);
+  if ((int)blockIdx.x >= p.kv_blocks) return append_queries<PAIRED>(p, ((int)blockIdx.x - p.kv_blocks) * WAVES + wave);
   const int in_team = wave & (p.team - 1);
   int unit = ((int)blockIdx.x * WAVES + wave) / p.team;
   const bool values = unit & 1;
@@ -177,12 +206,13 @@ __global__ __launch_bounds__(64 * WAVES, EIGHTS ? 4 : 2) void kv_append_kernel(c
   const long long ld = values ? p.ldv : p.ldk;
   const bool turn = !values && p.r.cos;
   constexpr int bytes = E4M3 ? 1 : 2;
-  const Place at = place_of(p);
-  // this wave's tokens: [t, t + 4) of the lane, every p.tokens * p.team
+  const Place at = place_of<PAIRED>(p);
+  constexpr int TOKENS = Share<PAIRED>::TOKENS, PARTS = Share<PAIRED>::PARTS;
+  // this wave's tokens: [t, t + TOKENS) of the lane, every p.tokens * p.team
   const int stride = p.tokens * p.team, start = (begin & -stride) + in_team * p.tokens;
   const int lane_end = at.lane ? end : 0;
-  Eight held[4];
-  take<EIGHTS>(p.r, x, ld, row0, place0, at.d, start + at.group * 4, begin, lane_end, turn, held);
+  Share<PAIRED> held;
+  take<PAIRED>(p.r, x, ld, row0, place0, at, start + at.group * TOKENS, begin, lane_end, turn, held);
   if (page < 0) return;                                                          // (the elements are on their way beside the page's number)
   unsigned char *to = (values ? c.v_pages + page * c.v_page_bytes : c.k_pages + page * c.k_page_bytes) + (long long)head * size * d_all * bytes;
   float *scale_at = (values ? c.v_scales : c.k_scales) + (E4M3 ? (long long)page * c.kv_heads + head : 0);
@@ -190,13 +220,17 @@ __global__ __launch_bounds__(64 * WAVES, EIGHTS ? 4 : 2) void kv_append_kernel(c
   float inverse = 1.f;
   if (E4M3) {
     float amax = 0.f;
+    auto largest_of = [&](const Share<PAIRED> &x) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) amax = largest(held[k], amax);
+      for (int k = 0; k < TOKENS; ++k)
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) amax = largest(x.y[k][i], amax);
+    };
+    largest_of(held);
     for (int t0 = start + stride; t0 < end; t0 += stride) {
-      Eight y[4];
-      take<EIGHTS>(p.r, x, ld, row0, place0, at.d, t0 + at.group * 4, begin, lane_end, turn, y);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) amax = largest(y[k], amax);
+      Share<PAIRED> more;
+      take<PAIRED>(p.r, x, ld, row0, place0, at, t0 + at.group * TOKENS, begin, lane_end, turn, more);
+      largest_of(more);
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
@@ -226,70 +260,77 @@ __global__ __launch_bounds__(64 * WAVES, EIGHTS ? 4 : 2) void kv_append_kernel(c
     if (in_team == 0 && lane == 0 && !(begin > 0 && scale == before)) *scale_at = scale;
   }
   for (int t0 = start; t0 < end; t0 += stride) {
-    const int t = t0 + at.group * 4;
-    if (t0 != start) take<EIGHTS>(p.r, x, ld, row0, place0, at.d, t, begin, lane_end, turn, held);
-    unsigned code[4][2];                                                // a token's eight codes
-    uint4v half[4];                                                     // or its halfs
+    const int t = t0 + at.group * TOKENS;
+    if (t0 != start) take<PAIRED>(p.r, x, ld, row0, place0, at, t, begin, lane_end, turn, held);
+    uint4v word[TOKENS][PARTS];                                         // eight halfs, or in x and y eight codes
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const Eight &y = held[k];
-      if (E4M3) {
-        code[k][0] = codes4(y.e[0] * inverse, y.e[1] * inverse, y.e[2] * inverse, y.e[3] * inverse);
-        code[k][1] = codes4(y.e[4] * inverse, y.e[5] * inverse, y.e[6] * inverse, y.e[7] * inverse);
-      } else {
-        half[k] = halves8(y);
+    for (int k = 0; k < TOKENS; ++k)
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        const Eight &y = held.y[k][i];
+        if (E4M3) word[k][i] = uint4v{codes4(y.e[0] * inverse, y.e[1] * inverse, y.e[2] * inverse, y.e[3] * inverse), codes4(y.e[4] * inverse, y.e[5] * inverse, y.e[6] * inverse, y.e[7] * inverse), 0, 0};
+        else word[k][i] = halves8(y);
       }
-    }
+    // element j of them
+    auto element = [&](int k, int i, int j) {
+      const uint4v w = word[k][i];
+      if (E4M3) return (j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 0xffu;
+      return (j < 2 ? w.x : j < 4 ? w.y : j < 6 ? w.z : w.w) >> (16 * (j & 1)) & 0xffffu;
+    };
     if (!values) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < TOKENS; ++k) {
         if (t + k < begin || t + k >= lane_end) continue;
-        if (E4M3) *reinterpret_cast<uint2v *>(to + (t + k) * d_all + at.d) = uint2v{code[k][0], code[k][1]};
-        else *reinterpret_cast<uint4v *>(to + ((t + k) * d_all + at.d) * 2) = half[k];
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+          if (E4M3) *reinterpret_cast<uint2v *>(to + (t + k) * d_all + at.d[i]) = uint2v{word[k][i].x, word[k][i].y};
+          else *reinterpret_cast<uint4v *>(to + ((t + k) * d_all + at.d[i]) * 2) = word[k][i];
+        }
       }
       continue;
     }
     // Values, whose tokens lie next to each other in the cache.
     if (t0 < begin || t0 + p.tokens > end) {                            // some tokens of these: one by one
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < TOKENS; ++k) {
         if (t + k < begin || t + k >= lane_end) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (E4M3) {
-            to[(at.d + i) * size + t + k] = (unsigned char)(code[k][i >> 2] >> (8 * (i & 3)));
-          } else {
-            const unsigned w = i < 2 ? half[k].x : i < 4 ? half[k].y : i < 6 ? half[k].z : half[k].w;
-            reinterpret_cast<unsigned short *>(to)[(at.d + i) * size + t + k] = (unsigned short)(w >> (16 * (i & 1)));
+        for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int at_element = (at.d[i] + j) * size + t + k;
+            if (E4M3) to[at_element] = (unsigned char)element(k, i, j);
+            else reinterpret_cast<unsigned short *>(to)[at_element] = (unsigned short)element(k, i, j);
           }
-        }
       }
       continue;
     }
-    // All of them: through LDS, where element 8 column + i is row i * columns + column of `tokens` tokens (adjacent lanes write adjacent rows).
+    // All of them: through LDS, where element 8 e + j is row j * (head_dim / 8) + e of `tokens` tokens (adjacent lanes write adjacent rows).
     unsigned char *tile = tiles[wave];
-    const int row_bytes = p.tokens * bytes;
+    const int row_bytes = p.tokens * bytes, eighths = d_all / 8;
     if (at.lane) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        unsigned char *w = tile + (i * p.columns + (at.d >> 3)) * row_bytes + at.group * 4 * bytes;
-        if (E4M3) {
-          const int sh = 8 * (i & 3);
-          *reinterpret_cast<unsigned *>(w) = (code[0][i >> 2] >> sh & 255) | (code[1][i >> 2] >> sh & 255) << 8 | (code[2][i >> 2] >> sh & 255) << 16 | (code[3][i >> 2] >> sh & 255) << 24;
-        } else {
-          unsigned h[4];
+      for (int i = 0; i < PARTS; ++i)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) h[k] = (i < 2 ? half[k].x : i < 4 ? half[k].y : i < 6 ? half[k].z : half[k].w) >> (16 * (i & 1)) & 0xffffu;
-          *reinterpret_cast<uint2v *>(w) = uint2v{h[0] | h[1] << 16, h[2] | h[3] << 16};
+        for (int j = 0; j < 8; ++j) {
+          unsigned char *w = tile + (j * eighths + (at.d[i] >> 3)) * row_bytes + at.group * TOKENS * bytes;
+          if constexpr (PAIRED) {
+            const unsigned both = element(0, i, j) | element(1, i, j) << (8 * bytes);
+            if (E4M3) *reinterpret_cast<unsigned short *>(w) = (unsigned short)both;
+            else *reinterpret_cast<unsigned *>(w) = both;
+          } else {
+            const unsigned low = element(0, i, j) | element(1, i, j) << (8 * bytes), high = element(2, i, j) | element(TOKENS - 1, i, j) << (8 * bytes);
+            if (E4M3) *reinterpret_cast<unsigned *>(w) = low | high << 16;
+            else *reinterpret_cast<uint2v *>(w) = uint2v{low, high};
+          }
         }
-      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int pieces = row_bytes >= 16 ? row_bytes / 16 : 1, wide = row_bytes / pieces;      // of a row: 16 bytes, or the eight that it has
     for (int u = lane; u < d_all * pieces; u += 64) {
       const int d = u / pieces, i = u - d * pieces;
-      const unsigned char *from = tile + ((d & 7) * p.columns + (d >> 3)) * row_bytes + i * wide;
+      const unsigned char *from = tile + ((d & 7) * eighths + (d >> 3)) * row_bytes + i * wide;
       unsigned char *w = to + ((long long)d * size + t0) * bytes + i * wide;
       if (wide == 16) *reinterpret_cast<uint4v *>(w) = *reinterpret_cast<const uint4v *>(from);
       else *reinterpret_cast<uint2v *>(w) = *reinterpret_cast<const uint2v *>(from);
@@ -305,9 +346,11 @@ int launch_kv_append(const KvParams &c, const __half *k, long long ldk, const __
                      __half *q_out, long long ldq_out, const Rotary &r, hipStream_t s) {
   AppendParams p{c, k, v, q, ldk, ldv, ldq, ldq_out, q_out, q_heads, 0, 1, 0, 1, 0, 1, 0, r};
   const int size = 1 << c.page_shift;
-  p.columns = c.head_dim / 8;
-  while (p.groups * 2 * p.columns <= 64 && p.groups * 8 <= size) p.groups *= 2;
-  p.tokens = 4 * p.groups;
+  const bool paired = !r.cos || (!r.interleaved && r.dim == c.head_dim);
+  const int each = paired ? 2 : 4;
+  p.columns = c.head_dim / (paired ? 16 : 8);
+  while (p.groups * 2 * p.columns <= 64 && p.groups * 2 * each <= size) p.groups *= 2;
+  p.tokens = each * p.groups;
   p.slots = (c.max_new + size - 2) / size + 1;
   // a wave to the tokens that it holds at a time, of those that a sequence can bring to a page
   const int most = c.max_new < size ? c.max_new : size;
@@ -317,8 +360,7 @@ int launch_kv_append(const KvParams &c, const __half *k, long long ldk, const __
   const long long q_waves = q ? (long long)c.n_seqs * p.q_tiles * q_heads : 0, blocks = kv_blocks + (q_waves + WAVES - 1) / WAVES;
   if (blocks > 0x7fffffff / WAVES) return VQ_ERR_SHAPE;
   p.kv_blocks = (int)kv_blocks;
-  const bool eights = !r.cos || (!r.interleaved && r.dim % 16 == 0);
-  auto kernel = c.e4m3 ? (eights ? kv_append_kernel<true, true> : kv_append_kernel<true, false>) : (eights ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
+  auto kernel = c.e4m3 ? (paired ? kv_append_kernel<true, true> : kv_append_kernel<true, false>) : (paired ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), 0, s, p);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }

@@ -319,3 +319,59 @@ def test_attention_on_a_stream_of_its_own(gpu_lib):
         got = gpu_lib.attention(qd, *dev.cache)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("lengths,news,q_heads,heads,dim,size,bits,window,sinks", [
+    ([200, 70], [4, 4], 8, 2, 128, 16, 8, 0, 0),
+    ([200, 70], [4, 4], 8, 2, 128, 16, 16, 0, 0),
+    ([150, 90], [7, 16], 2, 1, 64, 32, 16, 40, 3),
+    ([150, 90], [7, 16], 8, 2, 64, 64, 8, 40, 3),
+    ([300, 130], [130, 129], 4, 2, 128, 16, 8, 0, 0),
+    ([300, 130], [130, 129], 2, 2, 128, 64, 16, 70, 2),
+    ([300, 130], [130, 129], 2, 2, 64, 16, 16, 0, 0),
+    ([300], [300], 2, 1, 64, 128, 8, 90, 1),
+    ([90], [40], 2, 1, 80, 16, 16, 33, 2),
+])
+def test_keys_and_values_that_are_not_finite_reach_the_tokens_that_see_them_alone(gpu_lib, lengths, news, q_heads, heads, dim, size, bits, window, sinks):
+    """One token in the middle of the new ones of each sequence has a value that is NaN (in 16 bits also infinities, of one sign and of both), another a key:
+    tokens that do not see them get what they get without, bit for bit, the others what the sums give."""
+    import torch
+    rng, cache, table, k, v, q = _problem(16, lengths, news, q_heads, heads, dim, size, bits)
+    args = dict(max_new=max(news), window=window, sinks=sinks)
+
+    def run(k, v):
+        import copy
+        mine = copy.deepcopy(cache)
+        with np.errstate(invalid="ignore", over="ignore"):
+            mine.append(k, v, table, lengths, news)
+        dev = Device(mine, table, lengths, news)
+        out, lse = gpu_lib.attention(torch.from_numpy(q).cuda(), *dev.cache, starts=dev.starts, return_lse=True, **args)
+        torch.cuda.synchronize()
+        return out.cpu().numpy(), lse.cpu().numpy()
+    want, want_lse = run(k, v)
+    rows = [0] + list(np.cumsum(news))
+    for what, kinds in (("value", [np.nan] if bits == 8 else [np.nan, np.inf, -np.inf, None]), ("key", [np.nan])):
+        for kind in kinds:
+            k2, v2, hit = k.copy(), v.copy(), np.zeros((len(q), dim), bool)
+            for b, (length, new) in enumerate(zip(lengths, news)):
+                t = new // 2
+                places = (t, t + 1) if kind is None else (t,)
+                for place in places:
+                    if place >= new:
+                        continue
+                    sign = kind if kind is not None else (np.inf if place == t else -np.inf)
+                    (v2 if what == "value" else k2)[rows[b] + place, 0, dim // 2 + 1] = sign
+                    for u in range(new):
+                        at, j = length - new + u, length - new + place
+                        if j <= at and (not window or j > at - window or j < sinks):
+                            hit[rows[b] + u, dim // 2 + 1 if what == "value" else slice(None)] = True
+            got, lse = run(k2, v2)
+            group = q_heads // heads
+            hit = np.repeat(hit[:, None, :], q_heads, 1)
+            hit[:, group:] = False                                  # other key heads are not touched
+            # (in 8 bits a page's scale is that of its finite elements, of which one is gone: the others' codes may differ where it was the largest)
+            same = got.view(np.uint16)[~hit] == want.view(np.uint16)[~hit]
+            assert same.all(), (what, kind, (~same).sum())
+            assert not np.isfinite(got[hit]).any(), (what, kind)
+            if kind is not None and np.isinf(kind):
+                assert (got[hit] == kind).all()
