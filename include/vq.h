@@ -306,7 +306,7 @@ typedef enum vq_kv_type { VQ_KV_FP16 = 0, VQ_KV_E4M3 = 1 } vq_kv_type;
 typedef struct vq_kv_desc {
   uint32_t struct_size;                    /* = sizeof(vq_kv_desc)                                         */
   int32_t type;                            /* vq_kv_type                                                   */
-  int32_t kv_heads, head_dim;              /* >= 1; head_dim a multiple of 16, at most 256                 */
+  int32_t kv_heads, head_dim;              /* 1 .. 65535 (query heads too); a multiple of 16, at most 256  */
   int32_t page_tokens;                     /* 16, 32, 64, 128 or 256                                       */
   int32_t n_pages;                         /* pages in the pool                                            */
   int32_t n_seqs, n_tokens;                /* sequences and new tokens of this call                        */
@@ -351,8 +351,8 @@ int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void
  * Scores, statistics and sums are binary32; the probabilities (relative to the largest so far) are rounded to binary16 for the matrix cores, the result once.
  * Keys and values nobody sees may hold anything, NaN included.  softmax_scale must be finite and positive.
  * Workspace (device memory, 256-byte aligned, contents undefined afterwards): with vq_attention_workspace_bytes bytes a
- * sequence's keys are cut into parts where that fills the chip, and a second kernel joins them; with less or NULL each
- * sequence's keys are taken in one part.  Results are deterministic run to run for the same sizes and workspace.  */
+ * sequence's keys are cut into parts where that is faster (judged by the descriptor's sizes alone), and a second kernel joins them;
+ * with less or NULL each sequence's keys are taken in one part.  Results are deterministic run to run for the same sizes and workspace.  */
 size_t vq_attention_workspace_bytes(const vq_kv_desc *cache, int32_t q_heads, int32_t window, int32_t sinks);
 int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, int32_t window, int32_t sinks,
                  void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);

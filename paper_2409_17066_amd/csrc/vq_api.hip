@@ -374,7 +374,7 @@ int make_kv_params(const vq_kv_desc *d, KvParams *p) {
   if (d->struct_size != sizeof(vq_kv_desc) || d->reserved != 0) return VQ_ERR_SHAPE;
   if (d->type != VQ_KV_FP16 && d->type != VQ_KV_E4M3) return VQ_ERR_SHAPE;
   const bool e4m3 = d->type == VQ_KV_E4M3;
-  if (d->kv_heads < 1 || d->kv_heads > 65536 || d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16 != 0) return VQ_ERR_SHAPE;
+  if (d->kv_heads < 1 || d->kv_heads > 65535 || d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16 != 0) return VQ_ERR_SHAPE;
   int shift = 4;
   while (shift < 8 && (1 << shift) != d->page_tokens) ++shift;
   if ((1 << shift) != d->page_tokens) return VQ_ERR_SHAPE;
@@ -402,11 +402,11 @@ int make_kv_params(const vq_kv_desc *d, KvParams *p) {
 
 // Query heads, window and first tokens of a call of vq_attention.
 static int make_attention_params(const KvParams &c, int32_t q_heads, int32_t window, int32_t sinks, AttentionParams *a) {
-  if (q_heads < 1 || q_heads > 65536 || q_heads % c.kv_heads != 0 || window < 0 || sinks < 0) return VQ_ERR_SHAPE;
+  if (q_heads < 1 || q_heads > 65535 || q_heads % c.kv_heads != 0 || window < 0 || sinks < 0) return VQ_ERR_SHAPE;
   *a = AttentionParams{};
   a->q_heads = q_heads; a->group = q_heads / c.kv_heads;
   a->by_group = a->group > 1 ? (unsigned)((1ull << 32) / a->group) + 1 : 0;
-  if ((long long)c.max_new * a->group * a->group >= 1ll << 31) return VQ_ERR_SHAPE;          // (by_group is good for so many rows)
+  if ((long long)c.max_new * a->group * a->group >= 1ll << 30) return VQ_ERR_SHAPE;          // (by_group is good for so many rows and more)
   a->window = window; a->sinks = window ? sinks : 0;
   return VQ_OK;
 }
@@ -421,7 +421,7 @@ extern "C" int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk,
   if (!k || !v || (q && !q_out)) return VQ_ERR_NULL;
   const long long kv_width = (long long)c.kv_heads * c.head_dim;
   if (ldk < kv_width || ldv < kv_width) return VQ_ERR_SHAPE;
-  if (q && (q_heads < 1 || q_heads > 65536 || ldq < (long long)q_heads * c.head_dim || ldq_out < (long long)q_heads * c.head_dim)) return VQ_ERR_SHAPE;
+  if (q && (q_heads < 1 || q_heads > 65535 || ldq < (long long)q_heads * c.head_dim || ldq_out < (long long)q_heads * c.head_dim)) return VQ_ERR_SHAPE;
   if (!aligned(k, 2) || !aligned(v, 2) || (q && (!aligned(q, 2) || !aligned(q_out, 2)))) return VQ_ERR_ALIGNMENT;
   vq::Rotary r{};
   if (rotary) {

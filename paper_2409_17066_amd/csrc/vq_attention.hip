@@ -102,42 +102,67 @@ struct Plan {
   size_t o_bytes, ml_bytes;
 };
 
-Plan plan_of(const KvParams &c, const AttentionParams &a) {
-  Plan p{0, 1, false, 0, 0};
-  if (c.head_dim != 64 && c.head_dim != 128) return p;
-  const long long rows = (long long)c.max_new * a.group;
-  p.prompt = rows > 64;
-  p.tile_rows = p.prompt ? attention_prompt_rows() : attention_decode_rows(c, a);
-  const long long seen = a.window > 0 ? std::min<long long>(c.max_length, (long long)a.window + a.sinks + p.tile_rows / a.group + 64) : c.max_length;
-  const long long chunks = (seen + 63) / 64, groups = (long long)c.n_seqs * c.kv_heads * ((rows + p.tile_rows - 1) / p.tile_rows);
-  // Parts until there is a workgroup to a compute unit (of the prompt kernel two), of two runs at least: a second launch costs about 4 us.
-  const long long wanted = std::min((p.prompt ? 2LL : 1LL) * cu_count() / groups, chunks / (2 * RUN));
-  p.parts = (int)std::max(1LL, std::min(wanted, 64LL));
-  if (p.parts > 1) {
-    p.o_bytes = (size_t)c.n_seqs * c.kv_heads * p.parts * rows * c.head_dim * 4;
-    p.ml_bytes = (size_t)c.n_seqs * c.kv_heads * p.parts * rows * 8;
+// The kernel and number of parts whose time is estimated the least, in us, from measurements on heads of 64 and 128 elements, 8 and 16 bits, 8 and 32 key heads,
+// 1 to 16 sequences of 1024 to 32768 tokens with 16 to 256 rows a key head:
+//   decode: a workgroup to a compute unit, rounds of 3.2 us for eight chunks of 16 KB (more bytes take longer, and more rows more workgroups) behind 9 us;
+//   prompt: two to a compute unit, 1.3 us a chunk of both for up to 32 rows and 0.6 more for each further 32 of 128, behind 12 us, and where there is one
+//   alone 1.3 and 0.1 (half of that for 64 elements);
+// and for parts the second launch that joins them, 5 us and what it moves.  Measured (64 query and 8 key heads of 128 elements, 8 bits, us by the decode and by
+// the prompt kernel): 16 sequences of 4096 tokens 32 and 38 for 32 rows a key head, 59 and 49 for 64, 218 and 99 for 256; one of 1024 tokens 13 and 16 for 32
+// rows, 13 and 19 for 256.  Parts (16 rows): 4 sequences of 2048 tokens 17 in one and 14 in four, one of 1024 13 in one and 14 in two.
+Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
+  Plan best{0, 1, false, 0, 0};
+  if (c.head_dim != 64 && c.head_dim != 128) return best;
+  const long long rows = (long long)c.max_new * a.group, slots = cu_count();
+  float least = 0.f;
+  for (const bool prompt : {false, true}) {
+    if (!prompt && rows > 512) continue;
+    const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(c, a), run = prompt ? PROMPT_RUN : DECODE_RUN;
+    // tokens that a tile's rows look at: a window's and the first ones, or on the average all before half of the new ones
+    const long long all = c.max_length - (rows > tile ? c.max_new / 2 : 0), reach = a.window > 0 ? (long long)a.window + a.sinks + tile / a.group + 64 : all;
+    const long long chunks = (std::max(std::min(all, reach), 1LL) + 63) / 64, groups = (long long)c.n_seqs * c.kv_heads * ((rows + tile - 1) / tile);
+    const float quarters = (float)std::min((rows + 31) / 32, 4LL), size = (float)c.head_dim / 128.f;
+    const long long most = parts_allowed ? std::min((chunks + run - 1) / run, 64LL) : 1;
+    for (long long parts = 1;; parts *= 2) {
+      parts = std::min(parts, most);
+      const float rounds = std::max((float)(groups * parts) / (float)((prompt ? 2 : 1) * slots), 1.f), runs = (float)(((chunks + run - 1) / run + parts - 1) / parts);
+      const float step = !prompt ? 3.2f * size * (c.e4m3 ? 1.f : 2.f) : run * size * (groups * parts > slots ? 0.7f + 0.6f * quarters : 1.2f + 0.1f * quarters);
+      const float join = parts > 1 ? 5.f + (float)(c.n_seqs * parts * c.kv_heads * rows) * size * 1024.f / 4.5e6f : 0.f;
+      const float time = (prompt ? 12.f : 9.f) + join + rounds * runs * step;
+      if (least == 0.f || time < least) {
+        least = time;
+        best.tile_rows = tile;
+        best.parts = (int)parts;
+        best.prompt = prompt;
+      }
+      if (parts == most) break;
+    }
   }
-  return p;
+  if (best.parts > 1) {
+    best.o_bytes = (size_t)c.n_seqs * c.kv_heads * best.parts * rows * c.head_dim * 4;
+    best.ml_bytes = (size_t)c.n_seqs * c.kv_heads * best.parts * rows * 8;
+  }
+  return best;
 }
 
 }  // namespace
 
 size_t attention_workspace_bytes(const KvParams &c, const AttentionParams &a) {
-  const Plan p = plan_of(c, a);
+  const Plan p = plan_of(c, a, true);
   return (p.o_bytes + p.ml_bytes + 255) / 256 * 256;
 }
 
 int launch_attention(const KvParams &c, const AttentionParams &a, void *workspace, size_t workspace_bytes, hipStream_t s) {
-  const Plan p = plan_of(c, a);
+  Plan p = plan_of(c, a, true);
+  if (p.parts > 1 && workspace_bytes < p.o_bytes + p.ml_bytes) p = plan_of(c, a, false);
   if (p.tile_rows) {
-    const bool room = p.parts > 1 && workspace_bytes >= p.o_bytes + p.ml_bytes;
     float *o = static_cast<float *>(workspace);
-    const Split split{room ? p.parts : 1, o, room ? o + p.o_bytes / 4 : nullptr};
+    const Split split{p.parts, p.prompt ? PROMPT_RUN : DECODE_RUN, o, p.parts > 1 ? o + p.o_bytes / 4 : nullptr};
     const int rc = p.prompt ? launch_attention_prompt(c, a, split, s) : launch_attention_decode(c, a, split, s);
-    return rc != VQ_OK || !room ? rc : launch_attention_join(c, a, split, p.tile_rows, s);
+    return rc != VQ_OK || p.parts == 1 ? rc : launch_attention_join(c, a, split, p.tile_rows, s);
   }
   const long long blocks = (long long)c.n_seqs * c.max_new * a.q_heads;
-  if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
+  if (blocks > 0xffffffffll / 64) return VQ_ERR_SHAPE;
   if (c.e4m3) hipLaunchKernelGGL((attention_wave_kernel<true>), dim3((unsigned)blocks), dim3(64), 0, s, c, a);
   else hipLaunchKernelGGL((attention_wave_kernel<false>), dim3((unsigned)blocks), dim3(64), 0, s, c, a);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;

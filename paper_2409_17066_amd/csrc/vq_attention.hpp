@@ -4,14 +4,15 @@
 
 namespace vq {
 
-// How a sequence's keys are cut into parts: part p takes every `parts`-th run of eight chunks of 64 keys from run p on, so that what a workgroup looks at
-// first does not depend on the sequence's length.
-constexpr int RUN = 8;
+// How a sequence's keys are cut into parts: part p takes every `parts`-th run of `run` chunks of 64 keys (a power of two) from run p on, so that what a workgroup
+// looks at first does not depend on the sequence's length.
 struct Split {
-  int parts;
+  int parts, run;
   float *o, *ml;               // partial outputs [seq][kv head][part][row][head_dim], maxima and sums [seq][kv head][part][row][2]
 };
 
+// Chunks of a run, one for each wave of the decode kernel.
+constexpr int DECODE_RUN = 8, PROMPT_RUN = 4;
 // Rows of a key head to a workgroup of launch_attention_decode.
 int attention_decode_rows(const KvParams &c, const AttentionParams &a);
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
@@ -40,7 +41,7 @@ __device__ __forceinline__ Span span_of(const AttentionParams &a, const Sequence
   return v;
 }
 // Parts that have chunks, one at least.
-__device__ __forceinline__ int parts_of(const Split &s, int chunks) { return max(min(s.parts, (chunks + RUN - 1) / RUN), 1); }
+__device__ __forceinline__ int parts_of(const Split &s, int chunks) { return max(min(s.parts, (chunks + s.run - 1) / s.run), 1); }
 
 // Maximum and sum over the four rows of sixteen lanes, in every lane.  (The exchanged words are named before they are reinterpreted: a bit cast of
 // a vector's element was compiled as that of its first.)

@@ -13,7 +13,7 @@ namespace vq {
 
 namespace {
 
-constexpr int WAVES = RUN;
+constexpr int WAVES = DECODE_RUN;
 
 // RT: tiles of sixteen rows; D: elements of a head; MANY: rows may be of several new tokens, which see different keys.
 template <bool E4M3, int D, int RT, bool MANY>
@@ -23,11 +23,12 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
   constexpr bool AHEAD = !MANY || E4M3 || D == 64;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  const int part = (int)blockIdx.z, kv_head = (int)blockIdx.y, b = tiles > 1 ? (int)blockIdx.x / tiles : (int)blockIdx.x, tile = tiles > 1 ? (int)blockIdx.x % tiles : 0;
+  // (tiles of the same keys a multiple of all key heads apart: on the same XCD where those are a multiple of eight)
+  const int b = (int)blockIdx.x, kv_head = (int)blockIdx.y, part = tiles > 1 ? (int)blockIdx.z / tiles : (int)blockIdx.z, tile = tiles > 1 ? (int)blockIdx.z % tiles : 0;
   const int shift = c.page_shift, mask = (1 << shift) - 1;
   // Entries of the page table for places [of, of + 16).  Without a window the first ones do not depend on the sequence's length, and are asked for beside it.
   auto entry = [&](int of) { return of >> shift < c.table_pages ? c.page_table[b * c.table_stride + (of >> shift)] : -1; };
-  int i = part * RUN + wave, k_entry = 0, v_entry = 0;
+  int i = part * WAVES + wave, k_entry = 0, v_entry = 0;
   float *ml = lds, *out = lds + 2 * 16 * WAVES, *put_back = out;      // (a wave's first part of put_back is read before its results take the place)
   bool any_odd = false;
   if (a.window == 0) {
@@ -38,7 +39,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
   const int rows = s.rows * a.group, row0 = tile * 16 * RT, here = min(rows - row0, 16 * RT);
   if (here <= 0) return;
   const Span span = span_of(a, s, row0, 16 * RT);
-  const int begin = part * RUN, end = span.chunks, stride = split.parts * RUN;
+  const int begin = part * WAVES, end = span.chunks, stride = split.parts * WAVES;
   if (part > 0 && begin >= end) return;
   const int active = min(max(end - begin, 0), WAVES);            // waves that have a chunk
   if (a.window != 0 && i < end) {
@@ -365,11 +366,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvPa
 template <bool E4M3, int D, int RT, bool MANY>
 int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
   const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT);
-  const long long blocks = (long long)tiles * c.n_seqs;
-  if (blocks > 0x7fffffff / 512 || c.kv_heads > 65535) return VQ_ERR_SHAPE;
+  if (c.n_seqs > 0x7fffffff / 512 || (long long)tiles * s.parts > 65535) return VQ_ERR_SHAPE;
   const int lds = (2 * 16 + 16 * (D + 4) * (MANY ? RT : 1)) * WAVES * 4 + (MANY ? WAVES * Odd<E4M3>::KINDS * D * 8 : 0);
   VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT, MANY>));
-  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY>), dim3((unsigned)blocks, c.kv_heads, s.parts), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
+  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY>), dim3(c.n_seqs, c.kv_heads, tiles * s.parts), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 
@@ -397,7 +397,7 @@ int launch_attention_decode(const KvParams &c, const AttentionParams &a, const S
 
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream) {
   const dim3 blocks(c.max_new * a.group, c.kv_heads, c.n_seqs);
-  if (c.kv_heads > 65535 || c.n_seqs > 65535) return VQ_ERR_SHAPE;
+  if (c.n_seqs > 65535) return VQ_ERR_SHAPE;
   if (c.head_dim == 64) hipLaunchKernelGGL((attention_join_kernel<64>), blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
   else hipLaunchKernelGGL((attention_join_kernel<128>), blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;

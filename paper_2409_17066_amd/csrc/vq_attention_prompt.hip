@@ -63,10 +63,10 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   const int rows = s.rows * a.group, row0 = tile * ROWS;
   if (row0 >= rows) return;
   const Span span = span_of(a, s, row0, ROWS);
-  // chunks of this part: runs of RUN, every split.parts-th
-  if (part > 0 && part * RUN >= span.chunks) return;
-  const int jump = (split.parts - 1) * RUN;
-  auto following = [&](int chunk) { return chunk + 1 + ((chunk + 1) % RUN == 0 ? jump : 0); };
+  // chunks of this part: runs, every split.parts-th
+  if (part > 0 && part * split.run >= span.chunks) return;
+  const int jump = (split.parts - 1) * split.run, run_mask = split.run - 1;
+  auto following = [&](int chunk) { return chunk + 1 + (((chunk + 1) & run_mask) == 0 ? jump : 0); };
   auto first_of = [&](int chunk) { return (chunk < span.sink_chunks ? chunk : chunk + span.first - span.sink_chunks) * 64; };
 
   // this wave's rows
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   };
 
   // first places of the chunks that are computed, stored to LDS and looked up in the page table next
-  int chunk = part * RUN, j_now = first_of(chunk), j_next = 0, j_after = 0;
+  int chunk = part * split.run, j_now = first_of(chunk), j_next = 0, j_after = 0;
   const bool any = chunk < span.chunks;
   if (any) {
     entries(j_now);
