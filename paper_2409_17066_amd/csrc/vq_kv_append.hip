@@ -29,6 +29,7 @@ struct AppendParams {
 struct Eight {
   float e[8];
 };
+typedef short short2v __attribute__((ext_vector_type(2)));
 typedef float float4b __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ Eight widened(uint4v u) {
@@ -43,7 +44,8 @@ __device__ __forceinline__ Eight eight_of(const float *from) {
 
 // Pairs (a[i], b[i]) of elements j + i and dim / 2 + j + i, rotated.
 __device__ __forceinline__ void rotate_pairs(const Rotary &r, int at, int j, Eight &a, Eight &b) {
-  const Eight c = eight_of(r.cos + at * r.ld + j), s = eight_of(r.sin + at * r.ld + j);
+  const unsigned long long row = (unsigned long long)(unsigned)at * (unsigned long long)r.ld + j;
+  const Eight c = eight_of(r.cos + row), s = eight_of(r.sin + row);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float x = a.e[i], y = b.e[i];
@@ -91,15 +93,6 @@ __device__ __forceinline__ void rotate_eight(const Rotary &r, int at, const __ha
   }
 }
 
-__device__ __forceinline__ float largest(const Eight &x, float so_far) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float a = __builtin_fabsf(x.e[i]);
-    so_far = a <= 3.402823466e38f ? fmaxf(so_far, a) : so_far;       // (what is not finite does not take part)
-  }
-  return so_far;
-}
-
 // The smallest power of two S >= 2^-64 with amax <= 448 S: 448 is 1.75 * 2^8.
 __device__ __forceinline__ float scale_for(float amax) {
   const unsigned u = __builtin_bit_cast(unsigned, amax);
@@ -112,6 +105,12 @@ __device__ __forceinline__ float encodable(float x) { return __builtin_fabsf(x) 
 __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(encodable(a), encodable(b), 0, false);
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(encodable(c), encodable(d), w, true);
+}
+
+// Codes of the numbers over a power of two that makes them at most 448 in size; NaN stays NaN.
+__device__ __forceinline__ unsigned scaled_codes4(float a, float b, float c, float d, float scale) {
+  short2v w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(short2v{0, 0}, a, b, scale, false);
+  return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true));
 }
 
 // Four codes times the power of two `ratio` (at most 1), as codes again.
@@ -133,6 +132,42 @@ struct Share {
   static constexpr int TOKENS = PAIRED ? 2 : 4, PARTS = PAIRED ? 2 : 1;
   Eight y[TOKENS][PARTS];
 };
+// Largest size of the finite elements, `so_far` among them; odd: whether there are others.  (Three operations of the vector ALU for four elements but where
+// there are others.)
+__device__ __forceinline__ float max3_of_sizes(float so_far, float a, float b) {
+  float m;
+  asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(m) : "v"(so_far), "v"(a), "v"(b));
+  return m;
+}
+template <bool PAIRED>
+__device__ __forceinline__ float largest(const Share<PAIRED> &x, float so_far, bool &odd) {
+  float m = so_far;
+  bool nan = false;
+#pragma unroll
+  for (int k = 0; k < Share<PAIRED>::TOKENS; ++k)
+#pragma unroll
+    for (int i = 0; i < Share<PAIRED>::PARTS; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        const float a = x.y[k][i].e[j], b = x.y[k][i].e[j + 1];
+        nan |= __builtin_isunordered(a, b);
+        m = max3_of_sizes(m, a, b);
+      }
+  if (__builtin_expect(!__any(nan || m > 3.402823466e38f), 1)) return m;
+  odd = true;
+  m = so_far;
+#pragma unroll
+  for (int k = 0; k < Share<PAIRED>::TOKENS; ++k)
+#pragma unroll
+    for (int i = 0; i < Share<PAIRED>::PARTS; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float a = __builtin_fabsf(x.y[k][i].e[j]);
+        m = a <= 3.402823466e38f ? fmaxf(m, a) : m;
+      }
+  return m;
+}
+
 struct Place {
   int d[2], group;                                                  // elements of the parts
   bool lane;
@@ -143,20 +178,18 @@ __device__ __forceinline__ Place place_of(const AppendParams &p) {
   return Place{{d, d + p.c.head_dim / 2}, group, group < p.groups};
 }
 
-// A lane's tokens: rows row0 + t ... of x, where begin <= t < end, rotated if `turn`.
+// A lane's tokens: rows row0 + t ... of x, rotated if `turn`; the nearest of [begin, end) in place of others, so that nothing branches.
 template <bool PAIRED>
 __device__ __forceinline__ void take(const Rotary &r, const __half *x, long long ld, int row0, int place0, const Place &at, int t, int begin, int end, bool turn,
                                      Share<PAIRED> &s) {
 #pragma unroll
   for (int k = 0; k < Share<PAIRED>::TOKENS; ++k) {
-#pragma unroll
-    for (int i = 0; i < Share<PAIRED>::PARTS; ++i) s.y[k][i] = Eight{};
-    if (t + k < begin || t + k >= end) continue;
-    const __half *from = x + (row0 + t + k) * ld;
+    const int token = min(max(t + k, begin), end - 1);
+    const __half *from = x + (unsigned long long)(unsigned)(row0 + token) * (unsigned long long)ld;
 #pragma unroll
     for (int i = 0; i < Share<PAIRED>::PARTS; ++i) s.y[k][i] = widened(*reinterpret_cast<const uint4b *>(from + at.d[i]));
     if (!turn) continue;
-    const int row = min(max(r.position ? r.position[row0 + t + k] : place0 + t + k, 0), r.positions - 1);
+    const int row = min(max(r.position ? r.position[row0 + token] : place0 + token, 0), r.positions - 1);
     if constexpr (PAIRED) rotate_pairs(r, row, at.d[0], s.y[k][0], s.y[k][1]);
     else rotate_eight(r, row, from, at.d[0], s.y[k][0]);
   }
@@ -212,25 +245,20 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
   const int stride = p.tokens * p.team, start = (begin & -stride) + in_team * p.tokens;
   const int lane_end = at.lane ? end : 0;
   Share<PAIRED> held;
-  take<PAIRED>(p.r, x, ld, row0, place0, at, start + at.group * TOKENS, begin, lane_end, turn, held);
+  take<PAIRED>(p.r, x, ld, row0, place0, at, start + at.group * TOKENS, begin, end, turn, held);
   if (page < 0) return;                                                          // (the elements are on their way beside the page's number)
   unsigned char *to = (values ? c.v_pages + page * c.v_page_bytes : c.k_pages + page * c.k_page_bytes) + (long long)head * size * d_all * bytes;
   float *scale_at = (values ? c.v_scales : c.k_scales) + (E4M3 ? (long long)page * c.kv_heads + head : 0);
   const float before = E4M3 && begin > 0 ? *scale_at : 0.f;
-  float inverse = 1.f;
+  float scale = 1.f;
+  bool odd = false;                                                              // some element is not finite
   if (E4M3) {
     float amax = 0.f;
-    auto largest_of = [&](const Share<PAIRED> &x) {
-#pragma unroll
-      for (int k = 0; k < TOKENS; ++k)
-#pragma unroll
-        for (int i = 0; i < PARTS; ++i) amax = largest(x.y[k][i], amax);
-    };
-    largest_of(held);
+    amax = largest<PAIRED>(held, amax, odd);
     for (int t0 = start + stride; t0 < end; t0 += stride) {
       Share<PAIRED> more;
-      take<PAIRED>(p.r, x, ld, row0, place0, at, t0 + at.group * TOKENS, begin, lane_end, turn, more);
-      largest_of(more);
+      take<PAIRED>(p.r, x, ld, row0, place0, at, t0 + at.group * TOKENS, begin, end, turn, more);
+      amax = largest<PAIRED>(more, amax, odd);
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
@@ -239,10 +267,9 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
       __syncthreads();
       for (int w = 0; w < p.team; ++w) amax = fmaxf(amax, wave_max[wave - in_team + w]);
     }
-    const float scale = fmaxf(scale_for(amax), before);
-    inverse = 1.f / scale;
+    scale = fmaxf(scale_for(amax), before);
     if (begin > 0 && scale > before) {                                  // what the page holds already, in the new scale
-      const float ratio = before * inverse;
+      const float ratio = before / scale;
       const int me = in_team * 64 + lane, all = p.team * 64;
       if (values) {
         for (int u = me; u < d_all * begin; u += all) {
@@ -261,14 +288,19 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
   }
   for (int t0 = start; t0 < end; t0 += stride) {
     const int t = t0 + at.group * TOKENS;
-    if (t0 != start) take<PAIRED>(p.r, x, ld, row0, place0, at, t, begin, lane_end, turn, held);
+    if (t0 != start) take<PAIRED>(p.r, x, ld, row0, place0, at, t, begin, end, turn, held);
     uint4v word[TOKENS][PARTS];                                         // eight halfs, or in x and y eight codes
 #pragma unroll
     for (int k = 0; k < TOKENS; ++k)
 #pragma unroll
       for (int i = 0; i < PARTS; ++i) {
-        const Eight &y = held.y[k][i];
-        if (E4M3) word[k][i] = uint4v{codes4(y.e[0] * inverse, y.e[1] * inverse, y.e[2] * inverse, y.e[3] * inverse), codes4(y.e[4] * inverse, y.e[5] * inverse, y.e[6] * inverse, y.e[7] * inverse), 0, 0};
+        Eight &y = held.y[k][i];
+        if (E4M3) {
+          if (__builtin_expect(odd, 0))
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y.e[j] = __builtin_fabsf(y.e[j]) <= 3.402823466e38f ? y.e[j] : __builtin_nanf("");
+          word[k][i] = uint4v{scaled_codes4(y.e[0], y.e[1], y.e[2], y.e[3], scale), scaled_codes4(y.e[4], y.e[5], y.e[6], y.e[7], scale), 0, 0};
+        }
         else word[k][i] = halves8(y);
       }
     // element j of them
