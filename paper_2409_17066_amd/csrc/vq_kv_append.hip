@@ -1,12 +1,14 @@
 // New keys and values into a paged cache, and the rotation of queries and keys by their positions on the way.
 //
 // One launch.  A team of one, two or four waves takes one page, head and matrix (keys or values) that a sequence's new tokens reach, other waves take a head
-// of some queries.  Memory bounds it, and with fewer bytes on their way in each wave the chain from lengths to
-// page table to elements to scale does.  Every element is read once, rotated in binary32 and written once; in 8 bits the page's scale has to be known
-// before the first code is, so a lane keeps its first tokens in registers between the two, and reads what large pages hold beyond that again (from L2).
+// of some queries.  Memory bounds long prompts (four users' of 2624 tokens of 32 + 32 + 32 heads of 128 elements, 8 bits: 115 MB in 25.4 us, 4.5 TB/s, where a
+// large copy reaches 4.9), below that the chain from lengths to page table to elements to scale (one token: 4.2 us, of which an empty launch is half).  Every
+// element is read once, rotated in binary32 and written once; in 8 bits the page's scale has to be known
+// before the first code is, so a lane keeps its tokens in registers between the two; of pages that hold more than a team's lanes it reads them again (from L2).
 // A lane takes 32 elements at a time: of two tokens eight elements and the eight half a head further on, so that what it rotates are pairs and a token's
-// cosines and sines are read once for both (half the loads through L1 of one half each: prompts of four users, 2624 tokens of 32 + 32 + 32 heads, 40 ->
-// 31 us), or, where the rotation pairs other elements, eight elements of four tokens.
+// cosines and sines are read once for both (half the loads through L1 of one half each: those prompts 40 -> 31 us), or, where the rotation pairs
+// other elements, eight elements of four tokens.  Conversions that scale, and maxima of three at a time: 31 -> 29; 66 registers, and so seven
+// waves a SIMD, by not keeping addresses from round to round: 29 -> 25.
 #include "vq_kv.hpp"
 
 namespace vq {
@@ -22,7 +24,7 @@ struct AppendParams {
   __half *q_out;
   int q_heads, slots, team;                   // pages a sequence can reach; waves of a team
   int kv_blocks, q_tiles;                     // workgroups for keys and values; waves for one head of a sequence's queries
-  int columns, groups, tokens;                // lanes of a token, groups of tokens of a wave, tokens of a wave at a time
+  int columns, by_columns, groups, tokens;    // lanes of a token (and 2^16 over them, rounded up), groups of tokens of a wave, tokens of a wave at a time
   Rotary r;
 };
 
@@ -169,13 +171,14 @@ __device__ __forceinline__ float largest(const Share<PAIRED> &x, float so_far, b
 }
 
 struct Place {
-  int d[2], group;                                                  // elements of the parts
+  int d0, half, group;                                              // elements of the parts: d0 and half a head further
   bool lane;
+  __device__ __forceinline__ int d(int part) const { return d0 + part * half; }
 };
 template <bool PAIRED>
 __device__ __forceinline__ Place place_of(const AppendParams &p) {
-  const int lane = (int)threadIdx.x & 63, group = lane / p.columns, d = (lane - group * p.columns) * 8;
-  return Place{{d, d + p.c.head_dim / 2}, group, group < p.groups};
+  const int lane = (int)threadIdx.x & 63, group = lane * p.by_columns >> 16, d = (lane - group * p.columns) * 8;
+  return Place{d, p.c.head_dim / 2, group, group < p.groups};
 }
 
 // A lane's tokens: rows row0 + t ... of x, rotated if `turn`; the nearest of [begin, end) in place of others, so that nothing branches.
@@ -187,11 +190,11 @@ __device__ __forceinline__ void take(const Rotary &r, const __half *x, long long
     const int token = min(max(t + k, begin), end - 1);
     const __half *from = x + (unsigned long long)(unsigned)(row0 + token) * (unsigned long long)ld;
 #pragma unroll
-    for (int i = 0; i < Share<PAIRED>::PARTS; ++i) s.y[k][i] = widened(*reinterpret_cast<const uint4b *>(from + at.d[i]));
+    for (int i = 0; i < Share<PAIRED>::PARTS; ++i) s.y[k][i] = widened(*reinterpret_cast<const uint4b *>(from + at.d(i)));
     if (!turn) continue;
     const int row = min(max(r.position ? r.position[row0 + token] : place0 + token, 0), r.positions - 1);
-    if constexpr (PAIRED) rotate_pairs(r, row, at.d[0], s.y[k][0], s.y[k][1]);
-    else rotate_eight(r, row, from, at.d[0], s.y[k][0]);
+    if constexpr (PAIRED) rotate_pairs(r, row, at.d0, s.y[k][0], s.y[k][1]);
+    else rotate_eight(r, row, from, at.d0, s.y[k][0]);
   }
 }
 
@@ -210,11 +213,11 @@ __device__ __forceinline__ void append_queries(const AppendParams &p, int wave) 
   for (int k = 0; k < q.TOKENS; ++k)
 #pragma unroll
     for (int i = 0; i < q.PARTS; ++i)
-      if (t + k < s.rows) *reinterpret_cast<uint4b *>(p.q_out + (s.row0 + t + k) * p.ldq_out + from + at.d[i]) = halves8(q.y[k][i]);
+      if (t + k < s.rows) *reinterpret_cast<uint4b *>(p.q_out + (s.row0 + t + k) * p.ldq_out + from + at.d(i)) = halves8(q.y[k][i]);
 }
 
 template <bool E4M3, bool PAIRED>
-__global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_kernel(const AppendParams p) {
+__global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 5 : 2) void kv_append_kernel(const AppendParams p) {
   __shared__ float wave_max[WAVES];
   __shared__ __attribute__((aligned(16))) unsigned char tiles[WAVES][WAVE_LDS];
   const KvParams &c = p.c;
@@ -256,9 +259,8 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
     float amax = 0.f;
     amax = largest<PAIRED>(held, amax, odd);
     for (int t0 = start + stride; t0 < end; t0 += stride) {
-      Share<PAIRED> more;
-      take<PAIRED>(p.r, x, ld, row0, place0, at, t0 + at.group * TOKENS, begin, end, turn, more);
-      amax = largest<PAIRED>(more, amax, odd);
+      take<PAIRED>(p.r, x, ld, row0, place0, at, t0 + at.group * TOKENS, begin, end, turn, held);
+      amax = largest<PAIRED>(held, amax, odd);
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m));
@@ -286,9 +288,12 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
     }
     if (in_team == 0 && lane == 0 && !(begin > 0 && scale == before)) *scale_at = scale;
   }
+  const Place mine = at;
   for (int t0 = start; t0 < end; t0 += stride) {
+    Place at = mine;
+    asm volatile("" : "+v"(at.d0), "+v"(at.group));                     // (what follows from them is not kept from round to round: registers)
     const int t = t0 + at.group * TOKENS;
-    if (t0 != start) take<PAIRED>(p.r, x, ld, row0, place0, at, t, begin, end, turn, held);
+    if (E4M3 ? start + stride < end : t0 != start) take<PAIRED>(p.r, x, ld, row0, place0, at, t, begin, end, turn, held);
     uint4v word[TOKENS][PARTS];                                         // eight halfs, or in x and y eight codes
 #pragma unroll
     for (int k = 0; k < TOKENS; ++k)
@@ -315,8 +320,8 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
         if (t + k < begin || t + k >= lane_end) continue;
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) {
-          if (E4M3) *reinterpret_cast<uint2v *>(to + (t + k) * d_all + at.d[i]) = uint2v{word[k][i].x, word[k][i].y};
-          else *reinterpret_cast<uint4v *>(to + ((t + k) * d_all + at.d[i]) * 2) = word[k][i];
+          if (E4M3) *reinterpret_cast<uint2v *>(to + (t + k) * d_all + at.d(i)) = uint2v{word[k][i].x, word[k][i].y};
+          else *reinterpret_cast<uint4v *>(to + ((t + k) * d_all + at.d(i)) * 2) = word[k][i];
         }
       }
       continue;
@@ -330,7 +335,7 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
         for (int i = 0; i < PARTS; ++i)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int at_element = (at.d[i] + j) * size + t + k;
+            const int at_element = (at.d(i) + j) * size + t + k;
             if (E4M3) to[at_element] = (unsigned char)element(k, i, j);
             else reinterpret_cast<unsigned short *>(to)[at_element] = (unsigned short)element(k, i, j);
           }
@@ -345,7 +350,7 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
       for (int i = 0; i < PARTS; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          unsigned char *w = tile + (j * eighths + (at.d[i] >> 3)) * row_bytes + at.group * TOKENS * bytes;
+          unsigned char *w = tile + (j * eighths + (at.d(i) >> 3)) * row_bytes + at.group * TOKENS * bytes;
           if constexpr (PAIRED) {
             const unsigned both = element(0, i, j) | element(1, i, j) << (8 * bytes);
             if (E4M3) *reinterpret_cast<unsigned short *>(w) = (unsigned short)both;
@@ -376,11 +381,12 @@ __global__ __launch_bounds__(64 * WAVES, PAIRED && E4M3 ? 4 : 2) void kv_append_
 
 int launch_kv_append(const KvParams &c, const __half *k, long long ldk, const __half *v, long long ldv, const __half *q, long long ldq, int q_heads,
                      __half *q_out, long long ldq_out, const Rotary &r, hipStream_t s) {
-  AppendParams p{c, k, v, q, ldk, ldv, ldq, ldq_out, q_out, q_heads, 0, 1, 0, 1, 0, 1, 0, r};
+  AppendParams p{c, k, v, q, ldk, ldv, ldq, ldq_out, q_out, q_heads, 0, 1, 0, 1, 0, 0, 1, 0, r};
   const int size = 1 << c.page_shift;
   const bool paired = !r.cos || (!r.interleaved && r.dim == c.head_dim);
   const int each = paired ? 2 : 4;
   p.columns = c.head_dim / (paired ? 16 : 8);
+  p.by_columns = 65535 / p.columns + 1;
   while (p.groups * 2 * p.columns <= 64 && p.groups * 2 * each <= size) p.groups *= 2;
   p.tokens = each * p.groups;
   p.slots = (c.max_new + size - 2) / size + 1;
