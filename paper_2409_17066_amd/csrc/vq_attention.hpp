@@ -13,10 +13,13 @@ struct Split {
 
 // Chunks of a run, one for each wave of the decode kernel.
 constexpr int DECODE_RUN = 8, PROMPT_RUN = 4;
-// Rows of a key head to a workgroup of launch_attention_decode.
+int attention_decode_run(const KvParams &c);                       // DECODE_RUN, or half of it
+// The decode kernel, which takes every head: rows of a key head to a workgroup.
 int attention_decode_rows(const KvParams &c, const AttentionParams &a);
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
+// The prompt kernel: rows of a key head to a workgroup, and whether it takes heads of this size.
 int attention_prompt_rows();
+bool attention_prompt_takes(const KvParams &c);
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
 

@@ -13,18 +13,22 @@ namespace vq {
 
 namespace {
 
-constexpr int WAVES = DECODE_RUN;
+// Waves of a workgroup: as many as have room in LDS for what they join.
+constexpr int waves_of(bool e4m3, int dim) { return !e4m3 && dim > 192 ? DECODE_RUN / 2 : DECODE_RUN; }
 
-// RT: tiles of sixteen rows; D: elements of a head; MANY: rows may be of several new tokens, which see different keys.
-template <bool E4M3, int D, int RT, bool MANY>
-__global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles) {
+// RT: tiles of sixteen rows; D: elements of a head, or (not EXACT) the next multiple of 64, zeros behind the head's own; MANY: rows may be of several new
+// tokens, which see different keys.
+template <bool E4M3, int D, int RT, bool MANY, bool EXACT>
+__global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int tile0) {
+  constexpr int WAVES = waves_of(E4M3, D);
+  const int dim = EXACT ? D : c.head_dim;
   constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
   // The next chunk is loaded ahead where there are registers for it beside those of the rows' differences.
-  constexpr bool AHEAD = !MANY || E4M3 || D == 64;
+  constexpr bool AHEAD = !MANY || D == 64 || (E4M3 && D <= 128), V_AHEAD = D <= 128;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   // (tiles of the same keys a multiple of all key heads apart: on the same XCD where those are a multiple of eight)
-  const int b = (int)blockIdx.x, kv_head = (int)blockIdx.y, part = tiles > 1 ? (int)blockIdx.z / tiles : (int)blockIdx.z, tile = tiles > 1 ? (int)blockIdx.z % tiles : 0;
+  const int b = (int)blockIdx.x, kv_head = (int)blockIdx.y, part = tiles > 1 ? (int)blockIdx.z / tiles : (int)blockIdx.z, tile = tile0 + (tiles > 1 ? (int)blockIdx.z % tiles : 0);
   const int shift = c.page_shift, mask = (1 << shift) - 1;
   // Entries of the page table for places [of, of + 16).  Without a window the first ones do not depend on the sequence's length, and are asked for beside it.
   auto entry = [&](int of) { return of >> shift < c.table_pages ? c.page_table[b * c.table_stride + (of >> shift)] : -1; };
@@ -54,10 +58,13 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
   for (int rt = 0; rt < RT; ++rt) {
     const int r = min(row0 + rt * 16 + n, rows - 1), t = token_of(a, r);
     place[rt] = s.first + t;
-    const __half *x = a.q + (s.row0 + t) * a.ldq + ((long long)kv_head * a.group + r - t * a.group) * D;
+    const __half *x = a.q + (s.row0 + t) * a.ldq + ((long long)kv_head * a.group + r - t * a.group) * dim;
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i)
-      q[rt][i] = __builtin_bit_cast(half8v, (uint4v)*reinterpret_cast<const uint4b *>(x + (E4M3 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 32 + g * 8)));
+    for (int i = 0; i < STEPS; ++i) {
+      const int at = E4M3 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 32 + g * 8;
+      const uint4v w = *reinterpret_cast<const uint4b *>(x + (EXACT || at < dim ? at : 0));
+      q[rt][i] = __builtin_bit_cast(half8v, EXACT || at < dim ? w : uint4v{0, 0, 0, 0});
+    }
   }
 
   float m[RT], l[RT];
@@ -76,6 +83,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
     return there ? entry : 0;
   };
   uint4v k[4][KL], v[DT][VL];
+  auto has = [&](int dt) { return EXACT || dt * 16 < dim; };       // whether the head has elements 16 dt ... 16 dt + 15
   float k_scale = 1.f, v_scale = 1.f;
   bool v_there = false;
   auto entries_of = [&](int i) {
@@ -86,32 +94,37 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
     const int j = span.chunk(i) * 64 + 16 * (n >> 2);
     bool there;
     const int page = page_at(j, k_entry, there);
-    const unsigned char *from = c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask) + (n & 3)) * (D * BYTES) + g * 16;
+    const unsigned char *from = c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask) + (n & 3)) * (dim * BYTES) + g * 16;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int w = 0; w < KL; ++w) k[t][w] = *reinterpret_cast<const uint4v *>(from + t * 4 * D * BYTES + w * 64);
+      for (int w = 0; w < KL; ++w) {
+        const bool mine = EXACT || w * 64 + g * 16 < dim * BYTES;
+        const uint4v x = *reinterpret_cast<const uint4v *>(from + t * 4 * dim * BYTES + (mine ? w * 64 : 0));
+        k[t][w] = mine ? x : uint4v{0, 0, 0, 0};
+      }
     if (E4M3) k_scale = c.k_scales[(long long)page * c.kv_heads + kv_head];
   };
   auto load_v = [&](int i) {
     const int j = span.chunk(i) * 64 + 16 * g;
     const int page = page_at(j, v_entry, v_there);
-    const unsigned char *from = c.v_pages + page * c.v_page_bytes + (((((long long)kv_head * D + n) << shift) + (j & mask)) * BYTES);
+    const unsigned char *from = c.v_pages + page * c.v_page_bytes + (((((long long)kv_head * dim + n) << shift) + (j & mask)) * BYTES);
     const int step = 16 * BYTES << shift;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int w = 0; w < VL; ++w) v[dt][w] = *reinterpret_cast<const uint4v *>(from + dt * step + w * 16);
+      for (int w = 0; w < VL; ++w) v[dt][w] = has(dt) ? *reinterpret_cast<const uint4v *>(from + dt * step + w * 16) : uint4v{0, 0, 0, 0};
     if (E4M3) v_scale = v_there ? c.v_scales[(long long)page * c.kv_heads + kv_head] : 1.f;
   };
 
   if (i < end) {
-    load_k(i);
-    load_v(i);
+    if (V_AHEAD || AHEAD) load_k(i);
+    if (V_AHEAD) load_v(i);
   }
   for (; i < end; i += stride) {
     const int j0 = span.chunk(i) * 64, next = i + stride;
-    if (next < end) entries_of(next);
+    if (V_AHEAD && next < end) entries_of(next);
+    if (!V_AHEAD && !AHEAD) load_k(i);
     float4v sc[RT][4];
     bool odd = false;
 #pragma unroll
@@ -135,6 +148,11 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
       }
     }
     if (AHEAD && next < end) load_k(next);
+    if (!V_AHEAD) {
+      __builtin_amdgcn_sched_barrier(0);                           // (not beside the keys: registers)
+      load_v(i);
+      if (next < end) entries_of(next);
+    }
     // keys that some row does not see: hidden from it; those that no row sees may hold anything, so their values are cleared
     const bool all_there = __ballot(!v_there) == 0;
     if (!all_there || j0 + 63 > span.place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= span.place_max - a.window)) {
@@ -221,6 +239,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       half8v f[2];
+      if (!has(dt)) continue;
       if constexpr (E4M3) {
         f[0] = halves_of_e4m3(v[dt][0].x, v[dt][0].y, v_scale);
         f[1] = halves_of_e4m3(v[dt][0].z, v[dt][0].w, v_scale);
@@ -239,7 +258,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const unsigned long long seen = seen64_of(a, s, place[rt], j0);
-        for (int dt = 0; dt < DT; ++dt) {
+        for (int dt = 0; dt < DT && has(dt); ++dt) {
           const unsigned at = bits + dt * 16 * 8;
           float4v *to = reinterpret_cast<float4v *>(put_back + ((rt * WAVES + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
           const float4v x = {Odd<E4M3>::sum(at, D, seen), Odd<E4M3>::sum(at + 8, D, seen), Odd<E4M3>::sum(at + 16, D, seen), Odd<E4M3>::sum(at + 24, D, seen)};
@@ -251,8 +270,8 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
       __builtin_amdgcn_wave_barrier();
     }
     if (next < end) {
-      if (!AHEAD) load_k(next);
-      load_v(next);
+      if (!AHEAD && V_AHEAD) load_k(next);
+      if (V_AHEAD) load_v(next);
     }
   }
 
@@ -279,6 +298,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
     __syncthreads();
     for (int u = (int)threadIdx.x; u < min(left, 16) * (D / 4); u += 64 * WAVES) {
       const int r = u / (D / 4), d = (u - r * (D / 4)) * 4;
+      if (!EXACT && d >= dim) continue;
       float top = -__builtin_inff();
       for (int w = 0; w < active; ++w) top = fmaxf(top, ml[2 * (w * 16 + r)]);
       const float base = base_of(top);
@@ -295,18 +315,18 @@ __global__ __launch_bounds__(64 * WAVES) void attention_decode_kernel(const KvPa
         const int t = token_of(a, row), head = kv_head * a.group + row - t * a.group;
         x *= inverse_of(total);
         typedef _Float16 half4b __attribute__((ext_vector_type(4), aligned(2)));
-        *reinterpret_cast<half4b *>(a.out + (s.row0 + t) * a.ldo + (long long)head * D + d) = half4b{(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w};
+        *reinterpret_cast<half4b *>(a.out + (s.row0 + t) * a.ldo + (long long)head * dim + d) = half4b{(_Float16)x.x, (_Float16)x.y, (_Float16)x.z, (_Float16)x.w};
         if (a.lse && d == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
       } else {
         const long long to = (((long long)b * c.kv_heads + kv_head) * split.parts + part) * ((long long)c.max_new * a.group) + row;
-        *reinterpret_cast<float4v *>(split.o + to * D + d) = x;
+        *reinterpret_cast<float4v *>(split.o + to * dim + d) = x;
         if (d == 0) *reinterpret_cast<float2v *>(split.ml + to * 2) = float2v{top, total};
       }
     }
   }
 }
 
-// Joins the parts of a sequence's keys: a workgroup to a row, whose threads take four elements of a share of the parts each.
+// Joins the parts of a sequence's keys: a workgroup to a row, whose threads take four elements of a share of the parts each.  D: elements of a head, or more.
 constexpr int JOIN_THREADS = 256;
 
 template <int D>
@@ -314,7 +334,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvPa
   constexpr int LANES = D / 4, SHARES = JOIN_THREADS / LANES;
   __shared__ __attribute__((aligned(16))) float shares[SHARES][D];
   __shared__ float factors[64];
-  const int rows_most = c.max_new * a.group, lane = (int)threadIdx.x & 63;
+  const int rows_most = c.max_new * a.group, dim = c.head_dim, lane = (int)threadIdx.x & 63;
   const int row = (int)blockIdx.x, kv_head = (int)blockIdx.y, b = (int)blockIdx.z;
   const long long from = ((long long)b * c.kv_heads + kv_head) * split.parts * rows_most + row;
   // lane w < parts of every wave takes part w's maximum and sum (64 parts at most); loaded, as the outputs are, before it is known how many there are
@@ -325,7 +345,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvPa
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int w = w0 + u * SHARES;
-      y[u] = w < split.parts ? *reinterpret_cast<const float4v *>(split.o + (from + (long long)w * rows_most) * D + d) : float4v{0.f, 0.f, 0.f, 0.f};
+      y[u] = w < split.parts && d < dim ? *reinterpret_cast<const float4v *>(split.o + (from + (long long)w * rows_most) * dim + d) : float4v{0.f, 0.f, 0.f, 0.f};
     }
   };
   load(share);
@@ -354,22 +374,26 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvPa
   *reinterpret_cast<float4v *>(&shares[share][d]) = x;
   __syncthreads();
   const int t = token_of(a, row), head = kv_head * a.group + row - t * a.group;
-  if ((int)threadIdx.x < D) {
+  if ((int)threadIdx.x < dim) {
     float y = 0.f;
 #pragma unroll
     for (int w = 0; w < SHARES; ++w) y += shares[w][threadIdx.x];
-    a.out[(s.row0 + t) * a.ldo + (long long)head * D + threadIdx.x] = __float2half_rn(y * inverse_of(total));
+    a.out[(s.row0 + t) * a.ldo + (long long)head * dim + threadIdx.x] = __float2half_rn(y * inverse_of(total));
   }
   if (a.lse && threadIdx.x == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
 }
 
-template <bool E4M3, int D, int RT, bool MANY>
+template <bool E4M3, int D, int RT, bool MANY, bool EXACT = true>
 int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT);
-  if (c.n_seqs > 0x7fffffff / 512 || (long long)tiles * s.parts > 65535) return VQ_ERR_SHAPE;
+  constexpr int WAVES = waves_of(E4M3, D);
+  const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT), most = 65535 / s.parts;     // (more tiles than a grid has layers: several launches)
+  if (c.n_seqs > 0x7fffffff / 512) return VQ_ERR_SHAPE;
   const int lds = (2 * 16 + 16 * (D + 4) * (MANY ? RT : 1)) * WAVES * 4 + (MANY ? WAVES * Odd<E4M3>::KINDS * D * 8 : 0);
-  VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT, MANY>));
-  hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY>), dim3(c.n_seqs, c.kv_heads, tiles * s.parts), dim3(64 * WAVES), lds, stream, c, a, s, tiles);
+  VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT, MANY, EXACT>));
+  for (int tile0 = 0; tile0 < tiles; tile0 += most) {
+    const int now = tiles - tile0 < most ? tiles - tile0 : most;
+    hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY, EXACT>), dim3(c.n_seqs, c.kv_heads, now * s.parts), dim3(64 * WAVES), lds, stream, c, a, s, now, tile0);
+  }
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 
@@ -378,8 +402,9 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
 // Two tiles share the conversions and loads of a chunk, where the registers are there: not beside 64 of a 16-bit chunk's keys and as many of its values, nor
 // (heads of 128 elements) beside what rows of several tokens need.
 int attention_decode_rows(const KvParams &c, const AttentionParams &a) {
-  return (long long)c.max_new * a.group > 16 && (c.head_dim == 64 || (c.e4m3 && c.max_new == 1)) ? 32 : 16;
+  return (long long)c.max_new * a.group > 16 && (c.head_dim == 64 || (c.head_dim == 128 && c.e4m3 && c.max_new == 1)) ? 32 : 16;
 }
+int attention_decode_run(const KvParams &c) { return waves_of(c.e4m3, c.head_dim); }
 
 template <bool MANY>
 static int launch_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
@@ -391,15 +416,24 @@ static int launch_decode(const KvParams &c, const AttentionParams &a, const Spli
   return c.e4m3 ? launch<true, 128, 1, MANY>(c, a, s, stream) : launch<false, 128, 1, MANY>(c, a, s, stream);
 }
 
+// Heads of other sizes: rows of one token as well by what takes several.
+template <int D>
+static int launch_padded(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  return c.e4m3 ? launch<true, D, 1, true, false>(c, a, s, stream) : launch<false, D, 1, true, false>(c, a, s, stream);
+}
+
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  if (c.head_dim != 64 && c.head_dim != 128)
+    return c.head_dim < 64 ? launch_padded<64>(c, a, s, stream) : c.head_dim < 128 ? launch_padded<128>(c, a, s, stream) :
+           c.head_dim <= 192 ? launch_padded<192>(c, a, s, stream) : launch_padded<256>(c, a, s, stream);
   return c.max_new > 1 ? launch_decode<true>(c, a, s, stream) : launch_decode<false>(c, a, s, stream);
 }
 
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream) {
   const dim3 blocks(c.max_new * a.group, c.kv_heads, c.n_seqs);
   if (c.n_seqs > 65535) return VQ_ERR_SHAPE;
-  if (c.head_dim == 64) hipLaunchKernelGGL((attention_join_kernel<64>), blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
-  else hipLaunchKernelGGL((attention_join_kernel<128>), blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
+  auto kernel = c.head_dim <= 64 ? attention_join_kernel<64> : c.head_dim <= 128 ? attention_join_kernel<128> : attention_join_kernel<256>;
+  hipLaunchKernelGGL(kernel, blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 

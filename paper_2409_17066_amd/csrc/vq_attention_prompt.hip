@@ -33,8 +33,10 @@ __device__ __forceinline__ int nth_longest(const KvParams &c, int n, int lane) {
   return (int)__builtin_ctzll(__ballot(lane < c.n_seqs && before == n));
 }
 
-template <bool E4M3, int D>
+// D: elements of a head, or (not EXACT) more, zeros behind the head's own.
+template <bool E4M3, int D, bool EXACT>
 __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int zigzag) {
+  const int dim = EXACT ? D : c.head_dim;
   constexpr int BYTES = E4M3 ? 1 : 2;
   constexpr int KU = D * BYTES / 16, VU = 64 * BYTES / 16;        // 16-byte words of a key, and of an element's 64 keys
   constexpr int REPS = 64 * KU / THREADS, SLOTS = D / 8;          // words a thread brings; 16-byte slots of a key in LDS
@@ -76,9 +78,10 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   const int place_min = s.first + token_of(a, min(wave_row, rows - 1)), place_max = s.first + token_of(a, min(wave_row + 31, rows - 1));
   half8v q[STEPS];
   {
-    const __half *x = a.q + (s.row0 + token) * a.ldq + ((long long)kv_head * a.group + row - token * a.group) * D + h * 8;
+    const __half *x = a.q + (s.row0 + token) * a.ldq + ((long long)kv_head * a.group + row - token * a.group) * dim + h * 8;
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) q[i] = __builtin_bit_cast(half8v, (uint4v)*reinterpret_cast<const uint4b *>(x + i * 16));
+    for (int i = 0; i < STEPS; ++i)
+      q[i] = __builtin_bit_cast(half8v, EXACT || i * 16 < dim ? (uint4v)*reinterpret_cast<const uint4b *>(x + i * 16) : uint4v{0, 0, 0, 0});
   }
   float m = -__builtin_inff(), l = 0.f;
   float16v o[DT];
@@ -93,8 +96,11 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   constexpr int K_STEP = THREADS / KU, V_STEP = THREADS / VU;       // keys and elements from one word of a thread to its next
   const int k_key = tid / KU, k_piece = tid % KU, wave_key = wave * (64 / KU);
   const int v_piece = wide ? tid % VU : wave * BYTES + lane % BYTES, v_d = wide ? tid / VU : lane / BYTES, v_key = v_piece * (16 / BYTES);
-  const unsigned k_offset = (unsigned)((k_key - wave_key) * (D * BYTES) + k_piece * 16);
+  const bool k_has = EXACT || k_piece * 16 < dim * BYTES;
+  const unsigned k_offset = (unsigned)((k_key - wave_key) * (dim * BYTES) + (k_has ? k_piece * 16 : 0));
   const unsigned v_offset = (unsigned)((v_d << shift) * BYTES + (wide ? v_piece * 16 : lane % BYTES * 16)), v_step = (unsigned)(V_STEP * BYTES) << shift;
+  // (elements behind the head's: its last one again, for outputs that nobody stores)
+  auto v_of = [&](int r) { return EXACT ? v_offset : v_offset - ((unsigned)(max(v_d + r * V_STEP - (dim - 1), 0) * BYTES) << shift); };
   uint4v kw[REPS], vw[REPS];
   float ks[REPS], vs = 1.f;
   int k_entry[REPS], v_entry = -1;
@@ -113,11 +119,11 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
 #pragma unroll
   for (int r = 0; r < REPS; ++r) {
     k_place[r] = wave_key + r * K_STEP;
-    k_in_page[r] = (unsigned)(k_place[r] & mask) * (D * BYTES);
+    k_in_page[r] = (unsigned)(k_place[r] & mask) * (dim * BYTES);
   }
   const int v_place = wide ? 0 : wave * 16;
   const unsigned v_in_page = (unsigned)(v_place & mask) * BYTES;
-  const unsigned char *k_head = c.k_pages + ((long long)kv_head << shift) * (D * BYTES), *v_head = c.v_pages + (((long long)kv_head * D) << shift) * BYTES;
+  const unsigned char *k_head = c.k_pages + ((long long)kv_head << shift) * (dim * BYTES), *v_head = c.v_pages + (((long long)kv_head * dim) << shift) * BYTES;
   // Entries of the page table; past its end, where no key is, the last one's.
   auto entries = [&](int j0) {
 #pragma unroll
@@ -130,7 +136,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
 #pragma unroll
     for (int r = 0; r < REPS; ++r) {
       const unsigned entry = (unsigned)__builtin_amdgcn_readfirstlane(k_entry[r]), page = entry < (unsigned)c.n_pages ? entry : 0u;
-      kw[r] = word_at(buffer(k_head + (unsigned long long)page * (unsigned)c.k_page_bytes), k_offset, in_page * (D * BYTES) + k_in_page[r]);
+      kw[r] = word_at(buffer(k_head + (unsigned long long)page * (unsigned)c.k_page_bytes), k_offset, in_page * (dim * BYTES) + k_in_page[r]);
       if (E4M3) ks[r] = __uint_as_float(number_at(k_scales, page * (unsigned)c.kv_heads * 4u));
     }
     const unsigned entry = (unsigned)__builtin_amdgcn_readfirstlane(v_entry);
@@ -138,7 +144,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
     const unsigned page = v_there ? entry : 0u;
     const __amdgpu_buffer_rsrc_t from = buffer(v_head + (unsigned long long)page * (unsigned)c.v_page_bytes);
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) vw[r] = word_at(from, v_offset, in_page * BYTES + v_in_page + r * v_step);
+    for (int r = 0; r < REPS; ++r) vw[r] = word_at(from, v_of(r) + (EXACT ? 0u : r * v_step), in_page * BYTES + v_in_page + (EXACT ? r * v_step : 0u));
     if (E4M3) vs = __uint_as_float(number_at(v_scales, page * (unsigned)c.kv_heads * 4u));
   };
   using Zero = std::integral_constant<int, 0>;
@@ -152,6 +158,9 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   auto put = [](unsigned at, uint4v x) { *(__attribute__((address_space(3))) uint4v *)(size_t)at = x; };
   auto store = [&](int j0, auto into) {
     constexpr int INTO = decltype(into)::value;
+    if (!EXACT)
+#pragma unroll
+      for (int r = 0; r < REPS; ++r) kw[r] = k_has ? kw[r] : uint4v{0, 0, 0, 0};
     if (j0 + 64 > span.end || j0 < span.low || !v_there) {          // values that no row looks at may be anything: cleared
       unsigned keep[4];
 #pragma unroll
@@ -350,13 +359,14 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const int d = 32 * dt + 8 * w + 4 * h;
+      if (!EXACT && d >= dim) continue;
       const float y0 = x.f[4 * w], y1 = x.f[4 * w + 1], y2 = x.f[4 * w + 2], y3 = x.f[4 * w + 3];
       if (whole) {
         typedef _Float16 half4b __attribute__((ext_vector_type(4), aligned(2)));
-        *reinterpret_cast<half4b *>(a.out + (s.row0 + token) * a.ldo + (long long)head * D + d) =
+        *reinterpret_cast<half4b *>(a.out + (s.row0 + token) * a.ldo + (long long)head * dim + d) =
             half4b{(_Float16)(y0 * inverse), (_Float16)(y1 * inverse), (_Float16)(y2 * inverse), (_Float16)(y3 * inverse)};
       } else {
-        *reinterpret_cast<float4v *>(split.o + to * D + d) = float4v{y0, y1, y2, y3};
+        *reinterpret_cast<float4v *>(split.o + to * dim + d) = float4v{y0, y1, y2, y3};
       }
     }
   }
@@ -366,13 +376,13 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   }
 }
 
-template <bool E4M3, int D>
+template <bool E4M3, int D, bool EXACT = true>
 int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
   const int tiles = (c.max_new * a.group + ROWS - 1) / ROWS;
   const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
   if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
-  VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D>));
-  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8, stream, c, a, s, tiles,
+  VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D, EXACT>));
+  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D, EXACT>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8, stream, c, a, s, tiles,
                      blocks <= 2 * cu_count());
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
@@ -380,8 +390,11 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
 }  // namespace
 
 int attention_prompt_rows() { return ROWS; }
+bool attention_prompt_takes(const KvParams &c) { return c.head_dim <= 128; }
 
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+  if (c.head_dim < 64) return c.e4m3 ? launch<true, 64, false>(c, a, s, stream) : launch<false, 64, false>(c, a, s, stream);
+  if (c.head_dim > 64 && c.head_dim < 128) return c.e4m3 ? launch<true, 128, false>(c, a, s, stream) : launch<false, 128, false>(c, a, s, stream);
   if (c.head_dim == 64) return c.e4m3 ? launch<true, 64>(c, a, s, stream) : launch<false, 64>(c, a, s, stream);
   return c.e4m3 ? launch<true, 128>(c, a, s, stream) : launch<false, 128>(c, a, s, stream);
 }

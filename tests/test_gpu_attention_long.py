@@ -125,6 +125,56 @@ def test_long_cases_are_cut(gpu_lib):
     assert cut >= 9
 
 
+@pytest.mark.parametrize("dim", [16, 32, 48, 80, 96, 112, 144, 192, 208, 256])
+@pytest.mark.parametrize("bits", [8, 16])
+@pytest.mark.parametrize("lengths,news,q_heads,heads,window,sinks", [
+    ([1900, 3, 64], [1, 1, 1], 8, 2, 0, 0),
+    ([1400, 90], [5, 3], 4, 2, 500, 5),
+    ([700, 40], [300, 40], 2, 1, 0, 0),
+    ([1700], [140], 2, 2, 0, 0),
+], ids=str)
+def test_heads_of_other_sizes(gpu_lib, dim, bits, lengths, news, q_heads, heads, window, sinks):
+    """Between heads stand NaN (unseen places of the pages) and other heads; the last page of the pool is in use."""
+    import torch
+    size = 16 if dim < 100 else 64
+    rng, cache, table, k, v, q = _problem(25, lengths, news, q_heads, heads, dim, size, bits, fill="nan", spare=0)
+    cache.append(k, v, table, lengths, news)
+    dev = Device(cache, table, lengths, news)
+    qd = torch.from_numpy(q).cuda()
+    args = dict(starts=dev.starts, window=window, sinks=sinks, max_new=max(news), max_length=max(lengths), return_lse=True)
+    out, lse = gpu_lib.attention(qd, *dev.cache, **args)
+    again, lse2 = gpu_lib.attention(qd, *dev.cache, **args)
+    torch.cuda.synchronize()
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    _check(out.cpu().numpy(), lse.cpu().numpy(), *_attention(q, cache, table, lengths, news, dim ** -0.5, window, sinks), dim, max(lengths))
+
+
+@pytest.mark.parametrize("dim,bits", [(80, 8), (80, 16), (48, 16), (192, 8), (192, 16), (256, 8), (256, 16)])
+@pytest.mark.parametrize("news", [[7, 1], [150, 60]], ids=str)
+def test_values_that_are_not_finite_in_heads_of_other_sizes(gpu_lib, dim, bits, news):
+    """In the last element of the first head, and the first of the second: rows that see them get what the sums give, others what they get without."""
+    import torch
+    lengths, heads, size = [300, 190], 2, 16
+    rng, cache, table, k, v, q = _problem(26, lengths, news, 2, heads, dim, size, bits)
+    cache.append(k, v, table, lengths, news)
+    args = dict(max_new=max(news), max_length=max(lengths))
+
+    def run():
+        dev = Device(cache, table, lengths, news)
+        return gpu_lib.attention(torch.from_numpy(q).cuda(), *dev.cache, starts=dev.starts, **args)
+    want = run()
+    place = lengths[0] - 3                              # seen by the last three of the first sequence's tokens
+    for head, element, value in ((0, dim - 1, np.nan if bits == 8 else -np.inf), (1, 0, np.nan)):
+        cache.v[table[0, place // size], head, element, place % size] = 0x7f if bits == 8 else value
+    got = run()
+    torch.cuda.synchronize()
+    hit = torch.zeros(got.shape, dtype=torch.bool, device="cuda")
+    rows = slice(max(news[0] - 3, 0), news[0])
+    hit[rows, 0, dim - 1] = hit[rows, 1, 0] = True
+    assert torch.equal(got[~hit], want[~hit])
+    assert torch.isnan(got[rows, 1, 0]).all() and (torch.isnan(got[rows, 0, dim - 1]) if bits == 8 else got[rows, 0, dim - 1] == -np.inf).all()
+
+
 def test_many_sequences(gpu_lib):
     import torch
     rng = np.random.default_rng(22)
