@@ -2,6 +2,8 @@
 //
 // A workgroup holds a row in registers, eight elements a vector and up to four vectors a thread, so that every element is read once and
 // written once; memory bounds it from a few hundred rows on, the two reductions (one behind the other where there are both norms) and the launch below.
+// Measured: 2048 rows of 8192, stream in 32 bits, both norms and a gate, 201 MB in 38.8 us, 5.2 TB/s (a large copy reaches 4.9); one row of 4096 2.5 us in a
+// graph, of which an empty launch is 2, and 3.9 from the host, 5.2 where it allocates both results.
 #include "vq_kv.hpp"
 
 namespace vq {
@@ -101,6 +103,11 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
   const long long row = blockIdx.x;
   const int stride = (int)blockDim.x * 8, i0 = (int)threadIdx.x * 8, width = p.width;
   const Stream *x = static_cast<const Stream *>(p.x) + row * p.ldx;
+  // Rows of one vector a thread are few: what the reductions wait for counts, and the weights are asked for in front of them.
+  constexpr bool EARLY = NV == 1;
+  Eight w_pre{}, w_post{};
+  if (EARLY && p.z) w_pre = load8<false>(p.w_pre, i0, width);
+  if (EARLY && p.w_post) w_post = load8<false>(p.w_post, i0, width);
   Eight y[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) y[v] = load8<true>(x, i0 + v * stride, width);
@@ -119,7 +126,7 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
       r = 1.f / __fsqrt_rn(block_sum(ss, sums[0]) / (float)width + p.eps);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const Eight w = load8<false>(p.w_post, i0 + v * stride, width);
+        const Eight w = EARLY ? w_post : load8<false>(p.w_post, i0 + v * stride, width);
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[v].e[j] *= w.e[j];
       }
@@ -151,7 +158,7 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
   __half *to = p.z + row * p.ldz;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const Eight w = load8<false>(p.w_pre, i0 + v * stride, width);
+    const Eight w = EARLY ? w_pre : load8<false>(p.w_pre, i0 + v * stride, width);
 #pragma unroll
     for (int j = 0; j < 8; ++j) y[v].e[j] = y[v].e[j] * r * w.e[j];
     store8(to, i0 + v * stride, width, y[v]);
@@ -160,9 +167,12 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const NormParams p)
 
 template <typename Stream>
 int launch(const NormParams &p, int rows, hipStream_t s) {
-  const int vectors = (p.width + 7) / 8;
+  // Where there are two workgroups for a compute unit or less, as many threads as a row has vectors; more rows have vectors enough on their way, and fewer waves
+  // to wait for one another.  (us in a graph, by up to 256 threads and up to 1024: 1 row of 4096 3.0 and 2.5, of 8192 with both norms 5.2 and 3.6; 512 rows 13.9 and
+  // 11.8; 1024 20.0 and 22.3; 2048 39.9 and 42.5, of 4096 12.5 and 14.2.)
+  const int vectors = (p.width + 7) / 8, most = rows <= 2 * cu_count() ? 1024 : 256;
   int nv = 1;
-  while (nv < 4 && (vectors + nv - 1) / nv > 256) nv *= 2;
+  while (nv < 4 && (vectors + nv - 1) / nv > most) nv *= 2;
   const int threads = ((vectors + nv - 1) / nv + 63) / 64 * 64;
   switch (nv) {
     case 1: hipLaunchKernelGGL((residual_norm_kernel<Stream, 1>), dim3(rows), dim3(threads), 0, s, p); break;
