@@ -310,7 +310,7 @@ typedef struct vq_kv_desc {
   int32_t page_tokens;                     /* 16, 32, 64, 128 or 256                                       */
   int32_t n_pages;                         /* pages in the pool                                            */
   int32_t n_seqs, n_tokens;                /* sequences and new tokens of this call                        */
-  int32_t max_new, max_length;             /* of one sequence; max_length <= table_pages * page_tokens     */
+  int32_t max_new, max_length;             /* of one sequence; max_length <= table_pages * page_tokens and 2^30 */
   int32_t table_pages;                     /* entries of a row of page_table                               */
   int32_t reserved;                        /* 0                                                            */
   void *k_pages, *v_pages;                 /* 16-byte aligned                                              */
@@ -349,7 +349,8 @@ int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void
  * over the places j that token t at place p sees: j <= p, and with window > 0 also j > p - window or j < sinks.  A token that sees
  * nothing gets zeros.  lse (may be NULL): binary32 [n_tokens][q_heads], the logarithm of the sum of exp(score), -inf for such tokens.
  * Scores, statistics and sums are binary32; the probabilities (relative to the largest so far) are rounded to binary16 for the matrix cores, the result once.
- * Keys and values nobody sees may hold anything, NaN included.  softmax_scale must be finite and positive.
+ * Keys and values nobody sees may hold anything, NaN included.  Codes are widened to binary16: what they stand for has to lie within its range (as what
+ * vq_kv_append stores of numbers up to 63488 does), beyond it is infinite.  softmax_scale must be finite and positive.
  * Workspace (device memory, 256-byte aligned, contents undefined afterwards): with vq_attention_workspace_bytes bytes a
  * sequence's keys are cut into parts where that is faster (judged by the descriptor's sizes alone), and a second kernel joins them;
  * with less or NULL each sequence's keys are taken in one part.  Results are deterministic run to run for the same sizes and workspace.  */

@@ -378,7 +378,7 @@ int make_kv_params(const vq_kv_desc *d, KvParams *p) {
   int shift = 4;
   while (shift < 8 && (1 << shift) != d->page_tokens) ++shift;
   if ((1 << shift) != d->page_tokens) return VQ_ERR_SHAPE;
-  if (d->n_pages < 1 || d->n_seqs < 1 || d->n_tokens < 1 || d->max_new < 1 || d->max_new > d->n_tokens || d->max_length < 0) return VQ_ERR_SHAPE;
+  if (d->n_pages < 1 || d->n_seqs < 1 || d->n_tokens < 1 || d->max_new < 1 || d->max_new > d->n_tokens || d->max_length < 0 || d->max_length > 1 << 30) return VQ_ERR_SHAPE;
   if (d->table_pages < 0 || d->max_length > (long long)d->table_pages * d->page_tokens || d->table_stride < d->table_pages) return VQ_ERR_SHAPE;
   if (!d->starts && (d->n_tokens % d->n_seqs != 0 || d->max_new < d->n_tokens / d->n_seqs)) return VQ_ERR_SHAPE;
   if (!d->k_pages || !d->v_pages || !d->lengths || (!d->page_table && d->table_pages) || (e4m3 && (!d->k_scales || !d->v_scales))) return VQ_ERR_NULL;
@@ -407,7 +407,8 @@ static int make_attention_params(const KvParams &c, int32_t q_heads, int32_t win
   a->q_heads = q_heads; a->group = q_heads / c.kv_heads;
   a->by_group = a->group > 1 ? (unsigned)((1ull << 32) / a->group) + 1 : 0;
   if ((long long)c.max_new * a->group * a->group >= 1ll << 30) return VQ_ERR_SHAPE;          // (by_group is good for so many rows and more)
-  a->window = window; a->sinks = window ? sinks : 0;
+  constexpr int32_t most = 1 << 30;                                                          // (as long as any sequence, and places less it are numbers of 32 bits)
+  a->window = window < most ? window : most; a->sinks = window ? (sinks < most ? sinks : most) : 0;
   return VQ_OK;
 }
 

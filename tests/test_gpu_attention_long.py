@@ -175,6 +175,23 @@ def test_values_that_are_not_finite_in_heads_of_other_sizes(gpu_lib, dim, bits, 
     assert torch.isnan(got[rows, 1, 0]).all() and (torch.isnan(got[rows, 0, dim - 1]) if bits == 8 else got[rows, 0, dim - 1] == -np.inf).all()
 
 
+@pytest.mark.parametrize("dim", [64, 80, 128])
+def test_windows_and_first_tokens_longer_than_any_sequence(gpu_lib, dim):
+    """The largest numbers see what no window sees, also beside tokens that see nothing (more new tokens than the sequence holds)."""
+    import torch
+    for lengths, news in (([3, 700], [8, 8]), ([5, 500], [90, 90])):
+        rng, cache, table, k, v, q = _problem(27, lengths, news, 4, 2, dim, 16, 8)
+        cache.append(k, v, table, lengths, news)
+        dev, qd = Device(cache, table, lengths, news, uniform=True), torch.from_numpy(q).cuda()
+        args = dict(max_new=news[0], max_length=max(lengths), return_lse=True)
+        want = gpu_lib.attention(qd, *dev.cache, **args)
+        for window, sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (max(lengths), 0), (1, 2 ** 31 - 1), (40, max(lengths))):
+            got = gpu_lib.attention(qd, *dev.cache, window=window, sinks=sinks, **args)
+            torch.cuda.synchronize()
+            _check(got[0].cpu().numpy(), got[1].cpu().numpy(), *_attention(q, cache, table, lengths, news, dim ** -0.5, 0, 0), dim, max(lengths))
+            assert torch.equal(got[1] == -float("inf"), want[1] == -float("inf"))
+
+
 def test_many_sequences(gpu_lib):
     import torch
     rng = np.random.default_rng(22)

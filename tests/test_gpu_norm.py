@@ -56,6 +56,13 @@ def test_residual_norm(gpu_lib, rows, width, stream, post, gate, scale, pitch):
     assert (off <= 2.0 ** -11 * np.abs(want_z) + 2.0 ** -18 * (size * factor + np.abs(want_z) * (1 + root)) + 2.0 ** -25).all(), off.max()
 
 
+@pytest.mark.parametrize("rows,width", [(600, 1000), (700, 2049), (600, 4100), (530, 8192), (520, 12000)])
+@pytest.mark.parametrize("stream", [16, 32])
+def test_residual_norm_of_many_rows(gpu_lib, rows, width, stream):
+    test_residual_norm(gpu_lib, rows, width, stream, True, "channel", 0.5, 0)
+    test_residual_norm(gpu_lib, rows, width, stream, False, "token", 1.0, 5)
+
+
 def test_norm_alone_sum_alone_and_in_place(gpu_lib):
     import torch
     g = torch.Generator(device="cuda").manual_seed(3)

@@ -40,6 +40,7 @@ BAD_CACHES = [
     (dict(n_pages=0), vq.VQ_ERR_SHAPE), (dict(n_seqs=0), vq.VQ_ERR_SHAPE), (dict(n_tokens=0), vq.VQ_ERR_SHAPE),
     (dict(max_new=0), vq.VQ_ERR_SHAPE), (dict(max_new=7), vq.VQ_ERR_SHAPE),
     (dict(max_length=-1), vq.VQ_ERR_SHAPE), (dict(max_length=65), vq.VQ_ERR_SHAPE),
+    (dict(max_length=2 ** 30 + 1, table_pages=2 ** 27, table_stride=2 ** 27), vq.VQ_ERR_SHAPE),
     (dict(table_pages=-1), vq.VQ_ERR_SHAPE), (dict(table_stride=3), vq.VQ_ERR_SHAPE),
     (dict(starts=None, n_tokens=7), vq.VQ_ERR_SHAPE),                       # not as many for each
     (dict(starts=None, max_new=1), vq.VQ_ERR_SHAPE),                        # two each
