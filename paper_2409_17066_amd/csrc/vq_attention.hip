@@ -1,6 +1,7 @@
 // Attention of new tokens over a paged cache: which kernel takes a call, and in how many parts.
 #include "vq_attention.hpp"
 #include <algorithm>
+#include <cmath>
 
 namespace vq {
 
@@ -14,13 +15,14 @@ struct Plan {
 };
 
 // The kernel and number of parts whose time is estimated the least, in us, from measurements on heads of 64 and 128 elements, 8 and 16 bits, 8 and 32 key heads,
-// 1 to 16 sequences of 1024 to 32768 tokens with 16 to 256 rows a key head:
-//   decode: a workgroup to a compute unit, rounds of 3.2 us for eight chunks of 16 KB (more bytes take longer, and more rows more workgroups) behind 9 us;
-//   prompt: two to a compute unit, 1.3 us a chunk of both for up to 32 rows and 0.6 more for each further 32 of 128, behind 12 us, and where there is one
-//   alone 1.3 and 0.1 (half of that for 64 elements);
-// and for parts the second launch that joins them, 5 us and what it moves.  Heads of other sizes are counted as the next multiple of 64, as the kernels take them.  Measured (64 query and 8 key heads of 128 elements, 8 bits, us by the decode and by
-// the prompt kernel): 16 sequences of 4096 tokens 32 and 38 for 32 rows a key head, 59 and 49 for 64, 218 and 99 for 256; one of 1024 tokens 13 and 16 for 32
-// rows, 13 and 19 for 256.  Parts (16 rows): 4 sequences of 2048 tokens 17 in one and 14 in four, one of 1024 13 in one and 14 in two.
+// 1 to 200 sequences of 15 to 32768 tokens with 1 to 4144 rows a key head (heads of other sizes count as the next multiple of 64, as the kernels take them):
+//   decode: a workgroup of eight waves to a compute unit (more of smaller ones), rounds of 3.2 us for eight chunks of 16 KB behind 9 us;
+//   prompt: one workgroup to a compute unit takes 1.3 us a chunk for up to 32 rows and 0.1 more for each further 32 of 128, two 1.3 and 0.6, behind 12 us and 5
+//   for every further round of workgroups;
+// and for parts the second launch that joins them, 5 us, 0.3 ns a row and what it moves.  Measured (64 query and 8 key heads of 128 elements, 8 bits, us by the
+// decode and by the prompt kernel): 16 sequences of 4096 tokens 32 and 38 for 32 rows a key head, 59 and 49 for 64, 218 and 99 for 256; one of 1024 tokens 13 and
+// 16 for 32 rows, 13 and 19 for 256; 64 of 100 tokens, 32 heads, one row 14 and 38.  Parts (16 rows): 4 sequences of 2048 tokens 17 in one and 14 in four, one of 1024 13
+// in one and 14 in two; 518 tokens behind 1909 (prompt kernel) 73 in one and 108 in two.
 Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
   Plan best{};
   const long long rows = (long long)c.max_new * a.group, slots = cu_count();
@@ -35,10 +37,13 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
     const long long most = parts_allowed ? std::min((chunks + run - 1) / run, 64LL) : 1;
     for (long long parts = 1;; parts *= 2) {
       parts = std::min(parts, most);
-      const float rounds = std::max((float)(groups * parts) / (float)((prompt ? 2 : 1) * slots), 1.f), runs = (float)(((chunks + run - 1) / run + parts - 1) / parts);
-      const float step = !prompt ? 3.2f * size * (c.e4m3 ? 1.f : 2.f) : run * size * (groups * parts > slots ? 0.7f + 0.6f * quarters : 1.2f + 0.1f * quarters);
-      const float join = parts > 1 ? 5.f + (float)(c.n_seqs * parts * c.kv_heads * rows) * size * 1024.f / 4.5e6f : 0.f;
-      const float time = (prompt ? 12.f : 9.f) + join + rounds * runs * step;
+      const float alone = (float)slots * (prompt ? 1.f : (float)run / (float)std::min(attention_decode_waves(c, (int)parts), run));   // workgroups side by side
+      const float most_at_once = prompt ? 2.f * alone : alone, work = (float)(groups * parts), rounds = prompt ? std::max(work / most_at_once, 1.f) : std::ceil(work / most_at_once);
+      const float turns = parts > 1 ? (float)(((chunks + run - 1) / run + parts - 1) / parts) : prompt ? (float)chunks / (float)run : (float)((chunks + run - 1) / run);
+      const float one = 1.2f + 0.1f * quarters, two = 0.7f + 0.6f * quarters, shared = std::min(std::max(work / alone - 1.f, 0.f), 1.f);
+      const float step = !prompt ? 3.2f * size * (c.e4m3 ? 1.f : 2.f) : run * size * (one + (two - one) * shared);
+      const float join = parts > 1 ? 5.f + (float)(c.n_seqs * c.kv_heads * rows) * (0.3e-3f + (float)parts * size * 1024.f / 4.5e6f) : 0.f;
+      const float time = (prompt ? 12.f + 5.f * size * (rounds - 1.f) : 9.f) + join + rounds * turns * step;
       if (least == 0.f || time < least) {
         least = time;
         best.tile_rows = tile;

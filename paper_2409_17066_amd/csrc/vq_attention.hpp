@@ -14,6 +14,7 @@ struct Split {
 // Chunks of a run, one for each wave of the decode kernel.
 constexpr int DECODE_RUN = 8, PROMPT_RUN = 4;
 int attention_decode_run(const KvParams &c);                       // DECODE_RUN, or half of it
+int attention_decode_waves(const KvParams &c, int parts);          // waves of a workgroup of the decode kernel
 // The decode kernel, which takes every head: rows of a key head to a workgroup.
 int attention_decode_rows(const KvParams &c, const AttentionParams &a);
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);

@@ -18,14 +18,13 @@ namespace vq {
 
 namespace {
 
-// Waves of a workgroup: as many as have room in LDS for what they join.
+// Waves of a workgroup, at most: as many as have room in LDS for what they join.
 constexpr int waves_of(bool e4m3, int dim) { return !e4m3 && dim > 192 ? DECODE_RUN / 2 : DECODE_RUN; }
 
 // RT: tiles of sixteen rows; D: elements of a head, or (not EXACT) the next multiple of 64, zeros behind the head's own; MANY: rows may be of several new
 // tokens, which see different keys.
 template <bool E4M3, int D, int RT, bool MANY, bool EXACT>
-__global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int tile0) {
-  constexpr int WAVES = waves_of(E4M3, D);
+__global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int tile0, int waves) {
   const int dim = EXACT ? D : c.head_dim;
   constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
   // The next chunk is loaded ahead where there are registers for it beside those of the rows' differences.
@@ -37,8 +36,8 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
   const int shift = c.page_shift, mask = (1 << shift) - 1;
   // Entries of the page table for places [of, of + 16).  Without a window the first ones do not depend on the sequence's length, and are asked for beside it.
   auto entry = [&](int of) { return of >> shift < c.table_pages ? c.page_table[b * c.table_stride + (of >> shift)] : -1; };
-  int i = part * WAVES + wave, k_entry = 0, v_entry = 0;
-  float *ml = lds, *out = lds + 2 * 16 * WAVES, *put_back = out;      // (a wave's first part of put_back is read before its results take the place)
+  int i = part * waves + wave, k_entry = 0, v_entry = 0;
+  float *ml = lds, *out = lds + 2 * 16 * waves, *put_back = out;      // (a wave's first part of put_back is read before its results take the place)
   bool any_odd = false;
   if (a.window == 0) {
     k_entry = entry(i * 64 + 16 * (n >> 2));
@@ -48,9 +47,9 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
   const int rows = s.rows * a.group, row0 = tile * 16 * RT, here = min(rows - row0, 16 * RT);
   if (here <= 0) return;
   const Span span = span_of(a, s, row0, 16 * RT);
-  const int begin = part * WAVES, end = span.chunks, stride = split.parts * WAVES;
+  const int begin = part * waves, end = span.chunks, stride = split.parts * waves;
   if (part > 0 && begin >= end) return;
-  const int active = min(max(end - begin, 0), WAVES);            // waves that have a chunk
+  const int active = min(max(end - begin, 0), waves);            // waves that have a chunk
   if (a.window != 0 && i < end) {
     k_entry = entry(span.chunk(i) * 64 + 16 * (n >> 2));
     v_entry = entry(span.chunk(i) * 64 + 16 * g);
@@ -191,7 +190,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
           for (int w = 0; w < VL; ++w) odd |= Odd<E4M3>::any(v[dt][w]);
         odd = __ballot(odd) != 0;
         if (odd) {
-          unsigned bits = (unsigned)(size_t)(__attribute__((address_space(3))) float *)(put_back + RT * WAVES * 16 * PITCH) + wave * (Odd<E4M3>::KINDS * D * 8) + n * 8 + g * 2;
+          unsigned bits = (unsigned)(size_t)(__attribute__((address_space(3))) float *)(put_back + RT * waves * 16 * PITCH) + wave * (Odd<E4M3>::KINDS * D * 8) + n * 8 + g * 2;
           asm volatile("" : "+v"(bits));
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
@@ -259,13 +258,13 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
       }
     }
     if (MANY && odd) {                                             // (to LDS, and from there to the outputs behind the loop: beside what is loaded there are no registers)
-      const unsigned bits = (unsigned)(size_t)(__attribute__((address_space(3))) float *)(put_back + RT * WAVES * 16 * PITCH) + wave * (Odd<E4M3>::KINDS * D * 8) + g * 4 * 8;
+      const unsigned bits = (unsigned)(size_t)(__attribute__((address_space(3))) float *)(put_back + RT * waves * 16 * PITCH) + wave * (Odd<E4M3>::KINDS * D * 8) + g * 4 * 8;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const unsigned long long seen = seen64_of(a, s, place[rt], j0);
         for (int dt = 0; dt < DT && has(dt); ++dt) {
           const unsigned at = bits + dt * 16 * 8;
-          float4v *to = reinterpret_cast<float4v *>(put_back + ((rt * WAVES + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
+          float4v *to = reinterpret_cast<float4v *>(put_back + ((rt * waves + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
           const float4v x = {Odd<E4M3>::sum(at, D, seen), Odd<E4M3>::sum(at + 8, D, seen), Odd<E4M3>::sum(at + 16, D, seen), Odd<E4M3>::sum(at + 24, D, seen)};
           *to = any_odd ? *to + x : x;
         }
@@ -289,7 +288,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
     __syncthreads();
     if (MANY && any_odd) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[rt][dt] += *reinterpret_cast<const float4v *>(put_back + ((rt * WAVES + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
+      for (int dt = 0; dt < DT; ++dt) o[rt][dt] += *reinterpret_cast<const float4v *>(put_back + ((rt * waves + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
     }
     const float sum = rows_sum(l[rt]);
     if (wave < active && lane < 16) {
@@ -301,7 +300,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
       for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<float4v *>(out + (wave * 16 + n) * PITCH + dt * 16 + g * 4) = o[rt][dt];
     }
     __syncthreads();
-    for (int u = (int)threadIdx.x; u < min(left, 16) * (D / 4); u += 64 * WAVES) {
+    for (int u = (int)threadIdx.x; u < min(left, 16) * (D / 4); u += 64 * waves) {
       const int r = u / (D / 4), d = (u - r * (D / 4)) * 4;
       if (!EXACT && d >= dim) continue;
       float top = -__builtin_inff();
@@ -390,14 +389,14 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvPa
 
 template <bool E4M3, int D, int RT, bool MANY, bool EXACT = true>
 int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  constexpr int WAVES = waves_of(E4M3, D);
+  const int waves = attention_decode_waves(c, s.parts);
   const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT), most = 65535 / s.parts;     // (more tiles than a grid has layers: several launches)
   if (c.n_seqs > 0x7fffffff / 512) return VQ_ERR_SHAPE;
-  const int lds = (2 * 16 + 16 * (D + 4) * (MANY ? RT : 1)) * WAVES * 4 + (MANY ? WAVES * Odd<E4M3>::KINDS * D * 8 : 0);
+  const int lds = (2 * 16 + 16 * (D + 4) * (MANY ? RT : 1)) * waves * 4 + (MANY ? waves * Odd<E4M3>::KINDS * D * 8 : 0);
   VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT, MANY, EXACT>));
   for (int tile0 = 0; tile0 < tiles; tile0 += most) {
     const int now = tiles - tile0 < most ? tiles - tile0 : most;
-    hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY, EXACT>), dim3(c.n_seqs, c.kv_heads, now * s.parts), dim3(64 * WAVES), lds, stream, c, a, s, now, tile0);
+    hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY, EXACT>), dim3(c.n_seqs, c.kv_heads, now * s.parts), dim3(64 * waves), lds, stream, c, a, s, now, tile0, waves);
   }
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
@@ -408,6 +407,13 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
 // (heads of 128 elements) beside what rows of several tokens need.
 int attention_decode_rows(const KvParams &c, const AttentionParams &a) {
   return (long long)c.max_new * a.group > 16 && (c.head_dim == 64 || (c.head_dim == 128 && c.e4m3 && c.max_new == 1)) ? 32 : 16;
+}
+// Where no sequence has a chunk for every wave, no more waves than chunks: more workgroups share a compute unit (8 bits: 36 sequences of up to 13
+// tokens, 32 heads of 64 elements, 10.9 us by eight waves and 7.0 by one; 64 of 250 tokens, 8 key heads of 128, 12.7 by eight and 9.4 by four).
+int attention_decode_waves(const KvParams &c, int parts) {
+  int waves = waves_of(c.e4m3, c.head_dim);
+  while (parts == 1 && waves > 1 && c.max_length <= 32 * waves) waves /= 2;
+  return waves;
 }
 int attention_decode_run(const KvParams &c) { return waves_of(c.e4m3, c.head_dim); }
 
