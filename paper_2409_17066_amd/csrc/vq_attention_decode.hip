@@ -27,8 +27,8 @@ template <bool E4M3, int D, int RT, bool MANY, bool EXACT>
 __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int tile0, int waves) {
   const int dim = EXACT ? D : c.head_dim;
   constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
-  // The next chunk is loaded ahead where there are registers for it beside those of the rows' differences.
-  constexpr bool AHEAD = !MANY || D == 64 || (E4M3 && D <= 128), V_AHEAD = D <= 128;
+  // The next chunk is loaded ahead where there are registers for it beside those of the rows' differences, and its values where the keys leave them room.
+  constexpr bool AHEAD = !MANY || D == 64 || (E4M3 && D <= 128), V_AHEAD = D == 64 || (D == 128 && (EXACT || E4M3));
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   // (tiles of the same keys a multiple of all key heads apart: on the same XCD where those are a multiple of eight)
