@@ -39,6 +39,8 @@ void read_switches() {
       else if (n == 5 && !strncmp(e, "multi", 5)) sw.multi_off = v == '0';
       else if (n == 4 && !strncmp(e, "rows", 4)) sw.rows = v == '0' ? 0 : v == '1' ? 1 : -1;
       else if (n == 8 && !strncmp(e, "products", 8)) sw.products = v == '0' ? 0 : v == '1' ? 1 : -1;
+      else if (n == 9 && !strncmp(e, "attention", 9)) sw.attention = v;
+      else if (n == 5 && !strncmp(e, "parts", 5)) sw.parts = v >= '0' && v <= '6' ? v - '0' : -1;
       else if (n == 5 && !strncmp(e, "dense", 5)) sw.dense = v >= '0' && v <= '9' ? v - '0' : -1;
     }
     e = *end ? end + 1 : end;
@@ -437,6 +439,7 @@ extern "C" int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk,
 }
 
 extern "C" size_t vq_attention_workspace_bytes(const vq_kv_desc *cache, int32_t q_heads, int32_t window, int32_t sinks) {
+  vq::read_switches();
   vq::KvParams c;
   vq::AttentionParams a;
   if (vq::make_kv_params(cache, &c) != VQ_OK || vq::make_attention_params(c, q_heads, window, sinks, &a) != VQ_OK) return 0;
@@ -445,6 +448,7 @@ extern "C" size_t vq_attention_workspace_bytes(const vq_kv_desc *cache, int32_t 
 
 extern "C" int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, int32_t window, int32_t sinks,
                             void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  vq::read_switches();
   vq::KvParams c;
   vq::AttentionParams a;
   int rc = vq::make_kv_params(cache, &c);

@@ -28,7 +28,8 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
   const long long rows = (long long)c.max_new * a.group, slots = cu_count();
   float least = 0.f;
   for (const bool prompt : {false, true}) {
-    if (prompt ? !attention_prompt_takes(c) : rows > 512 && attention_prompt_takes(c)) continue;
+    const char forced = attention_prompt_takes(c) ? switches().attention : 'd';
+    if (forced == 'd' || forced == 'p' ? prompt != (forced == 'p') : !prompt && rows > 512) continue;
     const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(c, a), run = prompt ? PROMPT_RUN : attention_decode_run(c);
     // tokens that a tile's rows look at: a window's and the first ones, or on the average all before half of the new ones
     const long long all = c.max_length - (rows > tile ? c.max_new / 2 : 0), reach = a.window > 0 ? (long long)a.window + a.sinks + tile / a.group + 64 : all;
@@ -36,6 +37,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
     const float quarters = (float)std::min((rows + 31) / 32, 4LL), size = (float)((c.head_dim + 63) / 64) / 2.f;
     const long long most = parts_allowed ? std::min((chunks + run - 1) / run, 64LL) : 1;
     for (long long parts = 1;; parts *= 2) {
+      if (switches().parts >= 0) parts = 1LL << switches().parts;
       parts = std::min(parts, most);
       const float alone = (float)slots * (prompt ? 1.f : (float)run / (float)std::min(attention_decode_waves(c, (int)parts), run));   // workgroups side by side
       const float most_at_once = prompt ? 2.f * alone : alone, work = (float)(groups * parts), rounds = prompt ? std::max(work / most_at_once, 1.f) : std::ceil(work / most_at_once);
@@ -51,7 +53,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
         best.run = run;
         best.prompt = prompt;
       }
-      if (parts == most) break;
+      if (parts == most || switches().parts >= 0) break;
     }
   }
   if (best.parts > 1) {

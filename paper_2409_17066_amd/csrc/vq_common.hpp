@@ -48,10 +48,12 @@ int cu_count();
 //                and multiplied wherever that can be done
 //   dense=0|1..9 the dense product of the restore-then-multiply route: always the smallest tiles / the kind of that number (1: the largest)
 //   dequant=g    vq_dequant: generic kernels
+//   attention=d|p vq_attention: the decode kernel / the prompt kernel wherever it can
+//   parts=0..6   vq_attention: a sequence's keys in up to 2^n parts
 struct Switches {
-  char gemv = 0, gemm = 0, dequant = 0;
+  char gemv = 0, gemm = 0, dequant = 0, attention = 0;
   bool groups_loop = false, multi_off = false;
-  int dense = -1, rows = -1, products = -1;
+  int dense = -1, rows = -1, products = -1, parts = -1;
 };
 const Switches &switches();
 void read_switches();

@@ -26,9 +26,12 @@ def _layout(seed):
     return dim, bits, size, heads, group, lengths, news, window, sinks
 
 
+@pytest.mark.parametrize("switches", ["", "attention=d", "attention=p", "attention=d,parts=2", "attention=p,parts=3", "attention=d,parts=6"])
 @pytest.mark.parametrize("seed", range(60))
-def test_layouts_drawn_at_random(gpu_lib, seed):
+def test_layouts_drawn_at_random(gpu_lib, monkeypatch, seed, switches):
+    """The kernels that are chosen, and each of the two in one part and in several."""
     import torch
+    monkeypatch.setenv("VQ_SWITCHES", switches)
     dim, bits, size, heads, group, lengths, news, window, sinks = _layout(seed)
     if max(lengths) * heads * dim * (1 + group * max(news)) > 3e8:
         news = [min(n, 8) for n in news]
