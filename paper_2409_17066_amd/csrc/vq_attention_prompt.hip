@@ -385,7 +385,7 @@ template <bool E4M3, int D, bool EXACT = true>
 int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
   const int tiles = (c.max_new * a.group + ROWS - 1) / ROWS;
   const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
-  if (blocks > 0x7fffffff) return VQ_ERR_SHAPE;
+  if (blocks > 0xffffffffll / THREADS) return VQ_ERR_SHAPE;        // (threads of a grid)
   VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D, EXACT>));
   hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D, EXACT>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8, stream, c, a, s, tiles,
                      blocks <= 2 * cu_count());

@@ -396,7 +396,7 @@ int launch_kv_append(const KvParams &c, const __half *k, long long ldk, const __
   const long long kv_blocks = (2LL * c.n_seqs * p.slots * c.kv_heads * p.team + WAVES - 1) / WAVES;
   p.q_tiles = (c.max_new + p.tokens - 1) / p.tokens;
   const long long q_waves = q ? (long long)c.n_seqs * p.q_tiles * q_heads : 0, blocks = kv_blocks + (q_waves + WAVES - 1) / WAVES;
-  if (blocks > 0x7fffffff / WAVES) return VQ_ERR_SHAPE;
+  if (blocks > 0xffffffffll / (64 * WAVES)) return VQ_ERR_SHAPE;     // (threads of a grid)
   p.kv_blocks = (int)kv_blocks;
   auto kernel = c.e4m3 ? (paired ? kv_append_kernel<true, true> : kv_append_kernel<true, false>) : (paired ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WAVES), 0, s, p);

@@ -174,10 +174,17 @@ int launch(const NormParams &p, int rows, hipStream_t s) {
   int nv = 1;
   while (nv < 4 && (vectors + nv - 1) / nv > most) nv *= 2;
   const int threads = ((vectors + nv - 1) / nv + 63) / 64 * 64;
-  switch (nv) {
-    case 1: hipLaunchKernelGGL((residual_norm_kernel<Stream, 1>), dim3(rows), dim3(threads), 0, s, p); break;
-    case 2: hipLaunchKernelGGL((residual_norm_kernel<Stream, 2>), dim3(rows), dim3(threads), 0, s, p); break;
-    default: hipLaunchKernelGGL((residual_norm_kernel<Stream, 4>), dim3(rows), dim3(threads), 0, s, p); break;
+  auto kernel = nv == 1 ? residual_norm_kernel<Stream, 1> : nv == 2 ? residual_norm_kernel<Stream, 2> : residual_norm_kernel<Stream, 4>;
+  constexpr int MOST = 1 << 21;                                     // rows of a launch (a grid has fewer than 2^32 threads)
+  for (int row0 = 0; row0 < rows; row0 += MOST) {
+    NormParams q = p;
+    q.x = static_cast<const Stream *>(p.x) + row0 * p.ldx;
+    if (p.h) q.h = p.h + row0 * p.ldh;
+    if (p.gate) q.gate = p.gate + row0 * p.ldgate;
+    if (p.y) q.y = static_cast<Stream *>(p.y) + row0 * p.ldy;
+    if (p.z) q.z = p.z + row0 * p.ldz;
+    hipLaunchKernelGGL(kernel, dim3(rows - row0 < MOST ? rows - row0 : MOST), dim3(threads), 0, s, q);
+    if (rows - row0 <= MOST) break;
   }
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }

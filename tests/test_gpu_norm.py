@@ -63,6 +63,19 @@ def test_residual_norm_of_many_rows(gpu_lib, rows, width, stream):
     test_residual_norm(gpu_lib, rows, width, stream, False, "token", 1.0, 5)
 
 
+def test_more_rows_than_one_launch_takes(gpu_lib):
+    """Every row of a matrix of 2^21 + 2^20 + 5 rows gets what it gets by itself."""
+    import torch
+    rows, width = 2 ** 21 + 2 ** 20 + 5, 16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    h, x, w = (torch.randn(s, device="cuda", generator=g).half() for s in ((rows, width), (rows, width), (width,)))
+    gate = torch.randn((rows, width), device="cuda", generator=g).half()
+    y, z = gpu_lib.residual_norm(h, x, pre=w, post=w, gate=gate)
+    for at in (slice(0, 300), slice(2 ** 21 - 100, 2 ** 21 + 100), slice(rows - 200, rows)):
+        want = gpu_lib.residual_norm(h[at], x[at], pre=w, post=w, gate=gate[at])
+        assert torch.equal(y[at], want[0]) and torch.equal(z[at], want[1])
+
+
 def test_norm_alone_sum_alone_and_in_place(gpu_lib):
     import torch
     g = torch.Generator(device="cuda").manual_seed(3)
