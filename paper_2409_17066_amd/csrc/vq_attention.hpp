@@ -24,6 +24,13 @@ bool attention_prompt_takes(const KvParams &c);
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
 
+// Bytes from a page's start to word w (of the keys, sixteen bytes each, four lane groups apart) that lane n + 16 g of the decode kernel loads of a key in tile t of a chunk whose sixteen
+// keys begin at `place`; in place of words past the key's end its first one, which is not used: behind a pool's last key there is nothing.
+constexpr long long key_word_at(int kv_head, int page_shift, int place, int t, int w, int n, int g, int row_bytes) {
+  return (((long long)kv_head << page_shift) + (place & ((1 << page_shift) - 1)) + (n & 3)) * row_bytes + t * 4 * row_bytes +
+         (w * 64 + g * 16 < row_bytes ? w * 64 + g * 16 : 0);
+}
+
 #ifdef __HIPCC__
 // The rows of a key head are (new token t, query head of its group), t * group + g.  A tile of them sees keys [low, end) and [0, sinks), of
 // which some rows may see fewer; they are looked at in chunks of 64 keys: `sink_chunks` from 0 on, the others from `first` on.

@@ -98,14 +98,13 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
     const int j = span.chunk(i) * 64 + 16 * (n >> 2);
     bool there;
     const int page = page_at(j, k_entry, there);
-    const unsigned char *from = c.k_pages + page * c.k_page_bytes + (((long long)kv_head << shift) + (j & mask) + (n & 3)) * (dim * BYTES) + g * 16;
+    const unsigned char *from = c.k_pages + page * c.k_page_bytes;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int w = 0; w < KL; ++w) {
-        const bool mine = EXACT || w * 64 + g * 16 < dim * BYTES;
-        const uint4v x = *reinterpret_cast<const uint4v *>(from + t * 4 * dim * BYTES + (mine ? w * 64 : 0));
-        k[t][w] = mine ? x : uint4v{0, 0, 0, 0};
+        const uint4v x = *reinterpret_cast<const uint4v *>(from + key_word_at(kv_head, shift, j, t, w, n, g, dim * BYTES));
+        k[t][w] = EXACT || w * 64 + g * 16 < dim * BYTES ? x : uint4v{0, 0, 0, 0};
       }
     if (E4M3) k_scale = c.k_scales[(long long)page * c.kv_heads + kv_head];
   };
