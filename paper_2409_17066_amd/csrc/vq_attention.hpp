@@ -152,6 +152,11 @@ __device__ __forceinline__ unsigned long long seen64_of(const AttentionParams &a
 
 // A finite stand-in for the maximum of a row that has seen nothing yet.
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
+// The base of a row's exponents follows the maximum only when it has grown by 2^8: binary16 holds what lies in between.  (The difference is exact; m + 8 is not.)
+__device__ __forceinline__ bool outgrown(float now, float m) { return now - m > 8.f; }
+// Exponents are score * scale - base in one rounding and the base is a rounded product: past 2^22 they would be off by more than they may grow, and from 2^28 on
+// probabilities infinite.  There the products are rounded as the base is.
+__device__ __forceinline__ bool is_large(float base) { return __builtin_fabsf(base) > 4194304.f; }
 // One over a softmax's sum; zero for a row that sees nothing; what is not a number stays none.
 __device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -__builtin_inff() : (m + __log2f(l)) * 0.6931471805599453f; }

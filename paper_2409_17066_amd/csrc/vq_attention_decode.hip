@@ -87,7 +87,11 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
     return there ? entry : 0;
   };
   uint4v k[4][KL], v[DT][VL];
-  auto has = [&](int dt) { return EXACT || dt * 16 < dim; };       // whether the head has elements 16 dt ... 16 dt + 15
+  auto has = [&](int dt) {                                         // whether the head has elements 16 dt ... 16 dt + 15
+    int of = dim;
+    if (!EXACT) asm volatile("" : "+s"(of));                       // (compared where it is asked: kept from round to round it would be two scalar registers for each)
+    return EXACT || dt * 16 < of;
+  };
   float k_scale = 1.f, v_scale = 1.f;
   bool v_there = false;
   auto entries_of = [&](int i) {
@@ -211,9 +215,8 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
     for (int rt = 0; rt < RT; ++rt) {
       float top = fmaxf(fmaxf(fmaxf(sc[rt][0].x, sc[rt][0].y), fmaxf(sc[rt][0].z, sc[rt][0].w)), fmaxf(fmaxf(sc[rt][1].x, sc[rt][1].y), fmaxf(sc[rt][1].z, sc[rt][1].w)));
       top = fmaxf(top, fmaxf(fmaxf(fmaxf(sc[rt][2].x, sc[rt][2].y), fmaxf(sc[rt][2].z, sc[rt][2].w)), fmaxf(fmaxf(sc[rt][3].x, sc[rt][3].y), fmaxf(sc[rt][3].z, sc[rt][3].w))));
-      // The base of the exponents follows the maximum only when it has grown by 2^8: binary16 holds what lies in between.
       const float now = rows_max(top) * a.scale;
-      if (__ballot(now > m[rt] + 8.f)) {
+      if (__ballot(outgrown(now, m[rt]))) {
         const float next = fmaxf(m[rt], now), again = __builtin_amdgcn_exp2f(m[rt] - base_of(next));
         l[rt] *= again;
 #pragma unroll
@@ -221,6 +224,12 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
         m[rt] = next;
       }
       const float base = base_of(m[rt]);
+      float scale = a.scale;
+      if (__builtin_expect(is_large(base), 0)) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sc[rt][t] *= a.scale;
+        scale = 1.f;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -228,10 +237,10 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const float4v x = sc[rt][2 * h + u];
-          e[4 * u] = __builtin_amdgcn_exp2f(__fmaf_rn(x.x, a.scale, -base));
-          e[4 * u + 1] = __builtin_amdgcn_exp2f(__fmaf_rn(x.y, a.scale, -base));
-          e[4 * u + 2] = __builtin_amdgcn_exp2f(__fmaf_rn(x.z, a.scale, -base));
-          e[4 * u + 3] = __builtin_amdgcn_exp2f(__fmaf_rn(x.w, a.scale, -base));
+          e[4 * u] = __builtin_amdgcn_exp2f(__fmaf_rn(x.x, scale, -base));
+          e[4 * u + 1] = __builtin_amdgcn_exp2f(__fmaf_rn(x.y, scale, -base));
+          e[4 * u + 2] = __builtin_amdgcn_exp2f(__fmaf_rn(x.z, scale, -base));
+          e[4 * u + 3] = __builtin_amdgcn_exp2f(__fmaf_rn(x.w, scale, -base));
         }
         sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         // (rounded to nearest: what the matrix cores take; the sum is that of the unrounded ones)

@@ -293,15 +293,22 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       float low, high;
       across_halves(top, low, high);
       const float now = fmaxf(low, high) * a.scale;
-      // The base of the exponents follows the maximum only when it has grown by 2^8: binary16 holds what lies in between.
-      if (__ballot(now > m + 8.f)) {
+      float base = base_of(m);
+      if (__ballot(outgrown(now, m) || is_large(base))) {
         const float next = fmaxf(m, now), again = __builtin_amdgcn_exp2f(m - base_of(next));
         l *= again;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] *= again;
         m = next;
+        base = base_of(next);
+        if (is_large(base)) {                                        // (the differences in place of the scores: one more value in the loop costs scalar spills)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[t].f[r] = (sc[t].f[r] * a.scale - base) * (1.f / a.scale);
+          base = 0.f;
+        }
       }
-      const float base = base_of(m);
       half8v p[2][2];
       float sum = 0.f;
 #pragma unroll

@@ -1,0 +1,85 @@
+"""vq_attention at the ends of its numbers' ranges, against 64 bits."""
+import numpy as np
+import pytest
+
+from test_gpu_attention import Device, _problem
+from test_gpu_attention_long import _attention
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("lengths,news,q_heads,heads,dim,bits,window,sinks", [
+    ([700, 33, 1], [1, 1, 1], 4, 2, 128, 8, 0, 0),
+    ([9000], [1], 2, 1, 64, 16, 0, 0),                               # in parts
+    ([700, 90], [4, 4], 4, 2, 128, 16, 0, 0),
+    ([700, 90], [9, 5], 8, 2, 64, 8, 100, 3),
+    ([300, 40], [7, 1], 2, 1, 80, 8, 0, 0),
+    ([300, 40], [7, 40], 2, 1, 256, 16, 0, 0),
+    ([700, 200], [300, 200], 2, 1, 128, 8, 0, 0),                    # prompts
+    ([700, 200], [300, 200], 2, 2, 64, 16, 90, 1),
+    ([200], [200], 1, 1, 112, 16, 0, 0),
+])
+@pytest.mark.parametrize("size", [2.0, 2.0 ** 5, 2.0 ** 8, 2.0 ** 14])
+def test_scores_of_every_size(gpu_lib, lengths, news, q_heads, heads, dim, bits, window, sinks, size):
+    """Queries and keys of up to 50000: scores of up to 10^10, whose rounding steps are larger than what a softmax tells apart.  The largest score of a token is far
+    above its next in all but a few rows (left out): what comes out is that key's value."""
+    import torch
+    rng, cache, table, k, v, q = _problem(33, lengths, news, q_heads, heads, dim, 16, bits, fill="nan")
+    keys, values = ((rng.standard_normal((sum(lengths), heads, dim)) * gain).clip(-50000, 50000).astype(np.float16) for gain in (size, 1))
+    q = (rng.standard_normal(q.shape) * size).clip(-50000, 50000).astype(np.float16)
+    cache.append(keys, values, table, lengths, lengths)
+    dev = Device(cache, table, lengths, news)
+    out, lse = gpu_lib.attention(torch.from_numpy(q).cuda(), *dev.cache, starts=dev.starts, window=window, sinks=sinks, max_new=max(news), max_length=max(lengths),
+                                 return_lse=True)
+    torch.cuda.synchronize()
+    out, lse = out.cpu().numpy(), lse.cpu().numpy()
+    want, want_lse, _, _, terms = _attention(q, cache, table, lengths, news, dim ** -0.5, window, sinks)
+    error = (dim + 2) * 2.0 ** -24 * terms                           # of a score
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+    assert (np.abs(lse - want_lse) <= error[..., 0] + 2.0 ** -10 + 2.0 ** -22 * np.abs(want_lse)).all()
+    # rows of one key: whose largest score is above all others by more than the errors of both and what a softmax tells apart.  The probability and the result are
+    # rounded to binary16, and what else there is lies within 2^-18
+    alone = _margin(q, cache, table, lengths, news, dim ** -0.5, window, sinks) > 4 * error[..., 0] + 40
+    assert size < 2.0 ** 8 or alone.mean() > 0.9
+    off = np.abs(out[alone].astype(np.float64) - want[alone]) - ((2.0 ** -10 + 2.0 ** -18) * np.abs(want[alone]) + 2.0 ** -24)
+    assert off.max(initial=0) <= 0, off.max()
+
+
+def _margin(q, cache, table, lengths, news, scale, window, sinks):
+    """How far the largest score of every row lies above its next (infinitely where it is the only one)."""
+    from test_gpu_attention_long import _whole
+    margin = np.zeros(q.shape[:2])
+    group, row = q.shape[1] // cache.heads, 0
+    for pages, length, new in zip(table, lengths, news):
+        at, places = length - new + np.arange(new)[:, None], np.arange(length)
+        sees = places <= at
+        if window:
+            sees &= (places > at - window) | (places < sinks)
+        for g in range(q.shape[1]):
+            K, _, there = _whole(cache, pages, length, g // group)
+            s = np.where(sees & there, q[row: row + new, g].astype(np.float64) @ np.where(there[:, None], K, 0).T * scale, -np.inf)
+            top = np.sort(np.concatenate([np.full((new, 1), -np.inf), s], 1), 1)[:, -2:]
+            margin[row: row + new, g] = top[:, 1] - top[:, 0]
+        row += new
+    return margin
+
+
+@pytest.mark.parametrize("lengths,news,q_heads,heads,dim,bits", [
+    ([300, 90], [1, 1], 16, 1, 128, 8), ([300, 90], [5, 9], 4, 2, 64, 16), ([300, 90], [5, 9], 4, 2, 80, 8), ([300, 200], [130, 200], 2, 1, 128, 16), ([300, 200], [130, 200], 2, 2, 64, 8),
+])
+def test_a_query_of_large_scores_beside_others(gpu_lib, lengths, news, q_heads, heads, dim, bits):
+    """The other rows get what they get without it, bit for bit."""
+    import torch
+    rng, cache, table, k, v, q = _problem(34, lengths, news, q_heads, heads, dim, 16, bits)
+    cache.append(k, v, table, lengths, news)
+    dev = Device(cache, table, lengths, news)
+    results = []
+    for gain in (1, 10000):
+        q2 = q.copy()
+        q2[::7, 0] *= np.float16(gain)
+        results.append(gpu_lib.attention(torch.from_numpy(q2).cuda(), *dev.cache, starts=dev.starts, max_new=max(news), max_length=max(lengths), return_lse=True, scale=500.0))
+    torch.cuda.synchronize()
+    others = torch.ones(q.shape[:2], dtype=torch.bool, device="cuda")
+    others[::7, 0] = False
+    assert (results[1][1][::7, 0].abs() > 4194304).any() and all(torch.isfinite(x).all() for x in results[1])
+    assert torch.equal(results[0][0][others], results[1][0][others]) and torch.equal(results[0][1][others], results[1][1][others])
