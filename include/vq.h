@@ -348,7 +348,8 @@ int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void
  *     out[t][h] = sum_j softmax_j(softmax_scale * q[t][h] . K[j]) V[j]
  * over the places j that token t at place p sees: j <= p, and with window > 0 also j > p - window or j < sinks.  A token that sees
  * nothing gets zeros.  lse (may be NULL): binary32 [n_tokens][q_heads], the logarithm of the sum of exp(score), -inf for such tokens.
- * Scores, statistics and sums are binary32; the probabilities (relative to the largest so far) are rounded to binary16 for the matrix cores, the result once.
+ * Scores, statistics and sums are binary32; the probabilities (relative to a base at least 2^7 below the largest so far) are rounded to binary16 for the matrix
+ * cores, the result once.
  * Keys and values nobody sees may hold anything, NaN included.  Codes are widened to binary16: what they stand for has to lie within its range (as what
  * vq_kv_append stores of numbers up to 63488 does), beyond it is infinite.  softmax_scale must be finite and positive.
  * Workspace (device memory, 256-byte aligned, contents undefined afterwards): with vq_attention_workspace_bytes bytes a

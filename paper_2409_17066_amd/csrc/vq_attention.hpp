@@ -150,10 +150,13 @@ __device__ __forceinline__ unsigned long long seen64_of(const AttentionParams &a
          (unsigned long long)(seen_of(a, s, place, base + 32) | seen_of(a, s, place, base + 48) << 16) << 32;
 }
 
-// A finite stand-in for the maximum of a row that has seen nothing yet.
+// A finite stand-in for the base of a row that has seen nothing yet.
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
-// The base of a row's exponents follows the maximum only when it has grown by 2^8: binary16 holds what lies in between.  (The difference is exact; m + 8 is not.)
-__device__ __forceinline__ bool outgrown(float now, float m) { return now - m > 8.f; }
+// The base of a row's exponents lies 2^7 below its maximum and follows it when that has grown by 2^7 more: probabilities of up to 2^14 in binary16, which rounds to zero below
+// 2^-25, at least 2^-32 of the largest.  With the base at the maximum a long tail behind a key that outweighs it (a first token, say) is lost from 17 below on, where
+// it may be all that comes out.  (The difference is exact; m + 14 is not.)
+constexpr float BELOW = 7.f;
+__device__ __forceinline__ bool outgrown(float now, float m) { return now - m > 2.f * BELOW; }
 // Exponents are score * scale - base in one rounding and the base is a rounded product: past 2^22 they would be off by more than they may grow, and from 2^28 on
 // probabilities infinite.  There the products are rounded as the base is.
 __device__ __forceinline__ bool is_large(float base) { return __builtin_fabsf(base) > 4194304.f; }

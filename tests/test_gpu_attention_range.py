@@ -1,4 +1,7 @@
-"""vq_attention at the ends of its numbers' ranges, against 64 bits."""
+"""vq_attention at the ends of its numbers' ranges, against 64 bits.
+
+Bound of the error behind a long tail: that of tests/test_gpu_attention_long.py but for the probabilities' absolute error.  They are binary16 numbers relative to a
+base at least 2^7 below the largest so far, so that the absolute error 2^-25 of the small ones is 2^-32 of the largest."""
 import numpy as np
 import pytest
 
@@ -83,3 +86,54 @@ def test_a_query_of_large_scores_beside_others(gpu_lib, lengths, news, q_heads, 
     others[::7, 0] = False
     assert (results[1][1][::7, 0].abs() > 4194304).any() and all(torch.isfinite(x).all() for x in results[1])
     assert torch.equal(results[0][0][others], results[1][0][others]) and torch.equal(results[0][1][others], results[1][1][others])
+
+
+def _check(got, lse, want, want_lse, weight, floor, terms, dim, keys):
+    sums = (keys / 16 + 64) * 2.0 ** -24
+    scores = 2 * (dim + 2) * 2.0 ** -24 * terms
+    bound = (2.0 ** -10 + 2.0 ** -18 + 2 * sums + scores) * weight + 2.0 ** -32 * floor + 2.0 ** -24
+    off = np.abs(got.astype(np.float64) - want) - bound
+    assert np.isfinite(got).all() and off.max() <= 0, (np.unravel_index(off.argmax(), off.shape), off.max())
+    near = np.abs(lse - want_lse)
+    assert (near <= scores[..., 0] + 2.0 ** -18 + sums + 2.0 ** -22 * np.abs(want_lse)).all(), near.max()
+
+
+TAILS = [
+    # lengths, news, q heads, heads, dim, bits, window, sinks
+    ([3000, 70], [1, 1], 2, 2, 128, 8, 0, 0),
+    ([3000, 70], [1, 1], 2, 2, 64, 16, 0, 0),
+    ([9000], [1], 1, 1, 128, 8, 0, 0),                               # in parts
+    ([5000, 900], [4, 4], 4, 2, 128, 16, 0, 0),                      # drafted tokens
+    ([2000], [9], 4, 2, 64, 8, 0, 0),
+    ([2500, 600], [1, 3], 2, 1, 80, 8, 0, 0),                        # padded heads
+    ([2500], [1], 2, 1, 256, 16, 0, 0),
+    ([3000], [140], 1, 1, 128, 8, 0, 0),                             # chunks of prompts
+    ([2600, 700], [90, 33], 4, 2, 64, 16, 0, 0),
+    ([1500], [70], 1, 1, 96, 16, 0, 0),
+    ([4000, 500], [1, 1], 4, 2, 128, 8, 1500, 1),                    # the dominant key is a first token that stays
+    ([4000], [70], 2, 2, 128, 16, 1500, 4),
+]
+
+
+@pytest.mark.parametrize("case", TAILS, ids=str)
+@pytest.mark.parametrize("gap", [14.0, 17.0, 19.0])
+def test_the_tail_behind_a_key_of_no_value(gpu_lib, case, gap):
+    """Each sequence's first key has a score `gap` above all others and a value of zeros: what comes out is the tail alone."""
+    import torch
+    lengths, news, q_heads, heads, dim, bits, window, sinks = case
+    rng, cache, table, k, v, q = _problem(31, lengths, news, q_heads, heads, dim, 16, bits, fill="nan")
+    along = rng.standard_normal((heads, dim))
+    along /= np.linalg.norm(along, axis=1, keepdims=True)
+    tokens = sum(lengths)
+    keys = (0.3 * rng.standard_normal((tokens, heads, dim))).astype(np.float16)
+    values = (1 + 0.25 * rng.standard_normal((tokens, heads, dim))).astype(np.float16)
+    first = np.concatenate([[0], np.cumsum(lengths)])[:-1]
+    keys[first] = along * gap * np.sqrt(dim) / 8
+    values[first] = 0
+    q = (8 * np.repeat(along, q_heads // heads, 0) + 0.01 * rng.standard_normal(q.shape)).astype(np.float16)
+    cache.append(keys, values, table, lengths, lengths)
+    dev = Device(cache, table, lengths, news)
+    out, lse = gpu_lib.attention(torch.from_numpy(q).cuda(), *dev.cache, starts=dev.starts, window=window, sinks=sinks, max_new=max(news), max_length=max(lengths),
+                                 return_lse=True)
+    torch.cuda.synchronize()
+    _check(out.cpu().numpy(), lse.cpu().numpy(), *_attention(q, cache, table, lengths, news, dim ** -0.5, window, sinks), dim, max(lengths))
