@@ -154,7 +154,8 @@ __device__ __forceinline__ unsigned long long seen64_of(const AttentionParams &a
 __device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
 // The base of a row's exponents lies 2^7 below its maximum and follows it when that has grown by 2^7 more: probabilities of up to 2^14 in binary16, which rounds to zero below
 // 2^-25, at least 2^-32 of the largest.  With the base at the maximum a long tail behind a key that outweighs it (a first token, say) is lost from 17 below on, where
-// it may be all that comes out.  (The difference is exact; m + 14 is not.)
+// it may be all that comes out.  (The difference is exact; m + 14 is not.)  Every row's by its own scores
+// alone, so that no result depends on what rows a tile puts side by side.
 constexpr float BELOW = 7.f;
 __device__ __forceinline__ bool outgrown(float now, float m) { return now - m > 2.f * BELOW; }
 // Exponents are score * scale - base in one rounding and the base is a rounded product: past 2^22 they would be off by more than they may grow, and from 2^28 on

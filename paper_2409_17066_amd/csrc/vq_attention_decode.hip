@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
       top = fmaxf(top, fmaxf(fmaxf(fmaxf(sc[rt][2].x, sc[rt][2].y), fmaxf(sc[rt][2].z, sc[rt][2].w)), fmaxf(fmaxf(sc[rt][3].x, sc[rt][3].y), fmaxf(sc[rt][3].z, sc[rt][3].w))));
       const float now = rows_max(top) * a.scale;
       if (__ballot(outgrown(now, m[rt]))) {
-        const float next = fmaxf(m[rt], now - BELOW), again = __builtin_amdgcn_exp2f(m[rt] - base_of(next));
+        const float next = outgrown(now, m[rt]) ? now - BELOW : m[rt], again = __builtin_amdgcn_exp2f(m[rt] - base_of(next));
         l[rt] *= again;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[rt][dt] *= again;

@@ -295,7 +295,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       const float now = fmaxf(low, high) * a.scale;
       float base = base_of(m);
       if (__ballot(outgrown(now, m) || is_large(base))) {
-        const float next = fmaxf(m, now - BELOW), again = __builtin_amdgcn_exp2f(m - base_of(next));
+        const float next = outgrown(now, m) ? now - BELOW : m, again = __builtin_amdgcn_exp2f(m - base_of(next));
         l *= again;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] *= again;

@@ -88,6 +88,25 @@ def test_a_query_of_large_scores_beside_others(gpu_lib, lengths, news, q_heads, 
     assert torch.equal(results[0][0][others], results[1][0][others]) and torch.equal(results[0][1][others], results[1][1][others])
 
 
+@pytest.mark.parametrize("lengths,news,q_heads,heads,dim,bits", [
+    ([700, 90], [1, 1], 16, 1, 128, 8), ([700, 90], [1, 1], 8, 1, 64, 16), ([700, 90], [5, 9], 4, 2, 64, 16), ([700, 90], [5, 9], 4, 2, 80, 8),
+    ([700, 200], [130, 200], 2, 1, 128, 16), ([700, 200], [130, 200], 2, 2, 64, 8),
+])
+def test_rows_do_not_depend_on_one_another(gpu_lib, lengths, news, q_heads, heads, dim, bits):
+    """Every second query of another size: the others get the same bits, though their tiles' maxima grow at other keys."""
+    import torch
+    rng, cache, table, k, v, q = _problem(35, lengths, news, q_heads, heads, dim, 16, bits)
+    cache.append(k, v, table, lengths, news)
+    dev = Device(cache, table, lengths, news)
+    results = []
+    for gain in (1, 12):
+        q2 = q.copy()
+        q2[:, ::2] *= np.float16(gain)
+        results.append(gpu_lib.attention(torch.from_numpy(q2).cuda(), *dev.cache, starts=dev.starts, max_new=max(news), max_length=max(lengths), return_lse=True))
+    torch.cuda.synchronize()
+    assert torch.equal(results[0][0][:, 1::2], results[1][0][:, 1::2]) and torch.equal(results[0][1][:, 1::2], results[1][1][:, 1::2])
+
+
 def _check(got, lse, want, want_lse, weight, floor, terms, dim, keys):
     sums = (keys / 16 + 64) * 2.0 ** -24
     scores = 2 * (dim + 2) * 2.0 ** -24 * terms
