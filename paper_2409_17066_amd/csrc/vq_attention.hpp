@@ -81,6 +81,27 @@ __device__ __forceinline__ float rows_sum(float x) {
   return a + b;
 }
 
+// Scales past 2^7, with which a code may stand for more than binary16 holds (448 times 2^7 is 57344; 65504 is stored as the code of 256 times 2^8).  Keys are widened with
+// 2^7 and what is left of the scale multiplies their scores.  Values beyond the largest number count as that, as an infinity would be not a number in the sums of rows that do
+// not see it: of the widened ones (finite_of), or where those are not together in registers of the codes, at 2^16, of which the probability takes a factor of two.
+constexpr float WIDEST = 128.f;
+__device__ __forceinline__ bool is_wide(float scale) { return !(scale <= WIDEST); }
+__device__ __forceinline__ float rest_of(float scale) { return is_wide(scale) ? scale * (1.f / WIDEST) : 1.f; }
+__device__ __forceinline__ unsigned finite_of(unsigned halves) {
+  return halves - ((halves & 0x7fffu) == 0x7c00u ? 1u : 0u) - ((halves & 0x7fff0000u) == 0x7c000000u ? 0x10000u : 0u);
+}
+// Codes of values past 2^16 as those of 2^16; NaN stays.
+__device__ __forceinline__ unsigned limited(unsigned codes, float scale) {
+  const int k = 16 - ((int)(__float_as_uint(scale) >> 23 & 0xff) - 127);       // code 8 (k + 7) is 2^k, down to 2^-6, below that 2^(k + 9)
+  const unsigned most = (k >= -6 ? 8 * (k + 7) : 1u << max(k + 9, 0)) * 0x01010101u, size = codes & 0x7f7f7f7fu;
+  const unsigned more = (size + (0x7f7f7f7fu - most)) & ~(size + 0x01010101u) & 0x80808080u, all = more | (more - (more >> 7));
+  return (codes & ~(all & 0x7f7f7f7fu)) | (most & all);
+}
+__device__ __forceinline__ half8v finite_of(half8v x) {
+  const uint4v u = __builtin_bit_cast(uint4v, x);
+  return __builtin_bit_cast(half8v, uint4v{finite_of(u.x), finite_of(u.y), finite_of(u.z), finite_of(u.w)});
+}
+
 __device__ __forceinline__ half8v halves_of_e4m3(unsigned a, unsigned b, float scale) {
   const half2v w = halves_of_e4m3<false>(a, scale), x = halves_of_e4m3<true>(a, scale), y = halves_of_e4m3<false>(b, scale), z = halves_of_e4m3<true>(b, scale);
   return half8v{w.x, w.y, x.x, x.y, y.x, y.y, z.x, z.y};

@@ -134,14 +134,15 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
     if (!V_AHEAD && !AHEAD) load_k(i);
     float4v sc[RT][4];
     bool odd = false;
+    const float k_by = E4M3 ? fminf(k_scale, WIDEST) : 1.f;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       half8v f[STEPS];
 #pragma unroll
       for (int w = 0; w < KL; ++w) {
         if constexpr (E4M3) {
-          f[2 * w] = halves_of_e4m3(k[t][w].x, k[t][w].y, k_scale);
-          f[2 * w + 1] = halves_of_e4m3(k[t][w].z, k[t][w].w, k_scale);
+          f[2 * w] = halves_of_e4m3(k[t][w].x, k[t][w].y, k_by);
+          f[2 * w + 1] = halves_of_e4m3(k[t][w].z, k[t][w].w, k_by);
         } else {
           f[w] = __builtin_bit_cast(half8v, k[t][w]);
         }
@@ -153,6 +154,13 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
         for (int w = 0; w < STEPS; ++w) x = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[w], q[rt][w], x, 0, 0, 0);
         sc[rt][t] = x;
       }
+    }
+    if (E4M3 && __builtin_expect(__ballot(is_wide(k_scale)) != 0, 0)) {
+      const float rest = rest_of(__shfl(k_scale, 4 * g));           // (that lane has loaded keys of this one's sixteen)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sc[rt][t] *= rest;
     }
     if (AHEAD && next < end) load_k(next);
     if (!V_AHEAD) {
@@ -247,6 +255,20 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
         p[rt][h] = half8v{(_Float16)e[0], (_Float16)e[1], (_Float16)e[2], (_Float16)e[3], (_Float16)e[4], (_Float16)e[5], (_Float16)e[6], (_Float16)e[7]};
       }
       l[rt] += sum;
+    }
+    if (E4M3 && __builtin_expect(__ballot(is_wide(v_scale)) != 0, 0)) {
+      const _Float16 two = is_wide(v_scale) ? (_Float16)2.f : (_Float16)1.f;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) p[rt][h] *= half8v{two, two, two, two, two, two, two, two};
+      if (is_wide(v_scale)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int w = 0; w < VL; ++w) v[dt][w] = uint4v{limited(v[dt][w].x, v_scale), limited(v[dt][w].y, v_scale), limited(v[dt][w].z, v_scale), limited(v[dt][w].w, v_scale)};
+        v_scale *= 0.5f;
+      }
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {

@@ -48,8 +48,9 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   constexpr int K_BYTES = 64 * D * 2, BUFFER = 2 * K_BYTES;
   constexpr int STEPS = D / 16, DT = D / 32, AHEAD = 6;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  unsigned char *there = lds + 2 * BUFFER;                         // [2][4]: bit 0, whether each sixteen keys of a buffer have a page; 1: values to be put back
+  unsigned char *there = lds + 2 * BUFFER;                         // [2][4]: bit 0, whether each sixteen keys of a buffer have a page; 1: values to be put back; 2: rests of keys' scales
   auto bits_of = [](int buffer) { return 2 * BUFFER + 16 + buffer * (Odd<E4M3>::KINDS * D * 8); };
+  auto rests_of = [=](int buffer) { return bits_of(2) + buffer * (REPS * WAVES * 4); };      // [word][wave]
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
 
   // Long sequences first and of each the rows that see most, so that short work fills the end; where all workgroups are resident at once, so that
@@ -196,21 +197,44 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       }
       odd = __ballot(odd) != 0;
     }
+    auto words = [&](auto any_wide) {
+      constexpr bool WIDE = decltype(any_wide)::value;
 #pragma unroll
-    for (int r = 0; r < REPS; ++r) {
-      const int row = row_of_key(r * K_STEP);                       // how far key k_key + r * K_STEP is from k_key: row 4 has its slots mixed otherwise
-      const unsigned mixed = (SLOTS == 16 ? row & 15 : 0) * 16u, k_further = INTO * BUFFER + row * SLOTS * 16, v_further = INTO * BUFFER + r * V_STEP * 8 * 16;
-      if constexpr (E4M3) {
-        put((k_to ^ mixed) + k_further, __builtin_bit_cast(uint4v, halves_of_e4m3(kw[r].x, kw[r].y, ks[r])));
-        put((k_to ^ mixed ^ 16u) + k_further, __builtin_bit_cast(uint4v, halves_of_e4m3(kw[r].z, kw[r].w, ks[r])));
-        put(v_to + v_further, __builtin_bit_cast(uint4v, halves_of_e4m3(vw[r].x, vw[r].y, vs)));
-        put((v_to ^ 16u) + v_further, __builtin_bit_cast(uint4v, halves_of_e4m3(vw[r].z, vw[r].w, vs)));
-      } else {
-        put((k_to ^ mixed) + k_further, kw[r]);
-        put(v_to + v_further, vw[r]);
+      for (int r = 0; r < REPS; ++r) {
+        const int row = row_of_key(r * K_STEP);                     // how far key k_key + r * K_STEP is from k_key: row 4 has its slots mixed otherwise
+        const unsigned mixed = (SLOTS == 16 ? row & 15 : 0) * 16u, k_further = INTO * BUFFER + row * SLOTS * 16, v_further = INTO * BUFFER + r * V_STEP * 8 * 16;
+        if constexpr (E4M3) {
+          const float by = WIDE ? fminf(ks[r], WIDEST) : ks[r];
+          auto value = [&](unsigned a, unsigned b) {
+            const half8v x = halves_of_e4m3(a, b, vs);
+            return __builtin_bit_cast(uint4v, WIDE ? finite_of(x) : x);
+          };
+          put((k_to ^ mixed) + k_further, __builtin_bit_cast(uint4v, halves_of_e4m3(kw[r].x, kw[r].y, by)));
+          put((k_to ^ mixed ^ 16u) + k_further, __builtin_bit_cast(uint4v, halves_of_e4m3(kw[r].z, kw[r].w, by)));
+          put(v_to + v_further, value(vw[r].x, vw[r].y));
+          put((v_to ^ 16u) + v_further, value(vw[r].z, vw[r].w));
+        } else {
+          put((k_to ^ mixed) + k_further, kw[r]);
+          put(v_to + v_further, vw[r]);
+        }
       }
+    };
+    float widest = vs;
+    if (E4M3)
+#pragma unroll
+      for (int r = 0; r < REPS; ++r) widest = fmaxf(widest, ks[r]);
+    const bool any_wide = E4M3 && __ballot(is_wide(widest)) != 0;
+    if (E4M3 && __builtin_expect(any_wide, 0)) {
+      words(std::true_type{});
+      // What is left of the scales of keys, of which a wave brings sixteen or, of heads of more than 64 elements, eight of every 32.
+      if (lane == 0)
+#pragma unroll
+        for (int r = 0; r < REPS; ++r)
+          *(__attribute__((address_space(3))) float *)(size_t)(lds_at + rests_of(INTO) + (r * WAVES + wave) * 4) = rest_of(ks[r]);
+    } else {
+      words(std::false_type{});
     }
-    if (lane == 0) there[INTO * 4 + wave] = (unsigned char)(v_there | odd << 1);
+    if (lane == 0) there[INTO * 4 + wave] = (unsigned char)(v_there | odd << 1 | any_wide << 2);
   };
 
   // first places of the chunks that are computed, stored to LDS and looked up in the page table next
@@ -280,6 +304,18 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       __builtin_amdgcn_sched_group_barrier(0x8, AHEAD - DT, 0);
       const unsigned is = (unsigned)__builtin_amdgcn_readfirstlane(pages);
       if (is != 0x01010101u || j0 + 63 > place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= place_max - a.window)) {
+        if (E4M3 && (is & 0x04040404u)) {
+          // (what the wave that brought this lane's keys of a tile has left of their scale)
+          auto rest_at = [&](int r, int by) {
+            return is >> (8 * by) & 4 ? *(const __attribute__((address_space(3))) float *)(size_t)(lds_at + rests_of(OF) + (r * WAVES + by) * 4) : 1.f;
+          };
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const float rest = REPS == 1 ? rest_at(0, 2 * t + h) : rest_at(t, 2 * h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[t].f[r] *= rest;
+          }
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const unsigned seen = is >> (16 * t + 8 * h) & 1 ? seen_of(a, s, place, j0 + 32 * t + 16 * h) : 0;
@@ -394,7 +430,7 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
   const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
   if (blocks > 0xffffffffll / THREADS) return VQ_ERR_SHAPE;        // (threads of a grid)
   VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D, EXACT>));
-  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D, EXACT>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8, stream, c, a, s, tiles,
+  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D, EXACT>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8 + (E4M3 ? 2 * (D / 64) * WAVES * 4 : 0), stream, c, a, s, tiles,
                      blocks <= 2 * cu_count());
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }

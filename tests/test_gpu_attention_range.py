@@ -107,10 +107,10 @@ def test_rows_do_not_depend_on_one_another(gpu_lib, lengths, news, q_heads, head
     assert torch.equal(results[0][0][:, 1::2], results[1][0][:, 1::2]) and torch.equal(results[0][1][:, 1::2], results[1][1][:, 1::2])
 
 
-def _check(got, lse, want, want_lse, weight, floor, terms, dim, keys):
+def _check(got, lse, want, want_lse, weight, floor, terms, dim, keys, values=0.0):
     sums = (keys / 16 + 64) * 2.0 ** -24
     scores = 2 * (dim + 2) * 2.0 ** -24 * terms
-    bound = (2.0 ** -10 + 2.0 ** -18 + 2 * sums + scores) * weight + 2.0 ** -32 * floor + 2.0 ** -24
+    bound = (2.0 ** -10 + 2.0 ** -18 + values + 2 * sums + scores) * weight + 2.0 ** -32 * floor + 2.0 ** -24
     off = np.abs(got.astype(np.float64) - want) - bound
     assert np.isfinite(got).all() and off.max() <= 0, (np.unravel_index(off.argmax(), off.shape), off.max())
     near = np.abs(lse - want_lse)
@@ -156,3 +156,70 @@ def test_the_tail_behind_a_key_of_no_value(gpu_lib, case, gap):
                                  return_lse=True)
     torch.cuda.synchronize()
     _check(out.cpu().numpy(), lse.cpu().numpy(), *_attention(q, cache, table, lengths, news, dim ** -0.5, window, sinks), dim, max(lengths))
+
+
+LARGE = [
+    # lengths, news, q heads, heads, dim, page, window, sinks
+    ([200, 70], [4, 4], 8, 2, 128, 16, 0, 0),
+    ([150, 90], [7, 16], 8, 2, 64, 64, 40, 3),
+    ([150, 90], [20, 16], 2, 1, 64, 16, 0, 0),
+    ([300, 130], [130, 129], 4, 2, 128, 16, 0, 0),
+    ([300, 130], [130, 129], 2, 2, 64, 128, 70, 2),
+    ([300], [300], 2, 2, 128, 64, 0, 0),
+    ([90, 170], [40, 3], 2, 1, 80, 16, 33, 2),
+    ([90], [90], 2, 2, 48, 32, 0, 0),
+    ([200, 90], [9, 5], 2, 2, 192, 16, 0, 0),
+    ([200, 90], [9, 5], 2, 2, 256, 32, 50, 1),
+    ([3000, 500], [4, 4], 2, 2, 128, 16, 0, 0),                      # in parts
+    ([400, 33], [1, 1], 4, 2, 128, 16, 0, 0),                        # single tokens
+    ([400, 33], [1, 1], 4, 2, 112, 16, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", LARGE, ids=str)
+@pytest.mark.parametrize("switches", ["", "attention=d", "attention=p"])
+@pytest.mark.parametrize("top", [2.0 ** 8, 2.0 ** 12])
+def test_codes_that_stand_for_more_than_binary16_holds(gpu_lib, monkeypatch, case, switches, top):
+    """65504 and -65504 appended in 8 bits are the codes of 256 times 2^8.  In the pages of a token in the middle of the new ones of each sequence scales are that, or larger
+    yet: tokens that do not see it get, bit for bit, what they get where it stands for half of that, the others what the sums in 64 bits are.  Values beyond count as
+    65536 or as the largest number of binary16, 2^-11 less."""
+    import torch
+    monkeypatch.setenv("VQ_SWITCHES", switches)
+    lengths, news, q_heads, heads, dim, size, window, sinks = case
+    rng, cache, table, k, v, q = _problem(32, lengths, news, q_heads, heads, dim, size, 8)
+    cache.append(k, v, table, lengths, news)
+    q = (q * np.float16(2.0 ** -6)).astype(np.float16)              # (scores of keys that large stay small)
+    hit = np.zeros(len(q), bool)
+    at = []
+    row = 0
+    for b, (length, new) in enumerate(zip(lengths, news)):
+        place = length - new + new // 2
+        page = table[b, place // size]
+        cache.k_scales[page] = cache.v_scales[page] = top
+        cache.k[page], cache.v[page] = cache.k[page] & 0x9f, cache.v[page] & 0x9f          # (the page's other tokens: below 2^-3, times that)
+        at.append((page, place % size))
+        for u in range(new):
+            here = length - new + u
+            hit[row + u] = place <= here and (not window or place > here - window or place < sinks)
+        row += new
+
+    def run(code, key):
+        for page, offset in at:
+            cache.v[page, :, ::2, offset], cache.v[page, :, 1::2, offset] = code, code | 0x80
+            cache.k[page, :, offset, 1] = key
+        dev = Device(cache, table, lengths, news)
+        out, lse = gpu_lib.attention(torch.from_numpy(q).cuda(), *dev.cache, starts=dev.starts, window=window, sinks=sinks, max_new=max(news), max_length=max(lengths),
+                                     return_lse=True)
+        torch.cuda.synchronize()
+        return out.cpu().numpy(), lse.cpu().numpy()
+    half, half_lse = run(0x70, 0x70)
+    for code, key in ((0x78, 0x70), (0x70, 0x7b), (0x78, 0xfb)):     # 256; 352, which a rotated key reaches, and -352
+        got, lse = run(code, key)
+        assert np.array_equal(got[~hit].view(np.uint16), half[~hit].view(np.uint16)) and np.array_equal(lse[~hit], half_lse[~hit])
+        if top > 256:
+            for page, offset in at:
+                cache.v[page, :, ::2, offset], cache.v[page, :, 1::2, offset] = 0x58, 0xd8          # 16 times 2^12
+        want = _attention(q, cache, table, lengths, news, dim ** -0.5, window, sinks)
+        fits = np.abs(want[0]) < 65000                               # (a token that sees little else: more than the result's type holds)
+        assert np.array_equal(np.sign(got[~fits]), np.sign(want[0][~fits]))
+        _check(np.where(fits, got, 0), lse, np.where(fits, want[0], 0), *want[1:], dim, max(lengths), values=2.0 ** -11)
