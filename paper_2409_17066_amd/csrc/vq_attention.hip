@@ -27,6 +27,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
   Plan best{};
   const long long rows = (long long)c.max_new * a.group, slots = cu_count();
   float least = 0.f;
+  parts_allowed = parts_allowed && attention_join_takes(c, a);
   for (const bool prompt : {false, true}) {
     const char forced = attention_prompt_takes(c) ? switches().attention : 'd';
     if (forced == 'd' || forced == 'p' ? prompt != (forced == 'p') : !prompt && rows > 512) continue;
@@ -44,7 +45,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
       const float turns = parts > 1 ? (float)(((chunks + run - 1) / run + parts - 1) / parts) : prompt ? (float)chunks / (float)run : (float)((chunks + run - 1) / run);
       const float one = 1.2f + 0.1f * quarters, two = 0.7f + 0.6f * quarters, shared = std::min(std::max(work / alone - 1.f, 0.f), 1.f);
       const float step = !prompt ? 3.2f * size * (c.e4m3 ? 1.f : 2.f) : run * size * (one + (two - one) * shared);
-      const float join = parts > 1 ? 5.f + (float)(c.n_seqs * c.kv_heads * rows) * (0.3e-3f + (float)parts * size * 1024.f / 4.5e6f) : 0.f;
+      const float join = parts > 1 ? 5.f + (float)((long long)c.n_seqs * c.kv_heads * rows) * (0.3e-3f + (float)parts * size * 1024.f / 4.5e6f) : 0.f;
       const float time = (prompt ? 12.f + 5.f * size * (rounds - 1.f) : 9.f) + join + rounds * turns * step;
       if (least == 0.f || time < least) {
         least = time;

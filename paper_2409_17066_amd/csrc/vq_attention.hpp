@@ -22,6 +22,8 @@ int launch_attention_decode(const KvParams &c, const AttentionParams &a, const S
 int attention_prompt_rows();
 bool attention_prompt_takes(const KvParams &c);
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
+// The launch that joins parts: whether a grid can have so many rows and sequences.
+bool attention_join_takes(const KvParams &c, const AttentionParams &a);
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
 
 // Bytes from a page's start to word w (of the keys, sixteen bytes each, four lane groups apart) that lane n + 16 g of the decode kernel loads of a key in tile t of a chunk whose sixteen

@@ -470,9 +470,11 @@ int launch_attention_decode(const KvParams &c, const AttentionParams &a, const S
   return c.max_new > 1 ? launch_decode<true>(c, a, s, stream) : launch_decode<false>(c, a, s, stream);
 }
 
+bool attention_join_takes(const KvParams &c, const AttentionParams &a) {
+  return c.n_seqs <= 65535 && (long long)c.max_new * a.group <= 0xffffffffll / JOIN_THREADS;
+}
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream) {
   const dim3 blocks(c.max_new * a.group, c.kv_heads, c.n_seqs);
-  if (c.n_seqs > 65535) return VQ_ERR_SHAPE;
   auto kernel = c.head_dim <= 64 ? attention_join_kernel<64> : c.head_dim <= 128 ? attention_join_kernel<128> : attention_join_kernel<256>;
   hipLaunchKernelGGL(kernel, blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows);
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
