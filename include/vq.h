@@ -309,7 +309,7 @@ typedef struct vq_kv_desc {
   int32_t kv_heads, head_dim;              /* 1 .. 65535 (query heads too); a multiple of 16, at most 256  */
   int32_t page_tokens;                     /* 16, 32, 64, 128 or 256                                       */
   int32_t n_pages;                         /* pages in the pool                                            */
-  int32_t n_seqs, n_tokens;                /* sequences and new tokens of this call                        */
+  int32_t n_seqs, n_tokens;                /* sequences and new tokens of this call, tokens up to 2^30     */
   int32_t max_new, max_length;             /* of one sequence; max_length <= table_pages * page_tokens and 2^30 */
   int32_t table_pages;                     /* entries of a row of page_table                               */
   int32_t reserved;                        /* 0                                                            */

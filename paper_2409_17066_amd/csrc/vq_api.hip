@@ -380,7 +380,7 @@ int make_kv_params(const vq_kv_desc *d, KvParams *p) {
   int shift = 4;
   while (shift < 8 && (1 << shift) != d->page_tokens) ++shift;
   if ((1 << shift) != d->page_tokens) return VQ_ERR_SHAPE;
-  if (d->n_pages < 1 || d->n_seqs < 1 || d->n_tokens < 1 || d->max_new < 1 || d->max_new > d->n_tokens || d->max_length < 0 || d->max_length > 1 << 30) return VQ_ERR_SHAPE;
+  if (d->n_pages < 1 || d->n_seqs < 1 || d->n_tokens < 1 || d->n_tokens > 1 << 30 || d->max_new < 1 || d->max_new > d->n_tokens || d->max_length < 0 || d->max_length > 1 << 30) return VQ_ERR_SHAPE;
   if (d->table_pages < 0 || d->max_length > (long long)d->table_pages * d->page_tokens || d->table_stride < d->table_pages) return VQ_ERR_SHAPE;
   if (!d->starts && (d->n_tokens % d->n_seqs != 0 || d->max_new < d->n_tokens / d->n_seqs)) return VQ_ERR_SHAPE;
   if (!d->k_pages || !d->v_pages || !d->lengths || (!d->page_table && d->table_pages) || (e4m3 && (!d->k_scales || !d->v_scales))) return VQ_ERR_NULL;

@@ -91,3 +91,11 @@ def test_calls_are_launched_whole_or_not_at_all(tmp_path):
             assert 1 <= x and x * launch["threads"] < 2 ** 32 and 1 <= y <= 65535 and 1 <= z <= 65535 and launch["lds"] <= 160 * 1024, (call, launch)
             assert launch["threads"] <= 1024
     assert 0 < refused < len(calls) // 2
+
+
+def test_more_tokens_than_places(tmp_path):
+    """Numbers of new tokens whose pages cannot be counted in 32 bits, and places before a sequence's first that cannot."""
+    calls = [dict(entry=entry, q_heads=1, cache=cache(1, each, 1, 16, 256, 64, starts=starts)) for entry in ("append", "attention") for starts in (False, True)
+             for each in (2 ** 30 + 1, 2 ** 31 - 300, 2 ** 31 - 1)]
+    for call, answer in zip(calls, run(calls, tmp_path)):
+        assert answer["status"] == -2 and not answer["launches"] and not answer["asked"], (call, answer)
