@@ -292,6 +292,11 @@ float number(PyObject *o, const char *name) {
   if (x == -1.0 && PyErr_Occurred()) { PyErr_Clear(); refuse(name, "a number is expected"); }
   return (float)x;
 }
+bool truth(PyObject *o, const char *name) {
+  const int x = PyObject_IsTrue(o);
+  if (x < 0) { PyErr_Clear(); refuse(name, "a truth value is expected"); }
+  return x != 0;
+}
 int64_t leading(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.numel(); }       // (one row: its stride may say anything)
 
 // [tokens][heads][head_dim] with adjacent heads
@@ -363,8 +368,7 @@ PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (cos->sizes() != sin->sizes() || !apart(*cos, 1, 1) || !apart(*sin, 1, 1) || leading(*cos) != leading(*sin)) refuse("cos, sin", "[positions][pairs] of the same layout is expected");
     const at::Tensor *position = tensor(args[15], "position", at::kInt, 1, true);
     if (position && (position->size(0) != k.size(0) || !apart(*position, 0, 1))) refuse("position", "one entry for each token is expected");
-    const int turned = PyObject_IsTrue(args[16]);
-    if (turned < 0) { PyErr_Clear(); refuse("interleaved", "a truth value is expected"); }
+    const int turned = truth(args[16], "interleaved");
     r = vq_rotary{static_cast<const float *>(cos->data_ptr()), static_cast<const float *>(sin->data_ptr()), leading(*cos), narrow(cos->size(0), "cos"),
                   narrow(2 * cos->size(1), "cos"), turned, position ? static_cast<const int32_t *>(position->data_ptr()) : nullptr};
   }
@@ -401,7 +405,7 @@ PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (out && out->sizes() != q.sizes()) refuse("out", "the sizes of q are expected");
   const float scale = args[10] != Py_None ? number(args[10], "scale") : 1.f / std::sqrt((float)d.head_dim);
   const int32_t window = whole(args[11], "window"), sinks = whole(args[12], "sinks"), heads = narrow(q.size(1), "q");
-  const bool with_lse = args[14] == Py_True;
+  const bool with_lse = truth(args[14], "return_lse");
   void *wp = nullptr;
   size_t bytes = 0;
   at::TensorBase scratch, fresh, lse;

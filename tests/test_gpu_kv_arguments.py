@@ -1,0 +1,25 @@
+"""Arguments of kv_append() and attention() that say the same thing in different ways, or nothing."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _place(torch):
+    pages = [torch.zeros(s, dtype=torch.float16, device="cuda") for s in ((6, 2, 16, 64), (6, 2, 64, 16))]
+    table, lengths = torch.arange(6, dtype=torch.int32, device="cuda").reshape(2, 3), torch.tensor([20, 40], dtype=torch.int32, device="cuda")
+    return pages + [table, lengths], lambda heads: torch.ones((4, heads, 64), dtype=torch.float16, device="cuda")
+
+
+@pytest.mark.parametrize("truth", [True, 1, np.True_, "yes", False, 0, np.False_, None])
+def test_any_truth_value_asks_for_the_sums(gpu_lib, truth):
+    import torch
+    place, new = _place(torch)
+    got = gpu_lib.attention(new(4), *place, return_lse=truth)
+    if truth:
+        out, lse = got
+        assert out.shape == (4, 4, 64) and lse.shape == (4, 4)
+    else:
+        assert got.shape == (4, 4, 64)
+    with pytest.raises(ValueError):
+        gpu_lib.attention(new(4), *place, return_lse=torch.zeros(2, device="cuda"))
