@@ -364,6 +364,7 @@ PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
   vq_rotary r{};
   const at::Tensor *cos = tensor(args[13], "cos", at::kFloat, 2, true), *sin = tensor(args[14], "sin", at::kFloat, 2, true);
   if (!cos != !sin) refuse("cos, sin", "both or none is expected");
+  if (!cos && args[15] != Py_None) refuse("position", "without cos and sin there is nothing to look up");
   if (cos) {
     if (cos->sizes() != sin->sizes() || !apart(*cos, 1, 1) || !apart(*sin, 1, 1) || leading(*cos) != leading(*sin)) refuse("cos, sin", "[positions][pairs] of the same layout is expected");
     const at::Tensor *position = tensor(args[15], "position", at::kInt, 1, true);

@@ -23,3 +23,17 @@ def test_any_truth_value_asks_for_the_sums(gpu_lib, truth):
         assert got.shape == (4, 4, 64)
     with pytest.raises(ValueError):
         gpu_lib.attention(new(4), *place, return_lse=torch.zeros(2, device="cuda"))
+
+
+def test_positions_without_tables_are_refused(gpu_lib):
+    """A caller who gives positions expects a rotation."""
+    import torch
+    place, new = _place(torch)
+    position = torch.zeros(4, dtype=torch.int32, device="cuda")
+    table = torch.ones((48, 32), device="cuda")
+    for bad in (position, position.long(), 3):
+        with pytest.raises(ValueError):
+            gpu_lib.kv_append(new(2), new(2), *place, position=bad)
+    gpu_lib.kv_append(new(2), new(2), *place, cos=table, sin=table, position=position)
+    torch.cuda.synchronize()
+    assert place[0].any()
