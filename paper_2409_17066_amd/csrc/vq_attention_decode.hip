@@ -29,6 +29,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
   constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
   // The next chunk is loaded ahead where there are registers for it beside those of the rows' differences, and its values where the keys leave them room.
   constexpr bool AHEAD = !MANY || D == 64 || (E4M3 && D <= 128), V_AHEAD = D == 64 || (D == 128 && (EXACT || E4M3));
+  static_assert(!AHEAD || V_AHEAD, "the next keys are loaded by page numbers that are asked for in front of them only where the values are");
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   // (tiles of the same keys a multiple of all key heads apart: on the same XCD where those are a multiple of eight)
@@ -124,14 +125,14 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
     if (E4M3) v_scale = v_there ? c.v_scales[(long long)page * c.kv_heads + kv_head] : 1.f;
   };
 
-  if (i < end) {
-    if (V_AHEAD || AHEAD) load_k(i);
-    if (V_AHEAD) load_v(i);
+  if (V_AHEAD && i < end) {
+    load_k(i);
+    load_v(i);
   }
   for (; i < end; i += stride) {
     const int j0 = span.chunk(i) * 64, next = i + stride;
     if (V_AHEAD && next < end) entries_of(next);
-    if (!V_AHEAD && !AHEAD) load_k(i);
+    if (!V_AHEAD) load_k(i);
     float4v sc[RT][4];
     bool odd = false;
     const float k_by = E4M3 ? fminf(k_scale, WIDEST) : 1.f;
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
       __builtin_amdgcn_wave_barrier();
     }
     if (next < end) {
-      if (!AHEAD && V_AHEAD) load_k(next);
+      if (V_AHEAD && !AHEAD) load_k(next);
       if (V_AHEAD) load_v(next);
     }
   }
