@@ -338,7 +338,7 @@ typedef struct vq_rotary {
  * new tokens in it, or the page's scale so far if that is larger and the page holds earlier tokens of the sequence, which are
  * otherwise re-encoded to S (exact but for codes that become subnormal).  A code is x / S rounded to nearest even; what is not
  * finite becomes NaN.  Codes of places behind the sequence's end are left alone.  Two sequences must not share a page that
- * either appends to.  Doing the same call again changes nothing.
+ * either appends to.  The same call again leaves the cache as it is; queries that are rotated in place (q_out == q) it would turn once more.
  * k, v, q and q_out are 2-byte aligned, cos and sin 4-byte; q_out must not overlap anything else that is read.        */
 int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void *v, int64_t ldv, const void *q, int64_t ldq,
                  int32_t q_heads, void *q_out, int64_t ldq_out, const vq_rotary *rotary, void *hip_stream);

@@ -37,3 +37,23 @@ def test_positions_without_tables_are_refused(gpu_lib):
     gpu_lib.kv_append(new(2), new(2), *place, cos=table, sin=table, position=position)
     torch.cuda.synchronize()
     assert place[0].any()
+
+
+def test_a_call_that_is_repeated_with_queries_in_place(gpu_lib):
+    """The cache stays as it is; queries are rotated by every call, so that a repeated one needs them as they were."""
+    import torch
+    place, _ = _place(torch)
+    rng = torch.Generator(device="cuda").manual_seed(3)
+    k, v, q = (torch.randn((4, n, 64), generator=rng, device="cuda").half() for n in (2, 2, 4))
+    angle = torch.arange(48, device="cuda")[:, None] * 0.1 * torch.ones(32, device="cuda")
+    tables = dict(cos=angle.cos(), sin=angle.sin())
+    want = gpu_lib.kv_append(k, v, *place, q=q, **tables)
+    pages = [p.clone() for p in place[:2]]
+    mine = q.clone()
+    assert gpu_lib.kv_append(k, v, *place, q=mine, q_out=mine, **tables) is mine
+    assert torch.equal(mine, want) and all(torch.equal(a, b) for a, b in zip(pages, place))
+    gpu_lib.kv_append(k, v, *place, q=mine, q_out=mine, **tables)
+    assert not torch.equal(mine, want) and all(torch.equal(a, b) for a, b in zip(pages, place))
+    mine.copy_(q)
+    gpu_lib.kv_append(k, v, *place, q=mine, q_out=mine, **tables)
+    assert torch.equal(mine, want) and all(torch.equal(a, b) for a, b in zip(pages, place))
