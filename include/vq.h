@@ -350,8 +350,9 @@ int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void
  * nothing gets zeros.  lse (may be NULL): binary32 [n_tokens][q_heads], the logarithm of the sum of exp(score), -inf for such tokens.
  * Scores, statistics and sums are binary32; the probabilities (relative to a base at least 2^7 below the largest so far) are rounded to binary16 for the matrix
  * cores, the result once.
- * Keys and values nobody sees may hold anything, NaN included.  8-bit values of more than 65504 (65504 itself is stored as
- * the code of 65536) count as 65504 or 65536, of their sign.  softmax_scale must be finite and positive.
+ * Keys and values nobody sees may hold anything, NaN included.  Codes are widened to binary16: values of more than 65504 (which is stored as the
+ * code of 65536) count as 65504 or 65536, of their sign; keys may be of any size.  softmax_scale must be finite and positive.
+ * max_new times the square of q_heads / kv_heads must be below 2^30.
  * Workspace (device memory, 256-byte aligned, contents undefined afterwards): with vq_attention_workspace_bytes bytes a
  * sequence's keys are cut into parts where that is faster (judged by the descriptor's sizes alone), and a second kernel joins them;
  * with less or NULL each sequence's keys are taken in one part.  Results are deterministic run to run for the same sizes and workspace.  */

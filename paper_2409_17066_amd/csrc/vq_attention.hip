@@ -15,14 +15,15 @@ struct Plan {
 };
 
 // The kernel and number of parts whose time is estimated the least, in us, from measurements on heads of 64 and 128 elements, 8 and 16 bits, 8 and 32 key heads,
-// 1 to 200 sequences of 15 to 32768 tokens with 1 to 4144 rows a key head (heads of other sizes count as the next multiple of 64, as the kernels take them):
+// 1 to 200 sequences of 15 to 32768 tokens with 1 to 4144 rows a key head (heads of other sizes count as the next multiple of 64, as the kernels take them; every sequence as the longest):
 //   decode: a workgroup of eight waves to a compute unit (more of smaller ones), rounds of 3.2 us for eight chunks of 16 KB behind 9 us;
 //   prompt: one workgroup to a compute unit takes 1.3 us a chunk for up to 32 rows and 0.1 more for each further 32 of 128, two 1.3 and 0.6, behind 12 us and 5
 //   for every further round of workgroups;
 // and for parts the second launch that joins them, 5 us, 0.3 ns a row and what it moves.  Measured (64 query and 8 key heads of 128 elements, 8 bits, us by the
-// decode and by the prompt kernel): 16 sequences of 4096 tokens 32 and 38 for 32 rows a key head, 59 and 49 for 64, 218 and 99 for 256; one of 1024 tokens 13 and
-// 16 for 32 rows, 13 and 19 for 256; 64 of 100 tokens, 32 heads, one row 14 and 38.  Parts (16 rows): 4 sequences of 2048 tokens 17 in one and 14 in four, one of 1024 13
-// in one and 14 in two; 518 tokens behind 1909 (prompt kernel) 73 in one and 108 in two.
+// decode and by the prompt kernel): 16 sequences of 4096 tokens 32 and 39 for 32 rows a key head, 59 and 50 for 64, 217 and 102 for 256; one of 1024 tokens 11 and
+// 13 for 32 rows, 12 and 19 for 256; 64 of 100 tokens, 32 key heads, one row 15 and 39.  Parts (16 rows): 4 sequences of 2048 tokens 18 in one and 12 in four, one of 1024 11
+// in one and in two; heads of 64 elements, 518 tokens behind 1909 (prompt kernel) 58 in one and 95 in two.  Of 115 layouts by both kernels in 1 to 32 parts (profiles/attention_plan.txt) what is
+// chosen takes up to 10 % longer than the least in 100, and up to 29 % in the others.
 Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
   Plan best{};
   const long long rows = (long long)c.max_new * a.group, slots = cu_count();

@@ -8,10 +8,10 @@
 // operand A of O^T = V^T P^T.  Likewise the elements of a head are dealt to the lanes sixteen bytes at a time, in the queries as in the keys.  So there
 // are no shuffles but for the maximum over four lane groups, and the running maximum of a row scales registers of the same lane.
 //
-// Measured, 64 query and 8 key heads of 128 elements, 8 bits: one sequence of 131071 tokens 49 us, 5.5 TB/s (a large copy reaches 4.9, reads alone 4.1 by a plain
-// kernel), and 4.6 for the second launch that joins its 32 parts; sixteen sequences of up to 4096 22 and 4, 4.1 TB/s: start-up and the last chunks of the longest.  32
-// heads, one sequence of 509 tokens: 7.1, launch and the chain from page table to keys to the join of the waves.  Heads of other sizes (16 sequences of
-// 4096 tokens): 80 elements 24, 256 63, whose keys and values are not in registers together.
+// Measured, 64 query and 8 key heads of 128 elements, 8 bits: one sequence of 131071 tokens 49 us, 5.5 TB/s (a large copy reaches 4.9 of reads and writes), and 4.6 for the second
+// launch that joins its 32 parts; sixteen sequences of up to 4096 21.6 and 3.9, 4.2 TB/s: start-up and the last chunks of the longest.  32
+// heads, one sequence of 509 tokens: 7.2, launch and the chain from page table to keys to the join of the waves.  Heads of other sizes (16 sequences of
+// 4096 tokens): 80 elements 22, 256 63, whose keys and values are not in registers together.
 #include "vq_attention.hpp"
 
 namespace vq {

@@ -6,8 +6,8 @@
 // one exchange between two lanes, and the running maximum scales registers of the same lane.  Rows of a key tile are stored in an order that makes a lane's scores those of
 // sixteen consecutive keys, eight of which are what the lane has to give as operand B of O^T = V^T P^T: the probabilities never leave their registers.
 //
-// Measured, 8 bits, heads of 128 elements: chunks of 1024 tokens behind up to 15360, 64 query and 8 key heads, 940 TFLOP/s, where a large product of
-// matrices reaches 1100; a prompt of 2048 tokens, 32 heads, 56 us (613 TFLOP/s: one round of workgroups, whose last chunks run alone).  Matrix cores, vector ALUs and
+// Measured, 8 bits, heads of 128 elements: chunks of 1024 tokens behind up to 15360, 64 query and 8 key heads, 1.12 to 1.16 ms, 900 to 935 TFLOP/s, where a large product of
+// matrices reaches 1100; a prompt of 2048 tokens, 32 heads, 57 us (604 TFLOP/s: one round of workgroups, whose last chunks run alone), of 64 elements 42.  Matrix cores, vector ALUs and
 // LDS are each busy 40 % of the clocks of long contexts; fewer vector operations (scale in a vector register, four maxima side by side) and two chains of
 // products in place of one changed nothing: what is left is LDS (without its traffic 36 % less) and the power limit.
 #include "vq_attention.hpp"
