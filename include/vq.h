@@ -360,6 +360,30 @@ size_t vq_attention_workspace_bytes(const vq_kv_desc *cache, int32_t q_heads, in
 int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, int32_t window, int32_t sinks,
                  void *out, int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Attention behind shared prefixes.  Many sequences of a batch begin with the same tokens (a system prompt, a document) and list the same pages for them: their new
+ * tokens' attention to those is computed for all of a prefix's sequences at once, so that its keys and values are read once, and joined with each sequence's own.
+ * Prefix g is the first lengths[g] tokens (device memory) of sequences members[g] .. members[g + 1] - 1 and lies in the pages of row g of this page_table.  Sequences in front of
+ * members[0] or from members[n_prefixes] on have none.  The cache's own page_table lists every sequence's pages from its first token on, the prefix's among them, as for
+ * vq_attention (which gives the same results, up to roundings): a sequence is read through it where its first new token stands in front of the prefix's
+ * end, where it is one too many for max_members, and as a whole where the library judges that to be faster.  A length beyond max_length counts as max_length (what is behind
+ * it is each sequence's own).  */
+typedef struct vq_prefix_desc {
+  uint32_t struct_size;                    /* = sizeof(vq_prefix_desc)                                     */
+  int32_t n_prefixes;                      /* 1 .. 65535                                                   */
+  int32_t max_members, max_length;         /* sequences and tokens of one prefix, at most; max_length <= table_pages * page_tokens and 2^30 */
+  int32_t max_own;                         /* of a sequence's tokens behind its prefix, about (for the choice of kernels: more are looked at all the same) */
+  int32_t table_pages;                     /* entries of a row of page_table                               */
+  const int32_t *page_table; int64_t table_stride;   /* [n_prefixes][table_stride]                         */
+  const int32_t *lengths;                  /* [n_prefixes]                                                 */
+  const int32_t *members;                  /* [n_prefixes + 1], ascending, or NULL: one prefix, of all sequences */
+} vq_prefix_desc;
+
+/* Arguments, masks and errors as for vq_attention, without a window.  Workspace: with vq_attention_shared_workspace_bytes bytes prefixes are computed once for their
+ * sequences; with less (or NULL) the call is vq_attention.  Up to three launches; results are deterministic run to run for the same sizes and workspace.          */
+size_t vq_attention_shared_workspace_bytes(const vq_kv_desc *cache, const vq_prefix_desc *prefix, int32_t q_heads);
+int vq_attention_shared(const vq_kv_desc *cache, const vq_prefix_desc *prefix, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, void *out, int64_t ldo,
+                        float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Residual sum and norms between two blocks, for every row r < rows of `width` elements:
  *     y = x + scale * gate * post(h)      post(h) = h * rsqrt(mean(h^2) + eps) * w_post, or h where w_post is NULL
  *     z = y * rsqrt(mean(y^2) + eps) * w_pre
@@ -370,6 +394,32 @@ int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq, int32_t q_
 int vq_residual_norm(const void *h, int64_t ldh, const void *x, int64_t ldx, const void *w_post, const void *gate, int64_t ldgate, float scale,
                      const void *w_pre, float eps, int32_t stream32, int32_t rows, int32_t width, void *y, int64_t ldy, void *z, int64_t ldz,
                      void *hip_stream);
+
+/* ---- in front of the first layer and behind the last --------------------------------------------------------------------
+ * Embedding lookup: y[r] = scale * table[ids[r]], r < rows.  table: fp16 [vocabulary][ld], y: fp16, or binary32 with stream32 != 0, [rows][ldy]; the product is binary32,
+ * rounded once.  A row whose id is outside [0, vocabulary) gets zeros (vq_sample's -1, a padded batch).  ids and y in 32 bits are 4-byte aligned, the rest to 2
+ * bytes; width and vocabulary up to 2^24.                                                                        */
+int vq_embed(const int32_t *ids, int32_t rows, const void *table, int64_t ld, int32_t vocabulary, int32_t width, float scale, int32_t stream32, void *y, int64_t ldy,
+             void *hip_stream);
+
+/* The next token of each row of logits, fp16 [rows][ld], vocabulary of them (up to 2^24), and a number 0 <= uniform[row] < 1 (others count as the nearest such one, NaN as 0).  A token weighs
+ * w = exp((logit - largest logit) / temperature).  In the order of their logits, the largest first and of equal ones the lowest token, (1) the first top_k are kept (0 or less:
+ * all), (2) of these, with top_p < 1, those in front of which less than top_p of what (1) keeps lies (one at least), (3) of these, with min_p > 0, those with w >= min_p (more than 1 counts as 1).
+ * The token is the first whose weight takes the sum, in that order, past uniform[row] times the sum of all that are kept.  A temperature that is not above 0 gives the
+ * first token of that order; infinite temperature, equal weights.  Logits of minus infinity and NaN are never drawn; a row that has no other ones gives token -1
+ * (and probability 0).  Infinite logits outweigh all finite ones.
+ * Weights and their sums are binary64: all of this is decided by the row's numbers, not by an order of additions.
+ * probabilities (may be NULL): binary32, the token's weight over the sum of those that are kept.  Arrays of the settings (device memory, [rows], may be NULL) take the place of the numbers.  */
+typedef struct vq_sampling {
+  uint32_t struct_size;                    /* = sizeof(vq_sampling)                                        */
+  int32_t top_k;
+  float temperature, top_p, min_p;
+  const float *temperatures;
+  const int32_t *top_ks;
+  const float *top_ps, *min_ps;
+} vq_sampling;
+int vq_sample(const void *logits, int64_t ld, int32_t rows, int32_t vocabulary, const float *uniform, const vq_sampling *how, int32_t *tokens, float *probabilities,
+              void *hip_stream);
 
 /* Text for a status code (static storage).  */
 const char *vq_status_string(int status);

@@ -50,6 +50,20 @@ class vq_rotary(ctypes.Structure):
                 ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("position", ctypes.c_void_p)]
 
 
+class vq_prefix_desc(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32), ("n_prefixes", ctypes.c_int32), ("max_members", ctypes.c_int32), ("max_length", ctypes.c_int32),
+        ("max_own", ctypes.c_int32), ("table_pages", ctypes.c_int32), ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("lengths", ctypes.c_void_p), ("members", ctypes.c_void_p),
+    ]
+
+
+class vq_sampling(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("top_k", ctypes.c_int32), ("temperature", ctypes.c_float), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("temperatures", ctypes.c_void_p), ("top_ks", ctypes.c_void_p), ("top_ps", ctypes.c_void_p),
+                ("min_ps", ctypes.c_void_p)]
+
+
 class VQError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -115,7 +129,16 @@ def load():
     L.vq_residual_norm.argtypes = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
                                    ctypes.c_float, ctypes.c_void_p, ctypes.c_float, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
                                    ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
-    for f in (L.vq_kv_append, L.vq_attention, L.vq_residual_norm):
+    X = ctypes.POINTER(vq_prefix_desc)
+    L.vq_attention_shared_workspace_bytes.argtypes = [K, X, ctypes.c_int32]
+    L.vq_attention_shared_workspace_bytes.restype = ctypes.c_size_t
+    L.vq_attention_shared.argtypes = [K, X, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                      ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    L.vq_embed.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_int32,
+                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
+    L.vq_sample.argtypes = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.POINTER(vq_sampling), ctypes.c_void_p,
+                            ctypes.c_void_p, ctypes.c_void_p]
+    for f in (L.vq_kv_append, L.vq_attention, L.vq_residual_norm, L.vq_attention_shared, L.vq_embed, L.vq_sample):
         f.restype = ctypes.c_int
     L.vq_status_string.argtypes = [ctypes.c_int]
     L.vq_status_string.restype = ctypes.c_char_p
@@ -127,7 +150,7 @@ def load():
 
 
 EXPORTED = ["vq_validate", "vq_dequant", "vq_gemv", "vq_gemv_workspace_bytes", "vq_gemv_with_workspace", "vq_gemv_static_workspace", "vq_gemv_multi", "vq_gemm", "vq_gemm_default", "vq_gemm_workspace_bytes", "vq_gemm_fast_workspace_bytes",
-            "vq_gemm_default_workspace_bytes", "vq_gemm_default", "vq_assign", "vq_assign_down", "vq_quantize_columns", "vq_quantize_columns_workspace_bytes", "vq_kv_append", "vq_attention_workspace_bytes", "vq_attention", "vq_residual_norm", "vq_status_string", "vq_version"]
+            "vq_gemm_default_workspace_bytes", "vq_gemm_default", "vq_assign", "vq_assign_down", "vq_quantize_columns", "vq_quantize_columns_workspace_bytes", "vq_kv_append", "vq_attention_workspace_bytes", "vq_attention", "vq_residual_norm", "vq_attention_shared_workspace_bytes", "vq_attention_shared", "vq_embed", "vq_sample", "vq_status_string", "vq_version"]
 
 
 # ---- the C entry points, same names, raw pointers (ints) and sizes ---------------------------------------
@@ -230,6 +253,23 @@ def vq_residual_norm(h_ptr, ldh, x_ptr, ldx, w_post_ptr, gate_ptr, ldgate, scale
                                    z_ptr, ldz, stream)
 
 
+def vq_attention_shared_workspace_bytes(cache, prefix, q_heads):
+    return load().vq_attention_shared_workspace_bytes(ctypes.byref(cache), ctypes.byref(prefix), q_heads)
+
+
+def vq_attention_shared(cache, prefix, q_ptr, ldq, q_heads, softmax_scale, out_ptr, ldo, lse_ptr=None, workspace_ptr=None, workspace_bytes=0, stream=None):
+    return load().vq_attention_shared(ctypes.byref(cache) if cache is not None else None, ctypes.byref(prefix) if prefix is not None else None, q_ptr, ldq, q_heads,
+                                      softmax_scale, out_ptr, ldo, lse_ptr, workspace_ptr, workspace_bytes, stream)
+
+
+def vq_embed(ids_ptr, rows, table_ptr, ld, vocabulary, width, scale, stream32, y_ptr, ldy, stream=None):
+    return load().vq_embed(ids_ptr, rows, table_ptr, ld, vocabulary, width, scale, stream32, y_ptr, ldy, stream)
+
+
+def vq_sample(logits_ptr, ld, rows, vocabulary, uniform_ptr, how, tokens_ptr, probabilities_ptr=None, stream=None):
+    return load().vq_sample(logits_ptr, ld, rows, vocabulary, uniform_ptr, ctypes.byref(how) if how is not None else None, tokens_ptr, probabilities_ptr, stream)
+
+
 def vq_status_string(status):
     return load().vq_status_string(status).decode()
 
@@ -252,7 +292,8 @@ def _native():
         b.bind({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value
                 for name in ("vq_gemv", "vq_gemv_with_workspace", "vq_gemv_multi", "vq_gemm", "vq_gemm_default", "vq_gemm_workspace_bytes",
                              "vq_gemm_default_workspace_bytes", "vq_lend_gemv_bytes", "vq_lend_gemm_least_bytes", "vq_dequant", "vq_lend_assign",
-                             "vq_kv_append", "vq_attention", "vq_attention_workspace_bytes", "vq_residual_norm")})
+                             "vq_kv_append", "vq_attention", "vq_attention_workspace_bytes", "vq_residual_norm",
+                             "vq_attention_shared", "vq_attention_shared_workspace_bytes", "vq_embed", "vq_sample")})
         _bound = b
     return _bound
 
@@ -511,4 +552,38 @@ def residual_norm(h, x, pre=None, post=None, gate=None, scale=1.0, eps=1e-5, y=N
     r = (_bound or _native()).residual_norm(h, x, pre, post, gate, scale, eps, y, z)
     if r.__class__ is int:
         raise VQError(r, "vq_residual_norm")
+    return r
+
+
+def attention_shared(q, k_pages, v_pages, page_table, lengths, prefix_table, prefix_lengths, k_scales=None, v_scales=None, members=None, starts=None, scale=None,
+                     max_new=None, max_length=None, max_prefix=None, max_members=None, max_own=None, out=None, return_lse=False, workspace=None):
+    """attention() of sequences that begin with the same tokens, whose attention to those is computed once for all.  prefix_table: int32 [prefixes][pages of one],
+    prefix_lengths: int32 [prefixes], members: int32 [prefixes + 1], the first sequence of each prefix and the end of the last (None: one prefix, of all
+    sequences); page_table and lengths: the whole sequences, prefixes included, as for attention().  max_prefix, max_members, max_own: bounds of a prefix's length
+    and number of sequences, and about how much a sequence holds behind it (None: the tables' size, all, max_length).  The rest as for attention(), without a window."""
+    r = (_bound or _native()).attention_shared(k_pages, v_pages, page_table, lengths, k_scales, v_scales, starts, max_new, max_length, prefix_table, prefix_lengths,
+                                               members, max_prefix, max_members, max_own, q, scale, out, return_lse, workspace)
+    if r.__class__ is int:
+        raise VQError(r, "vq_attention_shared")
+    return r
+
+
+# ---- in front of the first layer and behind the last --------------------------------------------------------------------
+
+def embed(ids, table, scale=1.0, dtype=None, out=None):
+    """scale * table[ids]: ids: int32 [tokens], table: fp16 [vocabulary][width] device tensors -> fp16 (dtype None) or fp32 [tokens][width]; an id outside of the
+    table gives a row of zeros."""
+    r = (_bound or _native()).embed(ids, table, scale, dtype, out)
+    if r.__class__ is int:
+        raise VQError(r, "vq_embed")
+    return r
+
+
+def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, return_prob=False):
+    """The next token of each row: logits: fp16 [rows][vocabulary], uniform: fp32 [rows] numbers in [0, 1) -> int32 [rows], -1 for a row without finite logits; with
+    return_prob also its probability among what is kept, fp32 [rows].  temperature (0: the largest logit), top_k (0: all), top_p (1: all), min_p (0: all): numbers,
+    or device tensors [rows] (fp32, top_k int32)."""
+    r = (_bound or _native()).sample(logits, uniform, temperature, top_k, top_p, min_p, out, return_prob)
+    if r.__class__ is int:
+        raise VQError(r, "vq_sample")
     return r

@@ -9,6 +9,7 @@
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
@@ -33,6 +34,10 @@ decltype(&vq_kv_append) p_kv_append;
 decltype(&vq_attention) p_attention;
 decltype(&vq_attention_workspace_bytes) p_attention_workspace_bytes;
 decltype(&vq_residual_norm) p_residual_norm;
+decltype(&vq_attention_shared) p_attention_shared;
+decltype(&vq_attention_shared_workspace_bytes) p_attention_shared_workspace_bytes;
+decltype(&vq_embed) p_embed;
+decltype(&vq_sample) p_sample;
 
 PyObject *s_desc, *s_places;
 
@@ -395,27 +400,24 @@ PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
   VQ_CATCH
 }
 
-// attention(k_pages, v_pages, page_table, lengths, k_scales, v_scales, starts, max_new, max_length, q, scale, window, sinks, out, return_lse, workspace)
-PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  VQ_TRY
-  if (n != 16) refuse("attention", "16 arguments are expected");
-  const at::Tensor &q = *tokens(args[9], "q"), *out = tokens(args[13], "out", true);
-  vq_kv_desc d;
-  cache_of(args, q.size(0), d);
+// What attention and attention_shared have in common: the call with its workspace (args: scale, out, return_lse, workspace).
+template <typename Size, typename Call>
+PyObject *attend(const vq_kv_desc &d, const at::Tensor &q, PyObject *scale_of, PyObject *out_of, PyObject *lse_of, PyObject *workspace_of, Size size, Call call) {
+  const at::Tensor *out = tokens(out_of, "out", true);
   if (q.size(2) != d.head_dim) refuse("q", "[tokens][query heads][head_dim] is expected");
   if (out && out->sizes() != q.sizes()) refuse("out", "the sizes of q are expected");
-  const float scale = args[10] != Py_None ? number(args[10], "scale") : 1.f / std::sqrt((float)d.head_dim);
-  const int32_t window = whole(args[11], "window"), sinks = whole(args[12], "sinks"), heads = narrow(q.size(1), "q");
-  const bool with_lse = truth(args[14], "return_lse");
+  const float scale = scale_of != Py_None ? number(scale_of, "scale") : 1.f / std::sqrt((float)d.head_dim);
+  const int32_t heads = narrow(q.size(1), "q");
+  const bool with_lse = truth(lse_of, "return_lse");
   void *wp = nullptr;
   size_t bytes = 0;
   at::TensorBase scratch, fresh, lse;
-  if (args[15] == Py_None) {
-    bytes = p_attention_workspace_bytes(&d, heads, window, sinks);
+  if (workspace_of == Py_None) {
+    bytes = size(heads);
     wp = bytes ? borrow(scratch, bytes) : nullptr;
     if (!wp) bytes = 0;
   } else {
-    const at::Tensor &ws = *tensor(args[15], "workspace", at::kByte, 1);
+    const at::Tensor &ws = *tensor(workspace_of, "workspace", at::kByte, 1);
     if (!ws.is_contiguous()) refuse("workspace", "adjacent bytes are expected");
     bytes = (size_t)ws.numel();
     wp = bytes ? ws.data_ptr() : nullptr;
@@ -426,11 +428,136 @@ PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
   const int64_t ldo = out ? leading(*out) : q.size(1) * q.size(2), ldq = leading(q);
   const void *qp = q.data_ptr();
   float *lp = with_lse ? static_cast<float *>(lse.data_ptr()) : nullptr;
-  const int rc = released([&] { return p_attention(&d, qp, ldq, heads, scale, window, sinks, op, ldo, lp, wp, bytes, s); });
+  const int rc = released([&] { return call(qp, ldq, heads, scale, op, ldo, lp, wp, bytes, s); });
   if (rc != VQ_OK) return PyLong_FromLong(rc);
-  PyObject *result = out ? (Py_INCREF(args[13]), args[13]) : THPVariable_Wrap(std::move(fresh));
+  PyObject *result = out ? (Py_INCREF(out_of), out_of) : THPVariable_Wrap(std::move(fresh));
   if (!with_lse || !result) return result;
   PyObject *second = THPVariable_Wrap(std::move(lse)), *both = second ? PyTuple_Pack(2, result, second) : nullptr;
+  Py_DECREF(result);
+  Py_XDECREF(second);
+  return both;
+}
+
+// attention(k_pages, v_pages, page_table, lengths, k_scales, v_scales, starts, max_new, max_length, q, scale, window, sinks, out, return_lse, workspace)
+PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  VQ_TRY
+  if (n != 16) refuse("attention", "16 arguments are expected");
+  const at::Tensor &q = *tokens(args[9], "q");
+  vq_kv_desc d;
+  cache_of(args, q.size(0), d);
+  const int32_t window = whole(args[11], "window"), sinks = whole(args[12], "sinks");
+  return attend(d, q, args[10], args[13], args[14], args[15], [&](int32_t heads) { return p_attention_workspace_bytes(&d, heads, window, sinks); },
+                [&](const void *qp, int64_t ldq, int32_t heads, float scale, void *op, int64_t ldo, float *lp, void *wp, size_t bytes, void *s) {
+                  return p_attention(&d, qp, ldq, heads, scale, window, sinks, op, ldo, lp, wp, bytes, s);
+                });
+  VQ_CATCH
+}
+
+// attention_shared(k_pages, v_pages, page_table, lengths, k_scales, v_scales, starts, max_new, max_length, prefix_table, prefix_lengths, members, max_prefix, max_members, max_own,
+// q, scale, out, return_lse, workspace)
+PyObject *attention_shared(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  VQ_TRY
+  if (n != 20) refuse("attention_shared", "20 arguments are expected");
+  const at::Tensor &q = *tokens(args[15], "q");
+  vq_kv_desc d;
+  cache_of(args, q.size(0), d);
+  const at::Tensor &table = *tensor(args[9], "prefix_table", at::kInt, 2), &lengths = *tensor(args[10], "prefix_lengths", at::kInt, 1), *members = tensor(args[11], "members", at::kInt, 1, true);
+  const int64_t prefixes = lengths.size(0);
+  if (table.size(0) != prefixes || !apart(table, 1, 1)) refuse("prefix_table", "[prefixes][pages] with adjacent entries is expected");
+  if (!apart(lengths, 0, 1)) refuse("prefix_lengths", "adjacent entries are expected");
+  if (members && (members->size(0) != prefixes + 1 || !apart(*members, 0, 1))) refuse("members", "one entry more than prefixes is expected");
+  if (!members && prefixes != 1) refuse("members", "several prefixes need them");
+  vq_prefix_desc x{};
+  x.struct_size = sizeof x;
+  x.n_prefixes = narrow(prefixes, "prefix_lengths");
+  x.table_pages = narrow(table.size(1), "prefix_table");
+  x.max_length = args[12] != Py_None ? whole(args[12], "max_prefix") : narrow(table.size(1) * d.page_tokens, "max_prefix");
+  x.max_members = args[13] != Py_None ? whole(args[13], "max_members") : d.n_seqs;
+  x.max_own = args[14] != Py_None ? whole(args[14], "max_own") : d.max_length;
+  x.page_table = static_cast<const int32_t *>(table.data_ptr());
+  x.table_stride = leading(table);
+  x.lengths = static_cast<const int32_t *>(lengths.data_ptr());
+  x.members = members ? static_cast<const int32_t *>(members->data_ptr()) : nullptr;
+  return attend(d, q, args[16], args[17], args[18], args[19], [&](int32_t heads) { return p_attention_shared_workspace_bytes(&d, &x, heads); },
+                [&](const void *qp, int64_t ldq, int32_t heads, float scale, void *op, int64_t ldo, float *lp, void *wp, size_t bytes, void *s) {
+                  return p_attention_shared(&d, &x, qp, ldq, heads, scale, op, ldo, lp, wp, bytes, s);
+                });
+  VQ_CATCH
+}
+
+// embed(ids, table, scale, dtype or None, out or None)
+PyObject *embed(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  VQ_TRY
+  if (n != 5) refuse("embed", "five arguments are expected");
+  const at::Tensor &ids = *tensor(args[0], "ids", at::kInt, 1), &table = *tensor(args[1], "table", at::kHalf, 2);
+  if (!apart(ids, 0, 1)) refuse("ids", "adjacent entries are expected");
+  if (!apart(table, 1, 1)) refuse("table", "adjacent elements are expected");
+  const float scale = number(args[2], "scale");
+  at::ScalarType type = at::kHalf;
+  const bool given = args[4] != Py_None;
+  if (given && THPVariable_Check(args[4])) type = THPVariable_Unpack(args[4]).scalar_type();
+  if (args[3] != Py_None) {
+    if (!THPDtype_Check(args[3])) refuse("dtype", "a torch.dtype is expected");
+    const at::ScalarType asked = reinterpret_cast<THPDtype *>(args[3])->scalar_type;
+    if (given && asked != type) refuse("out", "the type of dtype is expected");
+    type = asked;
+  }
+  if (type != at::kHalf && type != at::kFloat) refuse(given ? "out" : "dtype", "float16 or float32 is expected");
+  const at::Tensor *out = tensor(args[4], "out", type, 2, true);
+  const int64_t rows = ids.size(0), width = table.size(1);
+  if (out && (out->size(0) != rows || out->size(1) != width || !apart(*out, 1, 1))) refuse("out", "[tokens][width] with adjacent elements is expected");
+  at::TensorBase fresh;
+  if (!out) fresh = empty({rows, width}, type);
+  void *yp = out ? out->data_ptr() : fresh.data_ptr(), *s = stream();
+  const int32_t m = narrow(rows, "ids"), words = narrow(table.size(0), "table"), w = narrow(width, "table");
+  const int32_t *ip = static_cast<const int32_t *>(ids.data_ptr());
+  const void *tp = table.data_ptr();
+  const int64_t ld = leading(table), ldy = out ? leading(*out) : width;
+  const int rc = released([&] { return p_embed(ip, m, tp, ld, words, w, scale, type == at::kFloat, yp, ldy, s); });
+  return tensor_or_status(rc, std::move(fresh), args[4]);
+  VQ_CATCH
+}
+
+// sample(logits, uniform, temperature, top_k, top_p, min_p, out or None, return_prob)
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  VQ_TRY
+  if (n != 8) refuse("sample", "eight arguments are expected");
+  const at::Tensor &logits = *tensor(args[0], "logits", at::kHalf, 2), &uniform = *tensor(args[1], "uniform", at::kFloat, 1);
+  if (!apart(logits, 1, 1)) refuse("logits", "adjacent elements are expected");
+  const int64_t rows = logits.size(0);
+  auto of_rows = [&](const at::Tensor &t, const char *name) {
+    if (t.size(0) != rows || !apart(t, 0, 1)) refuse(name, "one entry for each row is expected");
+    return t.data_ptr();
+  };
+  const float *up = static_cast<const float *>(of_rows(uniform, "uniform"));
+  vq_sampling how{};
+  how.struct_size = sizeof how;
+  auto setting = [&](PyObject *o, const char *name, float &one, const float *&each) {
+    if (THPVariable_Check(o)) each = static_cast<const float *>(of_rows(*tensor(o, name, at::kFloat, 1), name));
+    else one = number(o, name);
+  };
+  setting(args[2], "temperature", how.temperature, how.temperatures);
+  if (THPVariable_Check(args[3])) how.top_ks = static_cast<const int32_t *>(of_rows(*tensor(args[3], "top_k", at::kInt, 1), "top_k"));
+  else how.top_k = whole(args[3], "top_k");
+  setting(args[4], "top_p", how.top_p, how.top_ps);
+  setting(args[5], "min_p", how.min_p, how.min_ps);
+  const at::Tensor *out = tensor(args[6], "out", at::kInt, 1, true);
+  if (out) of_rows(*out, "out");
+  const bool with_prob = truth(args[7], "return_prob");
+  at::TensorBase fresh, prob;
+  if (!out) fresh = empty({rows}, at::kInt);
+  if (with_prob) prob = empty({rows}, at::kFloat);
+  int32_t *tp = static_cast<int32_t *>(out ? out->data_ptr() : fresh.data_ptr());
+  float *pp = with_prob ? static_cast<float *>(prob.data_ptr()) : nullptr;
+  const void *lp = logits.data_ptr();
+  void *s = stream();
+  const int64_t ld = leading(logits);
+  const int32_t m = narrow(rows, "logits"), words = narrow(logits.size(1), "logits");
+  const int rc = released([&] { return p_sample(lp, ld, m, words, up, &how, tp, pp, s); });
+  if (rc != VQ_OK) return PyLong_FromLong(rc);
+  PyObject *result = out ? (Py_INCREF(args[6]), args[6]) : THPVariable_Wrap(std::move(fresh));
+  if (!with_prob || !result) return result;
+  PyObject *second = THPVariable_Wrap(std::move(prob)), *both = second ? PyTuple_Pack(2, result, second) : nullptr;
   Py_DECREF(result);
   Py_XDECREF(second);
   return both;
@@ -497,6 +624,9 @@ PyMethodDef methods[] = {{"gemv", (PyCFunction)(void *)gemv, METH_FASTCALL, null
                          {"kv_append", (PyCFunction)(void *)kv_append, METH_FASTCALL, nullptr},
                          {"attention", (PyCFunction)(void *)attention, METH_FASTCALL, nullptr},
                          {"residual_norm", (PyCFunction)(void *)residual_norm, METH_FASTCALL, nullptr},
+                         {"attention_shared", (PyCFunction)(void *)attention_shared, METH_FASTCALL, nullptr},
+                         {"embed", (PyCFunction)(void *)embed, METH_FASTCALL, nullptr},
+                         {"sample", (PyCFunction)(void *)sample, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 // bind(addresses): the library's entry points, which the package has loaded
@@ -511,7 +641,8 @@ PyObject *bind(PyObject *, PyObject *addresses) {
       !at("vq_gemm_workspace_bytes", p_gemm_workspace_bytes) || !at("vq_lend_gemv_bytes", p_lend_gemv_bytes) || !at("vq_gemm_default_workspace_bytes", p_gemm_default_workspace_bytes) ||
       !at("vq_lend_gemm_least_bytes", p_lend_gemm_least_bytes) ||
        !at("vq_dequant", p_dequant) || !at("vq_lend_assign", p_lend_assign) || !at("vq_kv_append", p_kv_append) || !at("vq_attention", p_attention) ||
-       !at("vq_attention_workspace_bytes", p_attention_workspace_bytes) || !at("vq_residual_norm", p_residual_norm)) {
+       !at("vq_attention_workspace_bytes", p_attention_workspace_bytes) || !at("vq_residual_norm", p_residual_norm) ||
+       !at("vq_attention_shared", p_attention_shared) || !at("vq_attention_shared_workspace_bytes", p_attention_shared_workspace_bytes) || !at("vq_embed", p_embed) || !at("vq_sample", p_sample)) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point is missing");
     return nullptr;
   }

@@ -2,6 +2,8 @@
 #include "vq_common.hpp"
 #include "vq_kv.hpp"
 #include "vq_lend.h"
+#include <algorithm>
+#include <cfloat>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
@@ -40,6 +42,7 @@ void read_switches() {
       else if (n == 4 && !strncmp(e, "rows", 4)) sw.rows = v == '0' ? 0 : v == '1' ? 1 : -1;
       else if (n == 8 && !strncmp(e, "products", 8)) sw.products = v == '0' ? 0 : v == '1' ? 1 : -1;
       else if (n == 9 && !strncmp(e, "attention", 9)) sw.attention = v;
+      else if (n == 6 && !strncmp(e, "shared", 6)) sw.shared = v == '0' || v == '1' ? v : 0;
       else if (n == 5 && !strncmp(e, "parts", 5)) sw.parts = v >= '0' && v <= '6' ? v - '0' : -1;
       else if (n == 5 && !strncmp(e, "dense", 5)) sw.dense = v >= '0' && v <= '9' ? v - '0' : -1;
     }
@@ -414,6 +417,23 @@ static int make_attention_params(const KvParams &c, int32_t q_heads, int32_t win
   return VQ_OK;
 }
 
+// The prefixes of a call; what they bound is cut to what the call can have.
+static int make_prefixes(const vq_prefix_desc *d, const KvParams &c, Prefixes *x) {
+  if (!d) return VQ_ERR_NULL;
+  if (d->struct_size != sizeof(vq_prefix_desc) || d->n_prefixes < 1 || d->n_prefixes > 65535 || d->max_members < 1 || d->max_length < 0 || d->max_length > 1 << 30 || d->max_own < 0)
+    return VQ_ERR_SHAPE;
+  if (d->table_pages < 0 || d->max_length > ((long long)d->table_pages << c.page_shift) || d->table_stride < d->table_pages) return VQ_ERR_SHAPE;
+  if (!d->members && d->n_prefixes != 1) return VQ_ERR_SHAPE;
+  if (!d->lengths || (!d->page_table && d->table_pages)) return VQ_ERR_NULL;
+  if (!aligned(d->lengths, 4) || !aligned(d->page_table, 4) || !aligned(d->members, 4)) return VQ_ERR_ALIGNMENT;
+  *x = Prefixes{};
+  x->n = d->n_prefixes; x->most = std::min(d->max_members, c.n_seqs); x->max_length = d->max_length; x->max_own = std::min(d->max_own, c.max_length);
+  x->n_seqs = c.n_seqs; x->table_pages = d->table_pages; x->table_stride = d->table_stride;
+  x->rows_most = (int)std::min<long long>((long long)x->most * c.max_new, c.n_tokens);
+  x->page_table = d->page_table; x->lengths = d->lengths; x->members = d->members;
+  return VQ_OK;
+}
+
 }  // namespace vq
 
 extern "C" int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk, const void *v, int64_t ldv, const void *q, int64_t ldq,
@@ -438,6 +458,21 @@ extern "C" int vq_kv_append(const vq_kv_desc *cache, const void *k, int64_t ldk,
                               q ? q_heads : 0, static_cast<__half *>(q_out), ldq_out, r, static_cast<hipStream_t>(hip_stream));
 }
 
+static int checked_attention(const vq::KvParams &c, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, int32_t window, int32_t sinks, void *out, int64_t ldo,
+                             float *lse, void *workspace, vq::AttentionParams *a) {
+  if (!q || !out) return VQ_ERR_NULL;
+  const int rc = vq::make_attention_params(c, q_heads, window, sinks, a);
+  if (rc != VQ_OK) return rc;
+  const long long width = (long long)q_heads * c.head_dim;
+  if (ldq < width || ldo < width || !(softmax_scale > 0.f && softmax_scale <= 1e30f)) return VQ_ERR_SHAPE;
+  if (!aligned(q, 2) || !aligned(out, 2) || !aligned(lse, 4) || !aligned(workspace, 256)) return VQ_ERR_ALIGNMENT;
+  a->q = static_cast<const __half *>(q); a->ldq = ldq;
+  a->out = static_cast<__half *>(out); a->ldo = ldo;
+  a->lse = lse;
+  a->scale = softmax_scale * 1.4426950408889634f;
+  return VQ_OK;
+}
+
 extern "C" size_t vq_attention_workspace_bytes(const vq_kv_desc *cache, int32_t q_heads, int32_t window, int32_t sinks) {
   vq::read_switches();
   vq::KvParams c;
@@ -453,16 +488,50 @@ extern "C" int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq,
   vq::AttentionParams a;
   int rc = vq::make_kv_params(cache, &c);
   if (rc != VQ_OK) return rc;
-  if (!q || !out) return VQ_ERR_NULL;
-  if ((rc = vq::make_attention_params(c, q_heads, window, sinks, &a)) != VQ_OK) return rc;
-  const long long width = (long long)q_heads * c.head_dim;
-  if (ldq < width || ldo < width || !(softmax_scale > 0.f && softmax_scale <= 1e30f)) return VQ_ERR_SHAPE;
-  if (!aligned(q, 2) || !aligned(out, 2) || !aligned(lse, 4) || !aligned(workspace, 256)) return VQ_ERR_ALIGNMENT;
-  a.q = static_cast<const __half *>(q); a.ldq = ldq;
-  a.out = static_cast<__half *>(out); a.ldo = ldo;
-  a.lse = lse;
-  a.scale = softmax_scale * 1.4426950408889634f;
+  if ((rc = checked_attention(c, q, ldq, q_heads, softmax_scale, window, sinks, out, ldo, lse, workspace, &a)) != VQ_OK) return rc;
   return vq::launch_attention(c, a, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" size_t vq_attention_shared_workspace_bytes(const vq_kv_desc *cache, const vq_prefix_desc *prefix, int32_t q_heads) {
+  vq::read_switches();
+  vq::KvParams c;
+  vq::Prefixes x;
+  vq::AttentionParams a;
+  if (vq::make_kv_params(cache, &c) != VQ_OK || vq::make_prefixes(prefix, c, &x) != VQ_OK || vq::make_attention_params(c, q_heads, 0, 0, &a) != VQ_OK) return 0;
+  return vq::attention_shared_workspace_bytes(c, x, a);
+}
+
+extern "C" int vq_attention_shared(const vq_kv_desc *cache, const vq_prefix_desc *prefix, const void *q, int64_t ldq, int32_t q_heads, float softmax_scale, void *out,
+                                   int64_t ldo, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  vq::read_switches();
+  vq::KvParams c;
+  vq::Prefixes x;
+  vq::AttentionParams a;
+  int rc = vq::make_kv_params(cache, &c);
+  if (rc != VQ_OK || (rc = vq::make_prefixes(prefix, c, &x)) != VQ_OK) return rc;
+  if ((rc = checked_attention(c, q, ldq, q_heads, softmax_scale, 0, 0, out, ldo, lse, workspace, &a)) != VQ_OK) return rc;
+  return vq::launch_attention_shared(c, x, a, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int vq_embed(const int32_t *ids, int32_t rows, const void *table, int64_t ld, int32_t vocabulary, int32_t width, float scale, int32_t stream32, void *y,
+                        int64_t ldy, void *hip_stream) {
+  if (!ids || !table || !y) return VQ_ERR_NULL;
+  const int lim = 1 << 24;
+  if (rows < 1 || vocabulary < 1 || vocabulary > lim || width < 1 || width > lim || ld < width || ldy < width || !(scale >= -FLT_MAX && scale <= FLT_MAX)) return VQ_ERR_SHAPE;
+  if (!aligned(ids, 4) || !aligned(table, 2) || !aligned(y, stream32 ? 4 : 2)) return VQ_ERR_ALIGNMENT;
+  return vq::launch_embed(ids, rows, static_cast<const __half *>(table), ld, vocabulary, width, scale, stream32 != 0, y, ldy, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int vq_sample(const void *logits, int64_t ld, int32_t rows, int32_t vocabulary, const float *uniform, const vq_sampling *how, int32_t *tokens, float *probabilities,
+                         void *hip_stream) {
+  if (!logits || !uniform || !how || !tokens) return VQ_ERR_NULL;
+  if (how->struct_size != sizeof(vq_sampling) || rows < 1 || vocabulary < 1 || vocabulary > 1 << 24 || ld < vocabulary) return VQ_ERR_SHAPE;
+  if (!aligned(logits, 2) || !aligned(uniform, 4) || !aligned(tokens, 4) || !aligned(probabilities, 4) || !aligned(how->temperatures, 4) || !aligned(how->top_ks, 4) ||
+      !aligned(how->top_ps, 4) || !aligned(how->min_ps, 4))
+    return VQ_ERR_ALIGNMENT;
+  const vq::SampleParams p{static_cast<const __half *>(logits), ld, vocabulary, how->top_k, how->temperature, how->top_p, how->min_p, uniform, how->temperatures, how->top_ps,
+                           how->min_ps, how->top_ks, tokens, probabilities};
+  return vq::launch_sample(p, rows, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int vq_residual_norm(const void *h, int64_t ldh, const void *x, int64_t ldx, const void *w_post, const void *gate, int64_t ldgate,

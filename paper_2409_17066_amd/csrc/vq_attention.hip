@@ -12,6 +12,7 @@ struct Plan {
   int tile_rows, parts, run;
   bool prompt;
   size_t o_bytes, ml_bytes;
+  float time;                    // estimated, us
 };
 
 // The kernel and number of parts whose time is estimated the least, in us, from measurements on heads of 64 and 128 elements, 8 and 16 bits, 8 and 32 key heads,
@@ -24,7 +25,8 @@ struct Plan {
 // 13 for 32 rows, 12 and 19 for 256; 64 of 100 tokens, 32 key heads, one row 15 and 39.  Parts (16 rows): 4 sequences of 2048 tokens 18 in one and 12 in four, one of 1024 11
 // in one and in two; heads of 64 elements, 518 tokens behind 1909 (prompt kernel) 58 in one and 95 in two.  Of 115 layouts by both kernels in 1 to 32 parts (profiles/attention_plan.txt) what is
 // chosen takes up to 10 % longer than the least in 100, and up to 29 % in the others.
-Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
+// A prefix is a sequence all of whose rows see all of it; of what lies behind there are `length` keys at most.  Both always leave parts for another launch, which is not counted here.
+Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Half half, long long length) {
   Plan best{};
   const long long rows = (long long)c.max_new * a.group, slots = cu_count();
   float least = 0.f;
@@ -32,21 +34,21 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
   for (const bool prompt : {false, true}) {
     const char forced = attention_prompt_takes(c) ? switches().attention : 'd';
     if (forced == 'd' || forced == 'p' ? prompt != (forced == 'p') : !prompt && rows > 512) continue;
-    const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(c, a), run = prompt ? PROMPT_RUN : attention_decode_run(c);
+    const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(c, a, half == PREFIX || c.max_new == 1), run = prompt ? PROMPT_RUN : attention_decode_run(c);
     // tokens that a tile's rows look at: a window's and the first ones, or on the average all before half of the new ones
-    const long long all = c.max_length - (rows > tile ? c.max_new / 2 : 0), reach = a.window > 0 ? (long long)a.window + a.sinks + tile / a.group + 64 : all;
+    const long long all = length - (rows > tile && half != PREFIX ? c.max_new / 2 : 0), reach = a.window > 0 ? (long long)a.window + a.sinks + tile / a.group + 64 : all;
     const long long chunks = (std::max(std::min(all, reach), 1LL) + 63) / 64, groups = (long long)c.n_seqs * c.kv_heads * ((rows + tile - 1) / tile);
     const float quarters = (float)std::min((rows + 31) / 32, 4LL), size = (float)((c.head_dim + 63) / 64) / 2.f;
-    const long long most = parts_allowed ? std::min((chunks + run - 1) / run, 64LL) : 1;
+    const long long most = parts_allowed ? std::min((chunks + run - 1) / run, half == WHOLE ? 64LL : (long long)HALF_PARTS) : 1;
     for (long long parts = 1;; parts *= 2) {
       if (switches().parts >= 0) parts = 1LL << switches().parts;
       parts = std::min(parts, most);
-      const float alone = (float)slots * (prompt ? 1.f : (float)run / (float)std::min(attention_decode_waves(c, (int)parts), run));   // workgroups side by side
+      const float alone = (float)slots * (prompt ? 1.f : (float)run / (float)std::min(attention_decode_waves(c, (int)parts, (int)length), run));   // workgroups side by side
       const float most_at_once = prompt ? 2.f * alone : alone, work = (float)(groups * parts), rounds = prompt ? std::max(work / most_at_once, 1.f) : std::ceil(work / most_at_once);
       const float turns = parts > 1 ? (float)(((chunks + run - 1) / run + parts - 1) / parts) : prompt ? (float)chunks / (float)run : (float)((chunks + run - 1) / run);
       const float one = 1.2f + 0.1f * quarters, two = 0.7f + 0.6f * quarters, shared = std::min(std::max(work / alone - 1.f, 0.f), 1.f);
       const float step = !prompt ? 3.2f * size * (c.e4m3 ? 1.f : 2.f) : run * size * (one + (two - one) * shared);
-      const float join = parts > 1 ? 5.f + (float)((long long)c.n_seqs * c.kv_heads * rows) * (0.3e-3f + (float)parts * size * 1024.f / 4.5e6f) : 0.f;
+      const float join = parts > 1 ? (half == WHOLE ? 5.f : 0.f) + (float)((long long)c.n_seqs * c.kv_heads * rows) * (0.3e-3f + (float)parts * size * 1024.f / 4.5e6f) : 0.f;
       const float time = (prompt ? 12.f + 5.f * size * (rounds - 1.f) : 9.f) + join + rounds * turns * step;
       if (least == 0.f || time < least) {
         least = time;
@@ -54,18 +56,68 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) {
         best.parts = (int)parts;
         best.run = run;
         best.prompt = prompt;
+        best.time = time;
       }
       if (parts == most || switches().parts >= 0) break;
     }
   }
-  if (best.parts > 1) {
+  if (best.parts > 1 || half != WHOLE) {
     best.o_bytes = (size_t)c.n_seqs * c.kv_heads * best.parts * rows * c.head_dim * 4;
     best.ml_bytes = (size_t)c.n_seqs * c.kv_heads * best.parts * rows * 8;
   }
   return best;
 }
 
+Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) { return plan_of(c, a, parts_allowed, WHOLE, c.max_length); }
+
+// Attention behind shared prefixes: a launch for the prefixes, one for what lies behind, one that joins them.
+struct SharedPlan {
+  KvParams prefixes;             // as sequences
+  Plan prefix, own;
+  bool shares;                   // or every sequence by itself, where that is estimated to be faster
+  static size_t bytes(const Plan &half) { return (half.o_bytes + half.ml_bytes + 255) / 256 * 256; }
+  size_t bytes() const { return bytes(prefix) + bytes(own); }
+};
+SharedPlan shared_plan_of(const KvParams &c, const Prefixes &x, const AttentionParams &a) {
+  SharedPlan p{};
+  p.prefixes = c;
+  p.prefixes.n_seqs = x.n;
+  p.prefixes.max_new = x.rows_most;
+  p.prefixes.max_length = x.max_length;
+  p.prefixes.table_pages = x.table_pages;
+  p.prefixes.table_stride = x.table_stride;
+  p.prefixes.page_table = x.page_table;
+  p.prefixes.lengths = x.lengths;
+  // (rows of a prefix: token_of()'s division and a grid's layers)
+  if (!attention_join_takes(c, a) || x.max_length == 0 || (long long)x.rows_most * a.group * a.group >= 1ll << 30) return p;
+  p.prefix = plan_of(p.prefixes, a, true, PREFIX, x.max_length);
+  p.own = plan_of(c, a, true, OWN, std::min(x.max_own, c.max_length));
+  const char forced = switches().shared;
+  p.shares = forced ? forced == '1' : p.prefix.time + p.own.time + 5.f < plan_of(c, a, true).time;
+  return p;
+}
+
 }  // namespace
+
+size_t attention_shared_workspace_bytes(const KvParams &c, const Prefixes &x, const AttentionParams &a) {
+  const SharedPlan p = shared_plan_of(c, x, a);
+  return p.shares ? p.bytes() : attention_workspace_bytes(c, a);
+}
+
+int launch_attention_shared(const KvParams &c, const Prefixes &x, const AttentionParams &a, void *workspace, size_t workspace_bytes, hipStream_t s) {
+  const SharedPlan p = shared_plan_of(c, x, a);
+  if (!p.shares || workspace_bytes < p.bytes()) return launch_attention(c, a, workspace, workspace_bytes, s);
+  float *at = static_cast<float *>(workspace);
+  auto split_of = [&](const Plan &half) {
+    const Split split{half.parts, half.run, at, at + half.o_bytes / 4};
+    at += SharedPlan::bytes(half) / 4;
+    return split;
+  };
+  const Split prefix = split_of(p.prefix), own = split_of(p.own);
+  int rc = p.prefix.prompt ? launch_attention_prompt(p.prefixes, a, prefix, x, PREFIX, s) : launch_attention_decode(p.prefixes, a, prefix, x, PREFIX, s);
+  if (rc == VQ_OK) rc = p.own.prompt ? launch_attention_prompt(c, a, own, x, OWN, s) : launch_attention_decode(c, a, own, x, OWN, s);
+  return rc != VQ_OK ? rc : launch_attention_join_halves(c, a, own, p.own.tile_rows, p.prefixes, prefix, p.prefix.tile_rows, x, s);
+}
 
 size_t attention_workspace_bytes(const KvParams &c, const AttentionParams &a) {
   const Plan p = plan_of(c, a, true);

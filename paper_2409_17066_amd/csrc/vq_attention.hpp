@@ -1,8 +1,21 @@
 // What the attention kernels share: which keys a tile of rows looks at, and how partial results are passed on (internal).
 #pragma once
 #include "vq_kv.hpp"
+#include <type_traits>
 
 namespace vq {
+
+// What a kernel's sequences are.  WHOLE: those of the call.  PREFIX: the prefixes, whose rows are the new tokens of all of a prefix's sequences and see all of
+// it.  OWN: those of the call, of which what lies behind the prefix is looked at.
+enum Half { WHOLE, PREFIX, OWN };
+struct NoPrefixes {};
+template <Half HALF>
+using PrefixesOf = std::conditional_t<HALF == WHOLE, NoPrefixes, Prefixes>;
+template <Half HALF>
+PrefixesOf<HALF> prefixes_of(const Prefixes &x) {
+  if constexpr (HALF == WHOLE) return NoPrefixes{};
+  else return x;
+}
 
 // How a sequence's keys are cut into parts: part p takes every `parts`-th run of `run` chunks of 64 keys (a power of two) from run p on, so that what a workgroup
 // looks at first does not depend on the sequence's length.
@@ -14,14 +27,21 @@ struct Split {
 // Chunks of a run, one for each wave of the decode kernel.
 constexpr int DECODE_RUN = 8, PROMPT_RUN = 4;
 int attention_decode_run(const KvParams &c);                       // DECODE_RUN, or half of it
-int attention_decode_waves(const KvParams &c, int parts);          // waves of a workgroup of the decode kernel
-// The decode kernel, which takes every head: rows of a key head to a workgroup.
-int attention_decode_rows(const KvParams &c, const AttentionParams &a);
+int attention_decode_waves(const KvParams &c, int parts, int length);          // waves of a workgroup of the decode kernel, for sequences of up to `length` keys
+// The decode kernel, which takes every head: rows of a key head to a workgroup; `alike`: which see the same keys.
+int attention_decode_rows(const KvParams &c, const AttentionParams &a, bool alike);
 int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
+// The same for the two halves of attention behind shared prefixes, which always leave partial results.
+int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, Half half, hipStream_t stream);
 // The prompt kernel: rows of a key head to a workgroup, and whether it takes heads of this size.
 int attention_prompt_rows();
 bool attention_prompt_takes(const KvParams &c);
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
+int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, Half half, hipStream_t stream);
+// The launch that joins the parts of both halves (64 together at most), and of sequences without a prefix those of the second.
+constexpr int HALF_PARTS = 32;
+int launch_attention_join_halves(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, const KvParams &cp, const Split &sp, int prefix_tile_rows,
+                                 const Prefixes &x, hipStream_t stream);
 // The launch that joins parts: whether a grid can have so many rows and sequences.
 bool attention_join_takes(const KvParams &c, const AttentionParams &a);
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
@@ -34,6 +54,45 @@ constexpr long long key_word_at(int kv_head, int page_shift, int place, int t, i
 }
 
 #ifdef __HIPCC__
+// Whether sequence b of the call is computed in two halves: the number of its prefix (-1: no), the prefix's length, and the sequence's first row among the prefix's rows.  A
+// sequence whose new tokens begin in front of the prefix's end is looked at as a whole.
+struct Behind {
+  int prefix, length, row;
+};
+__device__ __forceinline__ Behind behind(const KvParams &c, const Prefixes &x, const Sequence &s, int b) {
+  int g = 0;
+  if (x.members) {                                                 // the last prefix that begins at or in front of b
+    int high = x.n;
+    while (high - g > 1) {
+      const int at = (g + high) >> 1;
+      if (x.members[at] <= b) g = at;
+      else high = at;
+    }
+  }
+  const PrefixRows r = prefix_rows(c, x, g);
+  Behind h{-1, 0, s.row0 - r.row0};
+  const int length = min(max(x.lengths[g], 0), x.max_length);
+  if (b >= r.first && b < r.last && s.first >= length && length > 0 && h.row >= 0 && h.row + s.rows <= x.rows_most) {
+    h.prefix = g;
+    h.length = length;
+  }
+  return h;
+}
+template <Half HALF>
+__device__ __forceinline__ Sequence sequence_of(const KvParams &c, const PrefixesOf<HALF> &x, int b) {
+  if constexpr (HALF == WHOLE) return sequence(c, b);
+  else if constexpr (HALF == PREFIX) {
+    const PrefixRows r = prefix_rows(c, x, b);
+    const int length = min(max(c.lengths[b], 0), c.max_length);
+    return Sequence{r.row0, r.rows, length - 1, length, 0};
+  }
+  else {
+    Sequence s = sequence(c, b);
+    s.begin = behind(c, x, s, b).length;
+    return s;
+  }
+}
+
 // The rows of a key head are (new token t, query head of its group), t * group + g.  A tile of them sees keys [low, end) and [0, sinks), of
 // which some rows may see fewer; they are looked at in chunks of 64 keys: `sink_chunks` from 0 on, the others from `first` on.
 struct Span {
@@ -42,12 +101,13 @@ struct Span {
 };
 // The new token of a row of a key head.
 __device__ __forceinline__ int token_of(const AttentionParams &a, int row) { return a.group > 1 ? (int)__umulhi((unsigned)row, a.by_group) : row; }
+template <Half HALF = WHOLE>
 __device__ __forceinline__ Span span_of(const AttentionParams &a, const Sequence &s, int row0, int rows) {
   Span v;
-  v.place_min = s.first + token_of(a, row0);
-  v.place_max = s.first + token_of(a, min(row0 + rows, s.rows * a.group) - 1);
+  v.place_min = HALF == PREFIX ? s.first : s.first + token_of(a, row0);
+  v.place_max = HALF == PREFIX ? s.first : s.first + token_of(a, min(row0 + rows, s.rows * a.group) - 1);
   v.end = max(min(v.place_max + 1, s.end), 0);
-  v.low = a.window > 0 ? max(v.place_min - a.window + 1, 0) : 0;
+  v.low = HALF == OWN ? s.begin : a.window > 0 ? max(v.place_min - a.window + 1, 0) : 0;
   v.first = v.low >> 6;
   v.sink_chunks = min((min(a.sinks, v.low) + 63) >> 6, v.first);
   v.chunks = v.end > 0 ? v.sink_chunks + max(((v.end + 63) >> 6) - v.first, 0) : 0;
@@ -110,9 +170,11 @@ __device__ __forceinline__ half8v halves_of_e4m3(unsigned a, unsigned b, float s
 }
 
 // Which of the places [base, base + 16) a token at `place` sees, as bits.
+template <Half HALF = WHOLE>
 __device__ __forceinline__ unsigned seen_of(const AttentionParams &a, const Sequence &s, int place, int base) {
   auto below = [&](int limit) { return (1u << min(max(limit - base, 0), 16)) - 1u; };
   const unsigned most = below(min(place + 1, s.end));
+  if constexpr (HALF == OWN) return most & ~below(s.begin);
   return a.window > 0 ? most & (~below(place - a.window + 1) | below(a.sinks)) : most;
 }
 // x where bit r of `seen` is set, else minus infinity.
@@ -168,9 +230,10 @@ struct Odd {
   }
 };
 // Which of 64 places from `base` on a token sees.
+template <Half HALF = WHOLE>
 __device__ __forceinline__ unsigned long long seen64_of(const AttentionParams &a, const Sequence &s, int place, int base) {
-  return (unsigned long long)(seen_of(a, s, place, base) | seen_of(a, s, place, base + 16) << 16) |
-         (unsigned long long)(seen_of(a, s, place, base + 32) | seen_of(a, s, place, base + 48) << 16) << 32;
+  return (unsigned long long)(seen_of<HALF>(a, s, place, base) | seen_of<HALF>(a, s, place, base + 16) << 16) |
+         (unsigned long long)(seen_of<HALF>(a, s, place, base + 32) | seen_of<HALF>(a, s, place, base + 48) << 16) << 32;
 }
 
 // A finite stand-in for the base of a row that has seen nothing yet.

@@ -23,8 +23,8 @@ constexpr int waves_of(bool e4m3, int dim) { return !e4m3 && dim > 192 ? DECODE_
 
 // RT: tiles of sixteen rows; D: elements of a head, or (not EXACT) the next multiple of 64, zeros behind the head's own; MANY: rows may be of several new
 // tokens, which see different keys.
-template <bool E4M3, int D, int RT, bool MANY, bool EXACT>
-__global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int tile0, int waves) {
+template <bool E4M3, int D, int RT, bool MANY, bool EXACT, Half HALF>
+__global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int tile0, int waves, const PrefixesOf<HALF> x) {
   const int dim = EXACT ? D : c.head_dim;
   constexpr int BYTES = E4M3 ? 1 : 2, KL = D * BYTES / 64, VL = BYTES, DT = D / 16, STEPS = D / 32, PITCH = D + 4;
   // The next chunk is loaded ahead where there are registers for it beside those of the rows' differences, and its values where the keys leave them room.
@@ -40,18 +40,18 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
   int i = part * waves + wave, k_entry = 0, v_entry = 0;
   float *ml = lds, *out = lds + 2 * 16 * waves, *put_back = out;      // (a wave's first part of put_back is read before its results take the place)
   bool any_odd = false;
-  if (a.window == 0) {
+  if (HALF != OWN && a.window == 0) {
     k_entry = entry(i * 64 + 16 * (n >> 2));
     v_entry = entry(i * 64 + 16 * g);
   }
-  const Sequence s = sequence(c, b);
+  const Sequence s = sequence_of<HALF>(c, x, b);
   const int rows = s.rows * a.group, row0 = tile * 16 * RT, here = min(rows - row0, 16 * RT);
   if (here <= 0) return;
-  const Span span = span_of(a, s, row0, 16 * RT);
+  const Span span = span_of<HALF>(a, s, row0, 16 * RT);
   const int begin = part * waves, end = span.chunks, stride = split.parts * waves;
   if (part > 0 && begin >= end) return;
   const int active = min(max(end - begin, 0), waves);            // waves that have a chunk
-  if (a.window != 0 && i < end) {
+  if ((HALF == OWN || a.window != 0) && i < end) {
     k_entry = entry(span.chunk(i) * 64 + 16 * (n >> 2));
     v_entry = entry(span.chunk(i) * 64 + 16 * g);
   }
@@ -62,12 +62,12 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = min(row0 + rt * 16 + n, rows - 1), t = token_of(a, r);
-    place[rt] = s.first + t;
-    const __half *x = a.q + (s.row0 + t) * a.ldq + ((long long)kv_head * a.group + r - t * a.group) * dim;
+    place[rt] = HALF == PREFIX ? s.first : s.first + t;
+    const __half *from = a.q + (s.row0 + t) * a.ldq + ((long long)kv_head * a.group + r - t * a.group) * dim;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       const int at = E4M3 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 32 + g * 8;
-      const uint4v w = *reinterpret_cast<const uint4b *>(x + (EXACT || at < dim ? at : 0));
+      const uint4v w = *reinterpret_cast<const uint4b *>(from + (EXACT || at < dim ? at : 0));
       q[rt][i] = __builtin_bit_cast(half8v, EXACT || at < dim ? w : uint4v{0, 0, 0, 0});
     }
   }
@@ -171,10 +171,10 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
     }
     // keys that some row does not see: hidden from it; those that no row sees may hold anything, so their values are cleared
     const bool all_there = __ballot(!v_there) == 0;
-    if (!all_there || j0 + 63 > span.place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= span.place_max - a.window)) {
+    if (!all_there || j0 + 63 > span.place_min || j0 + 64 > s.end || (HALF == OWN ? j0 < s.begin : a.window > 0 && j0 <= span.place_max - a.window)) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        const unsigned seen = v_there ? seen_of(a, s, place[rt], j0 + 16 * g) : 0;
+        const unsigned seen = v_there ? seen_of<HALF>(a, s, place[rt], j0 + 16 * g) : 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float4v x = sc[rt][t];
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
       const unsigned bits = (unsigned)(size_t)(__attribute__((address_space(3))) float *)(put_back + RT * waves * 16 * PITCH) + wave * (Odd<E4M3>::KINDS * D * 8) + g * 4 * 8;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        const unsigned long long seen = seen64_of(a, s, place[rt], j0);
+        const unsigned long long seen = seen64_of<HALF>(a, s, place[rt], j0);
         for (int dt = 0; dt < DT && has(dt); ++dt) {
           const unsigned at = bits + dt * 16 * 8;
           float4v *to = reinterpret_cast<float4v *>(put_back + ((rt * waves + wave) * 16 + n) * PITCH + dt * 16 + g * 4);
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * waves_of(E4M3, D)) void attention_decode_kerne
   }
 
   // the waves' results, joined through LDS, sixteen rows at a time
-  const bool whole = parts_of(split, span.chunks) == 1;
+  const bool whole = HALF == WHOLE && parts_of(split, span.chunks) == 1;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int left = here - rt * 16;
@@ -418,16 +418,64 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_kernel(const KvPa
   if (a.lse && threadIdx.x == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
 }
 
-template <bool E4M3, int D, int RT, bool MANY, bool EXACT = true>
-int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  const int waves = attention_decode_waves(c, s.parts);
+// Joins the halves of attention behind shared prefixes, a workgroup to a row as above: lane w of every wave takes part w of the prefix, or of what is the sequence's own behind
+// those.
+template <int D>
+__global__ __launch_bounds__(JOIN_THREADS) void attention_join_halves_kernel(const KvParams c, const AttentionParams a, const Split split, int tile_rows, const KvParams cp,
+                                                                             const Split of_prefix, int prefix_tile_rows, const Prefixes x) {
+  constexpr int LANES = D / 4, SHARES = JOIN_THREADS / LANES;
+  __shared__ __attribute__((aligned(16))) float shares[SHARES][D];
+  __shared__ float factors[64];
+  const int rows_most = c.max_new * a.group, dim = c.head_dim, lane = (int)threadIdx.x & 63;
+  const int row = (int)blockIdx.x, kv_head = (int)blockIdx.y, b = (int)blockIdx.z;
+  const Sequence s = sequence_of<OWN>(c, x, b);
+  if (row >= s.rows * a.group) return;
+  const Behind h = behind(c, x, s, b);
+  const int prefix_row = h.prefix < 0 ? 0 : h.row * a.group + row, before = h.prefix < 0 ? 0 : parts_of(of_prefix, (h.length + 63) >> 6);
+  const int parts = before + parts_of(split, span_of<OWN>(a, s, row & -tile_rows, tile_rows).chunks);
+  const long long own_from = ((long long)b * c.kv_heads + kv_head) * split.parts * rows_most + row;
+  const long long prefix_most = (long long)cp.max_new * a.group, prefix_from = ((long long)h.prefix * c.kv_heads + kv_head) * of_prefix.parts * prefix_most + prefix_row;
+  float2v mine = {-__builtin_inff(), 0.f};
+  if (lane < before) mine = *reinterpret_cast<const float2v *>(of_prefix.ml + (prefix_from + lane * prefix_most) * 2);
+  else if (lane < parts) mine = *reinterpret_cast<const float2v *>(split.ml + (own_from + (long long)(lane - before) * rows_most) * 2);
+  float top = mine.x;
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+  const float f = __builtin_amdgcn_exp2f(mine.x - base_of(top)), total = wave_sum(mine.y * f);
+  if (threadIdx.x < 64) factors[lane] = f;
+  __syncthreads();
+  const int share = (int)threadIdx.x / LANES, d = (int)(threadIdx.x % LANES) * 4;
+  float4v o = {0.f, 0.f, 0.f, 0.f};
+  for (int w = share; w < parts; w += SHARES) {
+    if (d >= dim) continue;
+    const float4v y = *reinterpret_cast<const float4v *>(w < before ? of_prefix.o + (prefix_from + w * prefix_most) * dim + d
+                                                                     : split.o + (own_from + (long long)(w - before) * rows_most) * dim + d);
+    const float fw = factors[w];
+    o.x = __fmaf_rn(y.x, fw, o.x); o.y = __fmaf_rn(y.y, fw, o.y); o.z = __fmaf_rn(y.z, fw, o.z); o.w = __fmaf_rn(y.w, fw, o.w);
+  }
+  *reinterpret_cast<float4v *>(&shares[share][d]) = o;
+  __syncthreads();
+  const int t = token_of(a, row), head = kv_head * a.group + row - t * a.group;
+  if ((int)threadIdx.x < dim) {
+    float y = 0.f;
+#pragma unroll
+    for (int w = 0; w < SHARES; ++w) y += shares[w][threadIdx.x];
+    a.out[(s.row0 + t) * a.ldo + (long long)head * dim + threadIdx.x] = __float2half_rn(y * inverse_of(total));
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[(long long)(s.row0 + t) * a.q_heads + head] = lse_of(top, total);
+}
+
+template <bool E4M3, int D, int RT, bool MANY, bool EXACT, Half HALF>
+int launch(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, hipStream_t stream) {
+  const int waves = attention_decode_waves(c, s.parts, HALF == OWN ? x.max_own : c.max_length);
   const int tiles = (c.max_new * a.group + 16 * RT - 1) / (16 * RT), most = 65535 / s.parts;     // (more tiles than a grid has layers: several launches)
   if (c.n_seqs > 0x7fffffff / 512) return VQ_ERR_SHAPE;
   const int lds = (2 * 16 + 16 * (D + 4) * (MANY ? RT : 1)) * waves * 4 + (MANY ? waves * Odd<E4M3>::KINDS * D * 8 : 0);
-  VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT, MANY, EXACT>));
+  VQ_ALLOW_FULL_LDS((attention_decode_kernel<E4M3, D, RT, MANY, EXACT, HALF>));
   for (int tile0 = 0; tile0 < tiles; tile0 += most) {
     const int now = tiles - tile0 < most ? tiles - tile0 : most;
-    hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY, EXACT>), dim3(c.n_seqs, c.kv_heads, now * s.parts), dim3(64 * waves), lds, stream, c, a, s, now, tile0, waves);
+    hipLaunchKernelGGL((attention_decode_kernel<E4M3, D, RT, MANY, EXACT, HALF>), dim3(c.n_seqs, c.kv_heads, now * s.parts), dim3(64 * waves), lds, stream, c, a, s, now, tile0, waves,
+                       prefixes_of<HALF>(x));
   }
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
@@ -436,39 +484,54 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
 
 // Two tiles share the conversions and loads of a chunk, where the registers are there: not beside 64 of a 16-bit chunk's keys and as many of its values, nor
 // (heads of 128 elements) beside what rows of several tokens need.
-int attention_decode_rows(const KvParams &c, const AttentionParams &a) {
-  return (long long)c.max_new * a.group > 16 && (c.head_dim == 64 || (c.head_dim == 128 && c.e4m3 && c.max_new == 1)) ? 32 : 16;
+int attention_decode_rows(const KvParams &c, const AttentionParams &a, bool alike) {
+  return (long long)c.max_new * a.group > 16 && (c.head_dim == 64 || (c.head_dim == 128 && c.e4m3 && alike)) ? 32 : 16;
 }
 // Where no sequence has a chunk for every wave, no more waves than chunks: more workgroups share a compute unit (8 bits: 36 sequences of up to 13
 // tokens, 32 heads of 64 elements, 10.9 us by eight waves and 7.0 by one; 64 of 250 tokens, 8 key heads of 128, 12.7 by eight and 9.4 by four).
-int attention_decode_waves(const KvParams &c, int parts) {
+int attention_decode_waves(const KvParams &c, int parts, int length) {
   int waves = waves_of(c.e4m3, c.head_dim);
-  while (parts == 1 && waves > 1 && c.max_length <= 32 * waves) waves /= 2;
+  while (parts == 1 && waves > 1 && length <= 32 * waves) waves /= 2;
   return waves;
 }
 int attention_decode_run(const KvParams &c) { return waves_of(c.e4m3, c.head_dim); }
 
-template <bool MANY>
-static int launch_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  const bool two = attention_decode_rows(c, a) == 32;
-  if (c.head_dim == 64) return c.e4m3 ? (two ? launch<true, 64, 2, MANY>(c, a, s, stream) : launch<true, 64, 1, MANY>(c, a, s, stream))
-                                      : (two ? launch<false, 64, 2, MANY>(c, a, s, stream) : launch<false, 64, 1, MANY>(c, a, s, stream));
+template <bool MANY, Half HALF>
+static int launch_decode(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, hipStream_t stream) {
+  const bool two = attention_decode_rows(c, a, !MANY) == 32;
+  if (c.head_dim == 64) return c.e4m3 ? (two ? launch<true, 64, 2, MANY, true, HALF>(c, a, s, x, stream) : launch<true, 64, 1, MANY, true, HALF>(c, a, s, x, stream))
+                                      : (two ? launch<false, 64, 2, MANY, true, HALF>(c, a, s, x, stream) : launch<false, 64, 1, MANY, true, HALF>(c, a, s, x, stream));
   if constexpr (!MANY)
-    if (two) return launch<true, 128, 2, MANY>(c, a, s, stream);
-  return c.e4m3 ? launch<true, 128, 1, MANY>(c, a, s, stream) : launch<false, 128, 1, MANY>(c, a, s, stream);
+    if (two) return launch<true, 128, 2, MANY, true, HALF>(c, a, s, x, stream);
+  return c.e4m3 ? launch<true, 128, 1, MANY, true, HALF>(c, a, s, x, stream) : launch<false, 128, 1, MANY, true, HALF>(c, a, s, x, stream);
 }
 
 // Heads of other sizes: rows of one token as well by what takes several.
-template <int D>
-static int launch_padded(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  return c.e4m3 ? launch<true, D, 1, true, false>(c, a, s, stream) : launch<false, D, 1, true, false>(c, a, s, stream);
+template <int D, Half HALF>
+static int launch_padded(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, hipStream_t stream) {
+  return c.e4m3 ? launch<true, D, 1, true, false, HALF>(c, a, s, x, stream) : launch<false, D, 1, true, false, HALF>(c, a, s, x, stream);
 }
 
-int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+template <Half HALF>
+static int launch_half(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, hipStream_t stream) {
   if (c.head_dim != 64 && c.head_dim != 128)
-    return c.head_dim < 64 ? launch_padded<64>(c, a, s, stream) : c.head_dim < 128 ? launch_padded<128>(c, a, s, stream) :
-           c.head_dim <= 192 ? launch_padded<192>(c, a, s, stream) : launch_padded<256>(c, a, s, stream);
-  return c.max_new > 1 ? launch_decode<true>(c, a, s, stream) : launch_decode<false>(c, a, s, stream);
+    return c.head_dim < 64 ? launch_padded<64, HALF>(c, a, s, x, stream) : c.head_dim < 128 ? launch_padded<128, HALF>(c, a, s, x, stream) :
+           c.head_dim <= 192 ? launch_padded<192, HALF>(c, a, s, x, stream) : launch_padded<256, HALF>(c, a, s, x, stream);
+  if constexpr (HALF != PREFIX)
+    if (c.max_new > 1) return launch_decode<true, HALF>(c, a, s, x, stream);
+  return launch_decode<false, HALF>(c, a, s, x, stream);
+}
+int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) { return launch_half<WHOLE>(c, a, s, Prefixes{}, stream); }
+int launch_attention_decode(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, Half half, hipStream_t stream) {
+  return half == PREFIX ? launch_half<PREFIX>(c, a, s, x, stream) : launch_half<OWN>(c, a, s, x, stream);
+}
+
+int launch_attention_join_halves(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, const KvParams &cp, const Split &sp, int prefix_tile_rows,
+                                 const Prefixes &x, hipStream_t stream) {
+  const dim3 blocks(c.max_new * a.group, c.kv_heads, c.n_seqs);
+  auto kernel = c.head_dim <= 64 ? attention_join_halves_kernel<64> : c.head_dim <= 128 ? attention_join_halves_kernel<128> : attention_join_halves_kernel<256>;
+  hipLaunchKernelGGL(kernel, blocks, dim3(JOIN_THREADS), 0, stream, c, a, s, tile_rows, cp, sp, prefix_tile_rows, x);
+  return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 
 bool attention_join_takes(const KvParams &c, const AttentionParams &a) {

@@ -39,8 +39,8 @@ __device__ __forceinline__ int nth_longest(const KvParams &c, int n, int lane) {
 }
 
 // D: elements of a head, or (not EXACT) more, zeros behind the head's own.
-template <bool E4M3, int D, bool EXACT>
-__global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int zigzag) {
+template <bool E4M3, int D, bool EXACT, Half HALF>
+__global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvParams c, const AttentionParams a, const Split split, int tiles, int zigzag, const PrefixesOf<HALF> x) {
   const int dim = EXACT ? D : c.head_dim;
   constexpr int BYTES = E4M3 ? 1 : 2;
   constexpr int KU = D * BYTES / 16, VU = 64 * BYTES / 16;        // 16-byte words of a key, and of an element's 64 keys
@@ -67,10 +67,10 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
     b = nth_longest(c, rest / split.parts / tiles, lane);
   }
   const int longer = (tiles + 1) / 2, tile = !zigzag || rank < longer ? tiles - 1 - rank : rank - longer;
-  const Sequence s = sequence(c, b);
+  const Sequence s = sequence_of<HALF>(c, x, b);
   const int rows = s.rows * a.group, row0 = tile * ROWS;
   if (row0 >= rows) return;
-  const Span span = span_of(a, s, row0, ROWS);
+  const Span span = span_of<HALF>(a, s, row0, ROWS);
   // chunks of this part: runs, every split.parts-th
   if (part > 0 && part * split.run >= span.chunks) return;
   const int jump = (split.parts - 1) * split.run, run_mask = split.run - 1;
@@ -80,14 +80,14 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   // this wave's rows
   const int wave_row = row0 + wave * 32;
   const bool has_rows = wave_row < rows;
-  const int row = min(wave_row + n, rows - 1), token = token_of(a, row), place = s.first + token;
-  const int place_min = s.first + token_of(a, min(wave_row, rows - 1)), place_max = s.first + token_of(a, min(wave_row + 31, rows - 1));
+  const int row = min(wave_row + n, rows - 1), token = token_of(a, row), place = HALF == PREFIX ? s.first : s.first + token;
+  const int place_min = HALF == PREFIX ? s.first : s.first + token_of(a, min(wave_row, rows - 1)), place_max = HALF == PREFIX ? s.first : s.first + token_of(a, min(wave_row + 31, rows - 1));
   half8v q[STEPS];
   {
-    const __half *x = a.q + (s.row0 + token) * a.ldq + ((long long)kv_head * a.group + row - token * a.group) * dim + h * 8;
+    const __half *from = a.q + (s.row0 + token) * a.ldq + ((long long)kv_head * a.group + row - token * a.group) * dim + h * 8;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i)
-      q[i] = __builtin_bit_cast(half8v, EXACT || i * 16 < dim ? (uint4v)*reinterpret_cast<const uint4b *>(x + i * 16) : uint4v{0, 0, 0, 0});
+      q[i] = __builtin_bit_cast(half8v, EXACT || i * 16 < dim ? (uint4v)*reinterpret_cast<const uint4b *>(from + i * 16) : uint4v{0, 0, 0, 0});
   }
   float m = -__builtin_inff(), l = 0.f;
   float16v o[DT];
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       }
       __builtin_amdgcn_sched_group_barrier(0x8, AHEAD - DT, 0);
       const unsigned is = (unsigned)__builtin_amdgcn_readfirstlane(pages);
-      if (is != 0x01010101u || j0 + 63 > place_min || j0 + 64 > s.end || (a.window > 0 && j0 <= place_max - a.window)) {
+      if (is != 0x01010101u || j0 + 63 > place_min || j0 + 64 > s.end || (HALF == OWN ? j0 < s.begin : a.window > 0 && j0 <= place_max - a.window)) {
         if (E4M3 && (is & 0x04040404u)) {
           // (what the wave that brought this lane's keys of a tile has left of their scale)
           auto rest_at = [&](int r, int by) {
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const unsigned seen = is >> (16 * t + 8 * h) & 1 ? seen_of(a, s, place, j0 + 32 * t + 16 * h) : 0;
+          const unsigned seen = is >> (16 * t + 8 * h) & 1 ? seen_of<HALF>(a, s, place, j0 + 32 * t + 16 * h) : 0;
 #pragma unroll
           for (int r = 0; r < 16; ++r) sc[t].f[r] = where_seen(seen, r, sc[t].f[r]);
         }
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
       }
       __builtin_amdgcn_sched_group_barrier(0x8, DT, 0);
       if (is & 0x02020202u) {
-        const unsigned long long seen = seen64_of(a, s, place, j0);
+        const unsigned long long seen = seen64_of<HALF>(a, s, place, j0);
         unsigned bits = lds_at + bits_of(OF) + h * 4 * 8;
         asm volatile("" : "+v"(bits));
 #pragma unroll
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   across_halves(l, low, high);
   const float total = low + high;
   if (wave_row + n >= rows) return;
-  const bool whole = parts_of(split, span.chunks) == 1;
+  const bool whole = HALF == WHOLE && parts_of(split, span.chunks) == 1;
   const float inverse = inverse_of(total);
   const int head = kv_head * a.group + row - token * a.group;
   const long long to = (((long long)b * c.kv_heads + kv_head) * split.parts + part) * ((long long)c.max_new * a.group) + row;
@@ -424,15 +424,23 @@ __global__ __launch_bounds__(THREADS, 2) void attention_prompt_kernel(const KvPa
   }
 }
 
-template <bool E4M3, int D, bool EXACT = true>
-int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
+template <bool E4M3, int D, bool EXACT, Half HALF>
+int launch(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, hipStream_t stream) {
   const int tiles = (c.max_new * a.group + ROWS - 1) / ROWS;
   const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
   if (blocks > 0xffffffffll / THREADS) return VQ_ERR_SHAPE;        // (threads of a grid)
-  VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D, EXACT>));
-  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D, EXACT>), dim3((unsigned)blocks), dim3(THREADS), 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8 + (E4M3 ? 2 * (D / 64) * WAVES * 4 : 0), stream, c, a, s, tiles,
-                     blocks <= 2 * cu_count());
+  const int lds = 2 * 2 * 64 * D * 2 + 16 + 2 * Odd<E4M3>::KINDS * D * 8 + (E4M3 ? 2 * (D / 64) * WAVES * 4 : 0), zigzag = blocks <= 2 * cu_count();
+  VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D, EXACT, HALF>));
+  hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D, EXACT, HALF>), dim3((unsigned)blocks), dim3(THREADS), lds, stream, c, a, s, tiles, zigzag, prefixes_of<HALF>(x));
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
+}
+
+template <Half HALF>
+int launch_half(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, hipStream_t stream) {
+  if (c.head_dim < 64) return c.e4m3 ? launch<true, 64, false, HALF>(c, a, s, x, stream) : launch<false, 64, false, HALF>(c, a, s, x, stream);
+  if (c.head_dim > 64 && c.head_dim < 128) return c.e4m3 ? launch<true, 128, false, HALF>(c, a, s, x, stream) : launch<false, 128, false, HALF>(c, a, s, x, stream);
+  if (c.head_dim == 64) return c.e4m3 ? launch<true, 64, true, HALF>(c, a, s, x, stream) : launch<false, 64, true, HALF>(c, a, s, x, stream);
+  return c.e4m3 ? launch<true, 128, true, HALF>(c, a, s, x, stream) : launch<false, 128, true, HALF>(c, a, s, x, stream);
 }
 
 }  // namespace
@@ -440,11 +448,9 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, hipStrea
 int attention_prompt_rows() { return ROWS; }
 bool attention_prompt_takes(const KvParams &c) { return c.head_dim <= 128; }
 
-int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) {
-  if (c.head_dim < 64) return c.e4m3 ? launch<true, 64, false>(c, a, s, stream) : launch<false, 64, false>(c, a, s, stream);
-  if (c.head_dim > 64 && c.head_dim < 128) return c.e4m3 ? launch<true, 128, false>(c, a, s, stream) : launch<false, 128, false>(c, a, s, stream);
-  if (c.head_dim == 64) return c.e4m3 ? launch<true, 64>(c, a, s, stream) : launch<false, 64>(c, a, s, stream);
-  return c.e4m3 ? launch<true, 128>(c, a, s, stream) : launch<false, 128>(c, a, s, stream);
+int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream) { return launch_half<WHOLE>(c, a, s, Prefixes{}, stream); }
+int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, Half half, hipStream_t stream) {
+  return half == PREFIX ? launch_half<PREFIX>(c, a, s, x, stream) : launch_half<OWN>(c, a, s, x, stream);
 }
 
 }  // namespace vq

@@ -39,9 +39,35 @@ struct AttentionParams {
 size_t attention_workspace_bytes(const KvParams &c, const AttentionParams &a);
 int launch_attention(const KvParams &c, const AttentionParams &a, void *workspace, size_t workspace_bytes, hipStream_t s);
 
+// Prefixes that sequences have in common.
+struct Prefixes {
+  int n, most, max_length, max_own;  // prefixes; sequences of one, tokens of one and of what a sequence holds behind its own, at most
+  int n_seqs, table_pages;           // sequences of the call; entries of a row of page_table
+  int rows_most;                     // new tokens of one prefix's sequences, at most
+  const int *page_table, *lengths, *members;
+  long long table_stride;
+};
+size_t attention_shared_workspace_bytes(const KvParams &c, const Prefixes &x, const AttentionParams &a);
+int launch_attention_shared(const KvParams &c, const Prefixes &x, const AttentionParams &a, void *workspace, size_t workspace_bytes, hipStream_t s);
+
 int launch_residual_norm(const __half *h, long long ldh, const void *x, long long ldx, const __half *w_post, const __half *gate, long long ldgate,
                          float scale, const __half *w_pre, float eps, bool stream32, int rows, int width, void *y, long long ldy, __half *z,
                          long long ldz, hipStream_t s);
+
+int launch_embed(const int *ids, int rows, const __half *table, long long ld, int vocabulary, int width, float scale, bool stream32, void *y, long long ldy, hipStream_t s);
+
+// Settings of a row: an array's entry, or the number where there is none.
+struct SampleParams {
+  const __half *logits;
+  long long ld;
+  int vocabulary, top_k;
+  float temperature, top_p, min_p;
+  const float *uniform, *temperatures, *top_ps, *min_ps;
+  const int *top_ks;
+  int *tokens;
+  float *probabilities;
+};
+int launch_sample(const SampleParams &p, int rows, hipStream_t s);
 
 #ifdef __HIPCC__
 typedef unsigned uint4v __attribute__((ext_vector_type(4)));
@@ -53,9 +79,9 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 
 // A sequence of the call: its new tokens are rows row0 ... row0 + rows - 1, token t stands at place first + t, and places
-// below `end` exist.
+// below `end` exist, of which those from `begin` on are looked at.
 struct Sequence {
-  int row0, rows, first, end;
+  int row0, rows, first, end, begin;
 };
 __device__ __forceinline__ Sequence sequence(const KvParams &c, int b) {
   Sequence s;
@@ -71,7 +97,24 @@ __device__ __forceinline__ Sequence sequence(const KvParams &c, int b) {
   s.rows = min(brings, c.max_new);
   s.first = length - brings;
   s.end = min(length, c.max_length);
+  s.begin = 0;
   return s;
+}
+
+// First row of sequence i's new tokens (i may be n_seqs: the row behind the last).
+__device__ __forceinline__ int row_of(const KvParams &c, int i) { return c.starts ? min(max(c.starts[i], 0), c.n_tokens) : i * c.each; }
+
+// The rows of a prefix: new tokens of its sequences, [row0, row0 + rows); what stands behind rows_most is left out.
+struct PrefixRows {
+  int first, last, row0, rows;       // sequences [first, last)
+};
+__device__ __forceinline__ PrefixRows prefix_rows(const KvParams &c, const Prefixes &x, int g) {
+  PrefixRows r;
+  r.first = x.members ? min(max(x.members[g], 0), x.n_seqs) : 0;
+  r.last = min(x.members ? min(max(x.members[g + 1], r.first), x.n_seqs) : x.n_seqs, r.first + x.most);
+  r.row0 = row_of(c, r.first);
+  r.rows = min(max(row_of(c, r.last) - r.row0, 0), x.rows_most);
+  return r;
 }
 
 // Page of block `block` (< table_pages) of sequence b, -1 where there is none.
