@@ -1,10 +1,11 @@
 // The next token of each row of logits: by temperature, the top_k largest, the smallest set that holds top_p of what they weigh, what weighs at least min_p of the largest, and a
 // given random number.
 //
-// Logits are binary16, of which there are 63489 values above minus infinity: a row's counts by value say all but which of equal tokens is meant.  So nothing is sorted and no token's
-// weight is computed: a workgroup counts its row in LDS (one bin for each value, the largest first), sums counts and weights over the bins in binary64, finds the borders
-// and the value that the random number falls on by these sums, and then that value's n-th occurrence in the row.
+// Logits are binary16, of which there are 31744 finite sizes and two signs: a row's counts by value say all but which of equal tokens is meant.  So nothing is sorted and no
+// token's weight is computed: a workgroup counts its row in LDS by value, sums counts and weights over the values in binary64, the largest first, finds the borders and the
+// value that the random number falls on by these sums, and then that value's n-th occurrence in the row.
 //
+// 32 neighbouring values of a sign (a run) lie a constant distance apart, so that their weights are w q^i, one exponential and a polynomial in q with the counts as coefficients.
 // Sums are of 64 bits, in an order that depends on nothing: which token a number falls on is decided by sums over the vocabulary, whose rounding in 32 bits (2^-24 times a sum's
 // terms) is as large as a rare token's share.
 #include "vq_kv.hpp"
@@ -14,32 +15,46 @@ namespace vq {
 namespace {
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
-// Bins in descending order of the values they stand for: infinity is bin 0, -65504 is bin LAST; what is left (minus infinity, NaN) has larger numbers.  A thread's sums are of slices of sixteen bins,
-// slice r * THREADS + thread for r < ROUNDS.
-constexpr int TOP_KEY = 0xFC00, LAST = TOP_KEY - 0x400, SLICE = 16, ROUNDS = 4, BINS = ROUNDS * THREADS * SLICE;
-static_assert(BINS > LAST && BINS == 65536, "a bin for every value");
+// Words of LDS by size (the number without its sign): occurrences of the positive number in the lower half, of the negative one in the upper.  Sizes from INF on are not finite.
+constexpr int INF = 0x7C00, WORDS = 0x8000, RUN = 32, RUNS = INF / RUN;
+// Runs in the order of their values: those of positive numbers, from the largest on, then those of negative ones.  Zero, of either sign, is the last value of the former.
+constexpr int ENTRIES = 2 * RUNS, PADDED = 2 * THREADS;
+constexpr int OCTAVES = INF / 1024;
+static_assert(ENTRIES <= PADDED && INF % RUN == 0 && 1024 % RUN == 0, "runs lie within a power of two");
 
-typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
-typedef short short2v __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) unsigned *Lds;
 
-// Bins of the two numbers of a word; -0 counts as +0.
-__device__ __forceinline__ unsigned bins_of(unsigned word) {
-  const half2v zero = {(_Float16)0.f, (_Float16)0.f};
-  const short2v x = __builtin_bit_cast(short2v, half2_of(word) + zero);
-  const short2v sign = x >> 15;
-  const ushort2v key = __builtin_bit_cast(ushort2v, x ^ (sign | (short2v){(short)0x8000, (short)0x8000}));
-  return __builtin_bit_cast(unsigned, (ushort2v){(unsigned short)TOP_KEY, (unsigned short)TOP_KEY} - key);
-}
-__device__ __forceinline__ float value_of(int bin) {
-  const unsigned key = (unsigned)(TOP_KEY - bin);
-  return __half2float(__ushort_as_half((unsigned short)(key & 0x8000u ? key ^ 0x8000u : key ^ 0xFFFFu)));
-}
-
-// Where a sum reaches a border: bins below `bin` and `n` of that bin's tokens are in front of it.
-struct Border {
-  int bin, n;
+// A value's place in the order of all: the i-th of run `entry`.
+struct Place {
+  int entry, i;
 };
-__device__ __forceinline__ Border nearer(Border a, Border b) { return a.bin < b.bin || (a.bin == b.bin && a.n < b.n) ? a : b; }
+// Where a sum reaches a border: what stands in front of `at` and `n` of that value's tokens are in front of it, and weigh `mass`.
+struct Border {
+  Place at;
+  int n;
+  double mass;
+};
+__device__ __forceinline__ int order_of(Place p) { return p.entry * RUN + p.i; }
+__device__ __forceinline__ bool in_front(Border a, Border b) { return order_of(a.at) < order_of(b.at) || (order_of(a.at) == order_of(b.at) && a.n < b.n); }
+__device__ __forceinline__ int size_of(Place p) { return p.entry < RUNS ? (RUNS - 1 - p.entry) * RUN + RUN - 1 - p.i : (p.entry - RUNS) * RUN + p.i; }
+__device__ __forceinline__ unsigned bits_of(Place p) { return (unsigned)size_of(p) | (p.entry < RUNS ? 0u : 0x8000u); }
+__device__ __forceinline__ Place place_of(unsigned bits) {
+  const int size = (int)(bits & 0x7FFFu), run = size / RUN;
+  return bits & 0x8000u && size ? Place{RUNS + run, size % RUN} : Place{RUNS - 1 - run, RUN - 1 - size % RUN};
+}
+__device__ __forceinline__ float number_of(unsigned bits) { return __half2float(__ushort_as_half((unsigned short)bits)); }
+
+// exp(y), y <= 0: 2^n times the series of exp on half a factor of two on either side of one, whose 14th term is below 2^-57.
+__device__ __forceinline__ double exp_of(double y) {
+  y = fmax(y, -1000.0);
+  const double n = __builtin_rint(y * 1.4426950408889634074), r = __fma_rn(n, -0x1.abc9e3b39803fp-56, __fma_rn(n, -0x1.62e42fefa39efp-1, y));
+  double p = 1.0 / 6227020800.0;
+#define VQ_TERM(FACTORIAL) p = __fma_rn(p, r, 1.0 / FACTORIAL)
+  VQ_TERM(479001600.0); VQ_TERM(39916800.0); VQ_TERM(3628800.0); VQ_TERM(362880.0); VQ_TERM(40320.0); VQ_TERM(5040.0); VQ_TERM(720.0); VQ_TERM(120.0);
+  VQ_TERM(24.0); VQ_TERM(6.0); VQ_TERM(2.0); VQ_TERM(1.0); VQ_TERM(1.0);
+#undef VQ_TERM
+  return ldexp(p, (int)n);
+}
 
 struct Row {
   const __half *logits;
@@ -48,349 +63,442 @@ struct Row {
   int top_k;
 };
 
-// What the workgroup shares beside the bins.
+// What the workgroup shares beside the counts: the sums up to each run's end, and what its waves tell each other.
 struct Scratch {
-  double mass[64], before_mass;
-  unsigned count[64], before_count, counts[SLICE];
-  int top, slice, below, valid, found[WAVES];
+  double mass[PADDED];
+  unsigned count[PADDED];
+  double wave_mass[WAVES];
+  double powers[OCTAVES][RUN / 4];    // by the power of two of a run's sizes: (the factor from a number's weight to the next one's)^(4 i)
+  double below_mass;
+  int below_entry, below_i;
+  unsigned wave_count[WAVES], wave_valid[WAVES], wave_top[WAVES], counts[RUN];
+  int found[WAVES], of_tail, bits, nth;
+  float probability;
 };
 
-// A workgroup's walk over a row: eight numbers a lane, each wave a range of its own.
+// A wave's part of a range of vectors of eight numbers.
 struct Walk {
-  int begin, end;                   // vectors of eight, of this wave
+  int begin, end;
 };
 __device__ __forceinline__ Walk walk_of(int first, int vectors, int wave) {
   const int each = (vectors + WAVES * 64 - 1) / (WAVES * 64) * 64;
-  Walk w;
-  w.begin = first + min(wave * each, vectors);
-  w.end = first + min((wave + 1) * each, vectors);
-  return w;
+  return Walk{first + min(wave * each, vectors), first + min((wave + 1) * each, vectors)};
 }
-__device__ __forceinline__ uint4v load8(const Row &r, int vector) {
-  const int i = vector * 8;
-  if (i + 8 <= r.vocabulary) return *reinterpret_cast<const uint4b *>(r.logits + i);
-  unsigned w[4];
+constexpr unsigned NONE = 0xFC00FC00u;                              // two minus infinities
+__device__ __forceinline__ uint4v load8(const Row &r, int vector) { return *reinterpret_cast<const uint4b *>(r.logits + (long long)vector * 8); }
+// What is left of a row behind its whole vectors, in the last thread of the workgroup; minus infinities in the others.
+__device__ __forceinline__ uint4v tail_of(const Row &r, int tid) {
+  uint4v x = {NONE, NONE, NONE, NONE};
+  const int from = r.vocabulary & ~7, n = r.vocabulary & 7;
+  if (n && tid == THREADS - 1) {
+    unsigned h[8];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int at = i + 2 * j;
-    const unsigned low = at < r.vocabulary ? __half_as_ushort(r.logits[at]) : 0xFC00u, high = at + 1 < r.vocabulary ? __half_as_ushort(r.logits[at + 1]) : 0xFC00u;
-    w[j] = low | high << 16;
+    for (int j = 0; j < 8; ++j) h[j] = j < n ? __half_as_ushort(r.logits[from + j]) : 0xFC00u;
+    x = uint4v{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
   }
-  return uint4v{w[0], w[1], w[2], w[3]};
+  return x;
 }
-// f(bins of a vector's four words, vector) for this wave's vectors; those past the end are of minus infinities.
+// The first HELD of a lane's vectors stay in registers.
+template <int HELD>
+struct Held {
+  uint4v x[HELD];
+};
+// f(a vector's four words) for this wave's vectors, AHEAD of which are on their way at once.
 template <int AHEAD, typename F>
 __device__ __forceinline__ void walk(const Row &r, Walk w, int lane, F f) {
   for (int v0 = w.begin; v0 < w.end; v0 += 64 * AHEAD) {
     uint4v x[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int v = v0 + u * 64 + lane;
-      x[u] = v < w.end ? load8(r, v) : uint4v{0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
-    }
+    for (int u = 0; u < AHEAD; ++u) x[u] = load8(r, min(v0 + u * 64 + lane, w.end - 1));
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-      if (v0 + u * 64 < w.end) f(uint4v{bins_of(x[u].x), bins_of(x[u].y), bins_of(x[u].z), bins_of(x[u].w)}, v0 + u * 64 + lane);
+      if (v0 + u * 64 + lane < w.end) f(x[u]);
   }
 }
+__device__ __forceinline__ unsigned half_at(uint4v x, int j) {
+  const unsigned w = j < 2 ? x.x : j < 4 ? x.y : j < 6 ? x.z : x.w;
+  return j & 1 ? w >> 16 : w & 0xffff;
+}
 
-// WIDE: counts of 32 bits, half of the bins at a time, for a row in which a value occurs more than 65535 times; otherwise two bins to a word.
+__device__ __forceinline__ void add(unsigned address, unsigned n) {
+  __hip_atomic_fetch_add((Lds)(size_t)address, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+// factor * the lower or upper half of a word + more
+template <bool UPPER>
+__device__ __forceinline__ unsigned of_half(unsigned word, unsigned factor, unsigned more) {
+  unsigned r;
+  if (UPPER) asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(r) : "v"(word), "s"(factor), "v"(more));
+  else asm("v_mad_u32_u16 %0, %1, %2, %3" : "=v"(r) : "v"(word), "s"(factor), "v"(more));
+  return r;
+}
+
+// Inclusive sums over the wave's lanes, by DPP: within rows of sixteen lanes, then the rows.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double x) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+  const unsigned low = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xF, false), high = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(double, (unsigned long long)low | (unsigned long long)high << 32);
+}
+__device__ __forceinline__ double sums_of(double x) {
+  x += moved<0x111, 0xF>(x);
+  x += moved<0x112, 0xF>(x);
+  x += moved<0x114, 0xF>(x);
+  x += moved<0x118, 0xF>(x);
+  x += moved<0x142, 0xA>(x);
+  x += moved<0x143, 0xC>(x);
+  return x;
+}
+__device__ __forceinline__ unsigned sums_of(unsigned x) {
+#define VQ_MOVED(CTRL, ROWS) x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false)
+  VQ_MOVED(0x111, 0xF); VQ_MOVED(0x112, 0xF); VQ_MOVED(0x114, 0xF); VQ_MOVED(0x118, 0xF); VQ_MOVED(0x142, 0xA); VQ_MOVED(0x143, 0xC);
+#undef VQ_MOVED
+  return x;
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+  const unsigned low = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, lane), high = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
+  return __builtin_bit_cast(double, (unsigned long long)low | (unsigned long long)high << 32);
+}
+__device__ __forceinline__ unsigned of_lane(unsigned x, int lane) { return (unsigned)__builtin_amdgcn_readlane((int)x, lane); }
+
+// WIDE: counts of 32 bits, of one sign after the other, for rows in which a number occurs more than 65535 times.
 template <bool WIDE>
 struct Drawer {
   const Row &r;
-  unsigned *bins;
+  unsigned *words;
   Scratch &s;
   int tid, lane, wave;
-  // sums up to the end of this thread's slices, and in front of them
-  unsigned count[ROUNDS], count_before[ROUNDS];
-  double mass[ROUNDS], mass_before[ROUNDS], per;          // per: one over the temperature
-  unsigned total_count;
-  double total_mass;
-  float top;
+  double top, per;                 // the largest logit; one over the temperature
 
-  __device__ __forceinline__ double weight(int bin) const { return s.top == 0 ? (bin == 0 ? 1.0 : 0.0) : exp(((double)value_of(bin) - (double)top) * per); }
+  // (1 for numbers above the largest, of which there are none)
+  __device__ __forceinline__ double weight(unsigned bits) const { return exp_of(fmin(((double)number_of(bits) - top) * per, 0.0)); }
 
-  // Counts the row's numbers with bins from `low` on; -> numbers of this thread that have a bin.
-  __device__ __forceinline__ unsigned count_bins(int low) {
-    uint4v *words = reinterpret_cast<uint4v *>(bins);
-    for (int i = tid; i < BINS / 8; i += THREADS) words[i] = uint4v{0, 0, 0, 0};
+  // Counts the row (WIDE: its numbers of one sign; zeros are positive); -> of this thread's numbers, those that are not NaN or minus infinity, and the largest ones of either half.
+  template <int HELD>
+  __device__ __forceinline__ unsigned count(bool negative, half2v &largest, Held<HELD> &held) {
+    const Walk of_wave = walk_of(0, r.vocabulary / 8, wave);
+    if constexpr (HELD > 0) {
+#pragma unroll
+      for (int u = 0; u < HELD; ++u)
+        if (of_wave.begin + u * 64 < of_wave.end) held.x[u] = load8(r, min(of_wave.begin + u * 64 + lane, of_wave.end - 1));
+    }
+    const uint4v tail = tail_of(r, tid);
+    uint4v *all = reinterpret_cast<uint4v *>(words);
+    for (int i = tid; i < WORDS / 4; i += THREADS) all[i] = uint4v{0, 0, 0, 0};
     __syncthreads();
+    const unsigned base = (unsigned)(size_t)(Lds)words;
     unsigned valid = 0;
-    auto add = [&](unsigned bin, unsigned n) {
-      if (WIDE ? bin - low < BINS / 2 && bin <= LAST : bin <= LAST) {
-        valid += n;
-        if (WIDE) atomicAdd(bins + (bin - low), n);
-        else atomicAdd(bins + (bin >> 1), bin & 1 ? n << 16 : n);
-      }
-    };
-    walk<WIDE ? 4 : 8>(r, walk_of(0, (r.vocabulary + 7) / 8, wave), lane, [&](uint4v b, int) {
-      // (eight times the same, as masks leave it: one addition)
-      if (b.x == b.y && b.z == b.w && b.x == b.z && (b.x & 0xffff) == b.x >> 16) {
-        add(b.x & 0xffff, 8);
+    largest = half2v{(_Float16)-__builtin_inff(), (_Float16)-__builtin_inff()};
+    auto one = [&](uint4v x) {
+      const uint4v size = x & 0x7FFF7FFFu;
+      auto larger = [](unsigned a, unsigned b) {
+        typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
+      };
+      const bool odd = ((larger(larger(size.x, size.y), larger(size.z, size.w)) + 0x04000400u) & 0x80008000u) != 0, alike = x.x == x.y && x.x == x.z && x.x == x.w;
+      largest = __builtin_elementwise_max(largest, __builtin_elementwise_max(__builtin_elementwise_max(half2_of(x.x), half2_of(x.y)), __builtin_elementwise_max(half2_of(x.z), half2_of(x.w))));
+      if (WIDE || odd || alike) {
+        // what is not counted, and eight times the same, as masks leave it: one addition, where 64 lanes that add one to the same word take 64 turns
+        if (alike && x.x == NONE) return;
+        const bool same = alike && (x.x & 0xffff) == x.x >> 16;
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {
+          const unsigned bits = half_at(x, j), m = bits & 0x7FFF, n = same ? 8 : 1;
+          const bool minus = bits >= 0x8000u && m;
+          if (m > INF || (m == INF && minus) || (same && j)) continue;
+          valid += n;
+          if (!WIDE) add(base + m * 4, bits & 0x8000u ? n << 16 : n);
+          else if (minus == negative) add(base + m * 4, n);
+        }
         return;
       }
-      add(b.x & 0xffff, 1); add(b.x >> 16, 1); add(b.y & 0xffff, 1); add(b.y >> 16, 1);
-      add(b.z & 0xffff, 1); add(b.z >> 16, 1); add(b.w & 0xffff, 1); add(b.w >> 16, 1);
-    });
-    __syncthreads();
+      valid += 8;
+      const uint4v sign = (x >> 15) & 0x00010001u;
+      auto two = [&](unsigned m, unsigned minus) {
+        add(of_half<false>(m, 4, base), of_half<false>(minus, 0xFFFF, 1));
+        add(of_half<true>(m, 4, base), of_half<true>(minus, 0xFFFF, 1));
+      };
+      two(size.x, sign.x); two(size.y, sign.y); two(size.z, sign.z); two(size.w, sign.w);
+    };
+    if constexpr (HELD > 0) {
+#pragma unroll
+      for (int u = 0; u < HELD; ++u)
+        if (of_wave.begin + u * 64 + lane < of_wave.end) one(held.x[u]);
+    } else {
+      walk<WIDE ? 2 : 8>(r, of_wave, lane, one);
+    }
+    one(tail);
     return valid;
   }
-
-  // The words of a slice, and which of its bins are not empty.
-  struct Words {
-    uint4v a, b, c, d;
-  };
-  __device__ __forceinline__ Words words_of(int slice) const {
-    const uint4v *w = reinterpret_cast<const uint4v *>(bins) + slice * (WIDE ? 4 : 2);
-    Words x{w[0], w[1], uint4v{0, 0, 0, 0}, uint4v{0, 0, 0, 0}};
-    if (WIDE) {
-      x.c = w[2];
-      x.d = w[3];
+  // The sum of all threads' `valid` and the largest number, for all of them.
+  __device__ __forceinline__ void tell(unsigned valid, half2v largest, unsigned &valid_of_all, float &top_of_all) {
+    float x = fmaxf((float)largest.x, (float)largest.y);
+    valid = sums_of(valid);
+#define VQ_LARGER(CTRL, ROWS) x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false)))
+    VQ_LARGER(0x111, 0xF); VQ_LARGER(0x112, 0xF); VQ_LARGER(0x114, 0xF); VQ_LARGER(0x118, 0xF); VQ_LARGER(0x142, 0xA); VQ_LARGER(0x143, 0xC);
+#undef VQ_LARGER
+    if (lane == 63) {
+      s.wave_valid[wave] = valid;
+      s.wave_top[wave] = __float_as_uint(x);
     }
-    return x;
-  }
-  __device__ __forceinline__ static unsigned some(const Words &x) {
-    const unsigned w[16] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w, x.c.x, x.c.y, x.c.z, x.c.w, x.d.x, x.d.y, x.d.z, x.d.w};
-    unsigned mask = 0;
-#pragma unroll
-    for (int i = 0; i < SLICE; ++i) mask |= (WIDE ? w[i] : i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffff) != 0 ? 1u << i : 0u;
-    return mask;
-  }
-  __device__ __forceinline__ unsigned count_at(int slice, int i) const {      // (slice: among those that are counted)
-    return WIDE ? bins[slice * SLICE + i] : reinterpret_cast<const unsigned short *>(bins)[slice * SLICE + i];
-  }
-
-  // Counts and weights of this thread's slices of the bins that are counted; the first of all bins that is not empty is the row's maximum.
-  template <int FROM, int TO>
-  __device__ __forceinline__ void sum_slices() {
-    unsigned mask[TO - FROM];
-    int first = BINS;
-#pragma unroll
-    for (int q = FROM; q < TO; ++q) {
-      mask[q - FROM] = some(words_of((q - FROM) * THREADS + tid));
-      if (mask[q - FROM] && first == BINS) first = (q * THREADS + tid) * SLICE + __builtin_ctz(mask[q - FROM]);
-    }
-    first = (int)wave_min_u32((unsigned)first);
-    if (lane == 0 && first < BINS) atomicMin(&s.top, first);
     __syncthreads();
-    top = value_of(min(s.top, LAST));
-    int below = BINS;
+    valid_of_all = 0;
+    top_of_all = -__builtin_inff();
 #pragma unroll
-    for (int q = FROM; q < TO; ++q) {
-      unsigned c = 0, left = mask[q - FROM];
-      double m = 0.0;
-      while (left) {
-        const int i = __builtin_ctz(left), bin = (q * THREADS + tid) * SLICE + i;
-        left &= left - 1;
-        const unsigned n = count_at((q - FROM) * THREADS + tid, i);
-        const double w = weight(bin);
-        c += n;
-        m += (double)n * w;
-        if (w < (double)r.min_p && bin < below) below = bin;
-      }
-      count[q] = c;
-      mass[q] = m;
+    for (int w = 0; w < WAVES; ++w) {
+      valid_of_all += s.wave_valid[w];
+      top_of_all = fmaxf(top_of_all, __uint_as_float(s.wave_top[w]));
     }
-    if (below < BINS) atomicMin(&s.below, below);
   }
 
-  // The slices' sums, from the first on.
+  // How far numbers of a power of two are apart.
+  __device__ __forceinline__ static double distance(int octave) { return (double)number_of((unsigned)octave * 1024 + 1) - (double)number_of((unsigned)octave * 1024); }
+  __device__ __forceinline__ void make_powers() {
+    if (tid < OCTAVES * (RUN / 4)) s.powers[tid / (RUN / 4)][tid % (RUN / 4)] = exp_of(-distance(tid / (RUN / 4)) * per * (double)(tid % (RUN / 4) * 4));
+  }
+  // Counts and weights of the runs of both signs (WIDE: of one), of a thread's 32 sizes, to the scratch.
+  __device__ __forceinline__ void sum_runs(bool negative) {
+    if (tid < PADDED - ENTRIES) {                                   // (entries behind the last run)
+      s.mass[ENTRIES + tid] = 0.0;
+      s.count[ENTRIES + tid] = 0;
+    }
+    if (tid >= RUNS) return;
+    const uint4v *from = reinterpret_cast<const uint4v *>(words) + tid * (RUN / 4);
+    // A run's powers of q begin at its largest number, that of largest size of the positive and of smallest size of the negative ones, and in the run of the row's largest number at
+    // that one, whose weight is one without a rounding (of equal logits the sums are whole numbers then).  Lanes begin in different quarters of their runs, whose first words lie in the
+    // same bank of LDS for every second lane.
+    const unsigned least = (unsigned)tid * RUN, of_top = __half_as_ushort(__float2half_rn((float)top)), top_size = of_top & 0x7FFFu;
+    const bool has_top = top_size / RUN == (unsigned)tid, top_plus = has_top && (of_top < 0x8000u || !top_size), top_minus = has_top && !top_plus;
+    const int from_plus = top_plus ? (int)(top_size % RUN) : RUN - 1, from_minus = top_minus ? (int)(top_size % RUN) : 0;
+    const double(&powers)[RUN / 4] = s.powers[tid / (1024 / RUN)];
+    const double q = exp_of(-distance(tid / (1024 / RUN)) * per), q2 = q * q;
+    struct Four {
+      unsigned a[4], b[4];
+    };
+    auto four = [&](int c) {
+      const uint4v w = from[c];
+      Four f = WIDE ? Four{{w.x, w.y, w.z, w.w}, {w.x, w.y, w.z, w.w}}
+                    : Four{{w.x & 0xffff, w.y & 0xffff, w.z & 0xffff, w.w & 0xffff}, {w.x >> 16, w.y >> 16, w.z >> 16, w.w >> 16}};
+      if (!WIDE && tid == 0 && c == 0) {                            // zeros
+        f.a[0] += f.b[0];
+        f.b[0] = 0;
+      }
+      return f;
+    };
+    double plus = 0.0, minus = 0.0;
+    unsigned n_plus = 0, n_minus = 0;
+#pragma unroll 1
+    for (int j = 0; j < RUN / 4; ++j) {
+      const int c = (j + (lane >> 1)) & 7;
+      const Four f = four(c);
+      auto power = [&](int e) {                                     // q^e
+        double p = powers[e >> 2];
+        if (has_top) p *= (e & 1 ? q : 1.0) * (e & 2 ? q2 : 1.0);
+        return p;
+      };
+      if (!WIDE || !negative) {
+        n_plus += (f.a[0] + f.a[1]) + (f.a[2] + f.a[3]);
+        const int e = from_plus - 4 * c - 3;
+        if (e >= 0) plus = __fma_rn(__fma_rn(__fma_rn(__fma_rn((double)f.a[0], q, (double)f.a[1]), q, (double)f.a[2]), q, (double)f.a[3]), power(e), plus);
+      }
+      if (!WIDE || negative) {
+        n_minus += (f.b[0] + f.b[1]) + (f.b[2] + f.b[3]);
+        const int e = 4 * c - from_minus;
+        if (e >= 0) minus = __fma_rn(__fma_rn(__fma_rn(__fma_rn((double)f.b[3], q, (double)f.b[2]), q, (double)f.b[1]), q, (double)f.b[0]), power(e), minus);
+      }
+    }
+    if (has_top) {                                                  // the four around the largest number, where the powers begin among them
+      const int c = (int)(top_size % RUN) / 4, at = (int)(top_size % 4);
+      const Four f = four(c);
+      double sum = 0.0;
+      if (top_plus && at < 3) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (i <= at) sum = __fma_rn(sum, q, (double)f.a[i]);
+        plus += sum;
+      }
+      if (top_minus && at > 0) {
+#pragma unroll
+        for (int i = 3; i > 0; --i)
+          if (i >= at) sum = __fma_rn(sum, q, (double)f.b[i]);
+        minus += sum;
+      }
+    }
+    const double w_plus = weight(least + RUN - 1), w_minus = weight(least | 0x8000u);
+    if (!WIDE || !negative) {
+      s.mass[RUNS - 1 - tid] = n_plus ? plus * w_plus : 0.0;
+      s.count[RUNS - 1 - tid] = n_plus;
+    }
+    if (!WIDE || negative) {
+      s.mass[RUNS + tid] = n_minus ? minus * w_minus : 0.0;
+      s.count[RUNS + tid] = n_minus;
+    }
+  }
+
+  // Sums up to each run's end in place of its own.
   __device__ __forceinline__ void scan() {
-#pragma unroll
-    for (int q = 0; q < ROUNDS; ++q) {
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const unsigned c = __shfl_up(count[q], d);
-        const double m = __shfl_up(mass[q], d);
-        if (lane >= d) {
-          count[q] += c;
-          mass[q] += m;
-        }
-      }
-      if (lane == 63) {
-        s.count[q * WAVES + wave] = count[q];
-        s.mass[q * WAVES + wave] = mass[q];
-      }
-      count_before[q] = __shfl_up(count[q], 1);
-      mass_before[q] = __shfl_up(mass[q], 1);
-      if (lane == 0) {
-        count_before[q] = 0;
-        mass_before[q] = 0.0;
-      }
+    __syncthreads();
+    const double m0 = s.mass[2 * tid], m1 = s.mass[2 * tid + 1];
+    const unsigned c0 = s.count[2 * tid], c1 = s.count[2 * tid + 1];
+    const double m = sums_of(m0 + m1);
+    const unsigned c = sums_of(c0 + c1);
+    if (lane == 63) {
+      s.wave_mass[wave] = m;
+      s.wave_count[wave] = c;
     }
     __syncthreads();
-    unsigned c = s.count[lane];
-    double m = s.mass[lane];
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const unsigned pc = __shfl_up(c, d);
-      const double pm = __shfl_up(m, d);
-      if (lane >= d) {
-        c += pc;
-        m += pm;
-      }
+    double before = 0.0;
+    unsigned count_before = 0;
+    for (int w = 0; w < wave; ++w) {
+      before += s.wave_mass[w];
+      count_before += s.wave_count[w];
     }
-    total_count = __shfl(c, 63);
-    total_mass = __shfl(m, 63);
-#pragma unroll
-    for (int q = 0; q < ROUNDS; ++q) {
-      const int at = q * WAVES + wave;
-      const unsigned pc = __shfl(c, (at - 1) & 63);
-      const double pm = __shfl(m, (at - 1) & 63);
-      if (at > 0) {
-        count[q] += pc;
-        count_before[q] += pc;
-        mass[q] += pm;
-        mass_before[q] += pm;
-      }
-    }
+    s.mass[2 * tid + 1] = before + m;
+    s.count[2 * tid + 1] = count_before + c;
+    s.mass[2 * tid] = before + m - m1;
+    s.count[2 * tid] = count_before + c - c1;
+    __syncthreads();
   }
 
-  // One slice: lane i of every wave has bin i (lanes 0 .. 15, others an empty one): its count and weight, and the sums up to the bin's end.
-  struct Bin {
-    int bin;
-    unsigned n, count;
-    double weight, mass;
+  // One run: lane i of the wave has its i-th value (lanes from RUN on: none): its bits, how often it occurs, its weight, and the sums up to it.
+  struct Value {
+    unsigned bits, n, count;
+    double weight, mass, before;   // before: in front of the run
   };
-  __device__ __forceinline__ Bin bin_of(int slice) {
-    Bin b;
-    b.bin = slice * SLICE + lane;
+  __device__ __forceinline__ Value values_of(int entry) {
+    Value v;
+    const Place p{entry, lane & (RUN - 1)};
+    v.bits = bits_of(p);
     if (WIDE) {
-      if (tid < SLICE) s.counts[tid] = 0;
+      // the row once more, equal ones in succession added together
       __syncthreads();
-      unsigned n = 0, of = 0;                                     // (equal ones in a row are added together)
+      if (tid < RUN) s.counts[tid] = 0;
+      __syncthreads();
+      unsigned n = 0;
+      int of = 0;
       auto flush = [&] {
         if (n) atomicAdd(&s.counts[of], n);
       };
-      walk<1>(r, walk_of(0, (r.vocabulary + 7) / 8, wave), lane, [&](uint4v x, int) {
-        const unsigned w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
+      walk<1>(r, walk_of(0, r.vocabulary / 8, wave), lane, [&](uint4v x) {
+#pragma unroll 1
         for (int j = 0; j < 8; ++j) {
-          const unsigned bin = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffff;
-          if ((int)(bin / SLICE) != slice) continue;
-          if (bin % SLICE != of) {
+          const unsigned bits = half_at(x, j);
+          if ((bits & 0x7FFFu) >= INF) continue;
+          const Place here = place_of(bits);
+          if (here.entry != entry) continue;
+          if (here.i != of) {
             flush();
             n = 0;
-            of = bin % SLICE;
+            of = here.i;
           }
           ++n;
         }
       });
       flush();
       __syncthreads();
-      b.n = lane < SLICE ? s.counts[lane] : 0;
+      v.n = s.counts[p.i];
     } else {
-      b.n = lane < SLICE ? count_at(slice, lane) : 0;
+      const unsigned w = words[size_of(p)];
+      v.n = v.bits & 0x8000u ? w >> 16 : v.bits ? w & 0xffff : (w & 0xffff) + (w >> 16);
+      if (v.bits == 0x8000u) v.n = 0;                               // (counted as zero)
     }
-    b.weight = b.n ? weight(b.bin) : 0.0;
-    b.count = b.n;
-    b.mass = (double)b.n * b.weight;
-#pragma unroll
-    for (int d = 1; d < SLICE; d <<= 1) {
-      const unsigned c = __shfl_up(b.count, d);
-      const double m = __shfl_up(b.mass, d);
-      if (lane >= d) {
-        b.count += c;
-        b.mass += m;
-      }
-    }
-    b.count += s.before_count;
-    b.mass += s.before_mass;
-    return b;
+    if (lane >= RUN) v.n = 0;
+    v.weight = weight(v.bits);
+    v.before = entry ? s.mass[entry - 1] : 0.0;
+    v.mass = v.before + sums_of((double)v.n * v.weight);
+    v.count = (entry ? s.count[entry - 1] : 0) + sums_of(v.n);
+    return v;
   }
 
-  // The first slice with tokens that `is` says yes to, by the sums up to its end; -1: none.  Leaves the sums in front of it in the scratch.
+  // The first run whose sums `is` says yes to; -1: none.
   template <typename Is>
-  __device__ __forceinline__ int slice_where(Is is) {
-    int first = BINS;
-#pragma unroll
-    for (int q = 0; q < ROUNDS; ++q)
-      if (first == BINS && count[q] != count_before[q] && is(q)) first = q * THREADS + tid;
-    __syncthreads();                                              // (what is there has been read)
-    if (tid == 0) s.slice = BINS;
-    __syncthreads();
-    const int of_wave = (int)wave_min_u32((unsigned)first);
-    if (lane == 0 && of_wave < BINS) atomicMin(&s.slice, of_wave);
-    __syncthreads();
-    const int slice = s.slice;
-    if (slice == BINS) return -1;
-#pragma unroll
-    for (int q = 0; q < ROUNDS; ++q)
-      if (q * THREADS + tid == slice) {
-        s.before_count = count_before[q];
-        s.before_mass = mass_before[q];
-      }
-    __syncthreads();
-    return slice;
+  __device__ __forceinline__ int entry_where(Is is) const {
+    constexpr int EACH = PADDED / 64;
+    const unsigned long long coarse = __ballot(is(s.count[lane * EACH + EACH - 1], s.mass[lane * EACH + EACH - 1]));
+    if (!coarse) return -1;
+    const int from = __builtin_ctzll(coarse) * EACH, at = from + (lane & (EACH - 1));
+    // (sums that rounding leaves in no order: the last one has been seen)
+    const unsigned long long fine = __ballot(is(s.count[at], s.mass[at]));
+    return from + __builtin_ctzll(fine);
   }
 
-  // What the tokens in front of a border weigh.
-  __device__ __forceinline__ double mass_until(Border e) {
-    if (e.bin > LAST) return total_mass;
-    const int slice = e.bin / SLICE;
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < ROUNDS; ++q)
-      if (q * THREADS + tid == slice) {
-        s.before_count = count_before[q];
-        s.before_mass = mass_before[q];
-      }
-    __syncthreads();
-    const Bin b = bin_of(slice);
-    const int at = e.bin % SLICE;
-    return in_front(b, at) + (double)e.n * __shfl(b.weight, at);
+  __device__ __forceinline__ Border end() const { return Border{{PADDED, 0}, 0, s.mass[PADDED - 1]}; }
+  // A border in front of the n-th token of value i.
+  __device__ __forceinline__ Border border_at(int entry, const Value &v, int i, int n) const {
+    return Border{{entry, i}, n, (i ? of_lane(v.mass, i - 1) : v.before) + (double)n * of_lane(v.weight, i)};
   }
-  __device__ __forceinline__ double in_front(const Bin &b, int at) const { return at ? __shfl(b.mass, at - 1) : s.before_mass; }
-
-  // Behind the k-th token.
+  // Behind the k-th token (of more).
   __device__ __forceinline__ Border kth(unsigned k) {
-    const int slice = slice_where([&](int q) { return count[q] >= k; });
-    if (slice < 0) return Border{BINS, 0};
-    const Bin b = bin_of(slice);
-    const int at = __builtin_ctzll(__ballot(lane < SLICE && b.n && b.count >= k) | 1ull << 63) & (SLICE - 1);
-    return Border{slice * SLICE + at, (int)(k - (__shfl(b.count, at) - __shfl(b.n, at)))};
+    const int entry = entry_where([&](unsigned c, double) { return c >= k; });
+    const Value v = values_of(entry);
+    const int i = __builtin_ctzll(__ballot(v.n && v.count >= k) | 1ull << 63) & (RUN - 1);
+    return border_at(entry, v, i, (int)(k - (of_lane(v.count, i) - of_lane(v.n, i))));
   }
-  // The token whose weight takes the sum to `target` (BEYOND: past it): the tokens in front of it.  The last one where rounding keeps all sums below.
-  template <bool BEYOND>
+  // In front of the token whose weight takes the sum past `target`; BEHIND: behind the one that takes it there.
+  template <bool BEHIND>
   __device__ __forceinline__ Border token_at(double target) {
-    auto reaches = [&](double m) { return BEYOND ? m > target : m >= target; };
-    int slice = slice_where([&](int q) { return reaches(mass[q]); });
-    if (slice < 0) slice = slice_where([&](int q) { return count[q] == total_count; });
-    const Bin b = bin_of(slice);
-    const unsigned long long some = __ballot(lane < SLICE && b.n), here = __ballot(lane < SLICE && b.n && reaches(b.mass));
-    const int at = here ? __builtin_ctzll(here) : 63 - __builtin_clzll(some);
-    const double w = __shfl(b.weight, at), ahead = (target - in_front(b, at)) / w;
-    // tokens of the bin whose sums stay in front: as many as whole weights fit, but for one that ends at the target where that is enough
-    double n = BEYOND ? floor(ahead) : ceil(ahead) - 1.0;
-    n = fmin(fmax(n, 0.0), (double)__shfl(b.n, at) - 1.0);
-    return Border{slice * SLICE + at, (int)n};
+    auto reaches = [&](double m) { return BEHIND ? m >= target : m > target; };
+    // (where rounding lets a run without tokens reach it: the next one; where it keeps all sums below: the last token)
+    int entry = entry_where([&](unsigned c, double m) { return c > 0 && reaches(m); });
+    const unsigned all = s.count[PADDED - 1];
+    if (entry >= 0) {
+      const unsigned up_to = s.count[entry];
+      if (up_to == (entry ? s.count[entry - 1] : 0)) entry = entry_where([&](unsigned c, double) { return c > up_to; });
+    }
+    if (entry < 0) entry = entry_where([&](unsigned c, double) { return c == all; });
+    const Value v = values_of(entry);
+    const unsigned long long some = __ballot(v.n != 0), here = __ballot(v.n != 0 && reaches(v.mass));
+    const int i = here ? __builtin_ctzll(here) : some ? 63 - __builtin_clzll(some) : 0;
+    const double before = i ? of_lane(v.mass, i - 1) : v.before, ahead = (target - before) / of_lane(v.weight, i);
+    // tokens of this value in front: as many as whole weights fit; behind: one that ends at the target is enough
+    const double n = fmin(fmax(BEHIND ? ceil(ahead) - 1.0 : floor(ahead), 0.0), (double)of_lane(v.n, i) - 1.0);
+    return border_at(entry, v, i, (int)n + BEHIND);
+  }
+  // In front of the first value that weighs less than min_p: about max + T log(min_p), and which of 64 there by their weights.
+  __device__ __forceinline__ Border below_min_p() {
+    const double x = top + log((double)r.min_p) / per;
+    if (!(x > -65504.0)) return end();
+    const int about = order_of(place_of(__half_as_ushort(__float2half_rn((float)x)))) - 32 + lane;
+    static_assert(RUN == 32, "");
+    const bool below = about >= 0 && (about >= ENTRIES * RUN || weight(bits_of(Place{about >> 5, about & (RUN - 1)})) < (double)r.min_p);
+    const unsigned long long b = __ballot(below);
+    const int first = about - lane + (b ? (int)__builtin_ctzll(b) : 64);
+    if (first >= ENTRIES * RUN) return end();
+    return border_at(first >> 5, values_of(first >> 5), first & (RUN - 1), 0);
   }
 
-  // The token among the row's (bin, how many equal ones stand in front of it) that is drawn, and its probability.
-  __device__ __forceinline__ Border drawn(float &probability) {
-    Border end{BINS, 0};
-    if (r.top_k > 0 && (unsigned)r.top_k < total_count) end = kth((unsigned)r.top_k);
+  // What top_k and top_p keep.
+  __device__ __forceinline__ Border kept() {
+    Border e = end();
+    if (r.top_k > 0 && (unsigned)r.top_k < s.count[PADDED - 1]) e = kth((unsigned)r.top_k);
     if (r.top_p < 1.f) {
-      Border p = token_at<false>((double)fmaxf(r.top_p, 0.f) * mass_until(end));
-      ++p.n;
-      end = nearer(end, p);
+      const Border p = token_at<true>((double)fmaxf(r.top_p, 0.f) * e.mass);
+      if (in_front(p, e)) e = p;
     }
-    if (s.below < BINS) end = nearer(end, Border{s.below, 0});
-    const double all = mass_until(end);
-    Border t = token_at<true>((double)r.uniform * all);
-    if (!(t.bin < end.bin || (t.bin == end.bin && t.n < end.n))) {
-      // (rounding: the last one in front of the border)
-      t = end.n > 0 ? Border{end.bin, end.n - 1} : t;
-    }
-    probability = (float)(weight(t.bin) / all);
+    return e;
+  }
+  // The token among the row's in front of a border, by the value's order and how many equal ones stand in front of it, and its probability.
+  __device__ __forceinline__ Border drawn(Border e, float &probability) {
+    const Border t = token_at<false>((double)r.uniform * e.mass);
+    probability = (float)(weight(bits_of(t.at)) / e.mass);
     return t;
   }
 };
 
+// Infinite logits, n of them: of equal weight, and nothing else has any.
+__device__ __forceinline__ Border infinite_of(const Row &r, unsigned n, float &probability) {
+  if (r.top_k > 0) n = min(n, (unsigned)r.top_k);
+  if (r.top_p < 1.f) n = max((unsigned)ceil((double)fmaxf(r.top_p, 0.f) * (double)n), 1u);
+  probability = (float)(1.0 / (double)n);
+  return Border{{0, 0}, (int)((double)r.uniform * (double)n), 0.0};
+}
+
+// HELD: vectors of eight numbers that a lane keeps (all of its row's), or 0: the row is read again at the end.
+template <int HELD>
 __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
-  extern __shared__ __attribute__((aligned(16))) unsigned bins[];
-  Scratch &s = *reinterpret_cast<Scratch *>(bins + BINS / 2);
-  const int row = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  extern __shared__ __attribute__((aligned(16))) unsigned words[];
+  Scratch &s = *reinterpret_cast<Scratch *>(words + WORDS);
+  const int row = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Row r;
   r.logits = p.logits + row * p.ld;
   r.vocabulary = p.vocabulary;
@@ -401,104 +509,187 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
   r.uniform = fminf(fmaxf(p.uniform[row], 0.f), 0x1.fffffep-1f);
   if (!(r.top_p < 1.f)) r.top_p = 1.f;                              // (NaN too)
   r.min_p = r.min_p > 0.f ? fminf(r.min_p, 1.f) : 0.f;
-  if (tid == 0) {
-    s.top = BINS;
-    s.below = BINS;
-    s.valid = 0;
-  }
-  Border at{BINS, 0};
-  float probability = 0.f;
+  Drawer<false> d{r, words, s, tid, lane, wave};
+  half2v largest;
+  Held<HELD> held;
+  unsigned valid = d.count(false, largest, held);
+  float top;
   const bool hot = r.temperature > 0.f;
-  Drawer<false> d{r, bins, s, tid, lane, wave};
-  d.per = hot ? 1.0 / (double)r.temperature : 0.0;
-  const unsigned valid = d.count_bins(0);
-  if (p.vocabulary > 65535) {
-    unsigned all = valid;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) all += __shfl_xor(all, x);
-    if (lane == 0) atomicAdd(&s.valid, (int)all);
-  }
-  d.sum_slices<0, ROUNDS>();
-  d.scan();
-  if (p.vocabulary > 65535 && d.total_count != (unsigned)s.valid) {
-    // a bin has overflowed: once more, half of the bins after the other
-    __syncthreads();
+  d.per = 1.0 / (double)r.temperature;
+  if (hot) d.make_powers();
+  d.tell(valid, largest, valid, top);
+  if (valid == 0) {
     if (tid == 0) {
-      s.top = BINS;
-      s.below = BINS;
+      p.tokens[row] = -1;
+      if (p.probabilities) p.probabilities[row] = 0.f;
     }
-    Drawer<true> e{r, bins, s, tid, lane, wave};
-    e.per = d.per;
-    e.count_bins(0);
-    e.sum_slices<0, ROUNDS / 2>();
-    __syncthreads();
-    e.count_bins(BINS / 2);
-    e.sum_slices<ROUNDS / 2, ROUNDS>();
-    e.scan();
-    if (e.total_count) {
-      at = Border{s.top, 0};
-      probability = 1.f;
-      if (hot) at = e.drawn(probability);
-    }
-  } else if (d.total_count) {
-    at = Border{s.top, 0};
-    probability = 1.f;
-    if (hot) at = d.drawn(probability);
+    return;
   }
-
-  // where the value's at.n-th occurrence (from zero) is: the wave in whose range it is, the step of that range, the token
-  int token = -1;
-  if (at.bin < BINS) {
-    int first = 0, vectors = (p.vocabulary + 7) / 8, left = at.n;
-    for (;;) {
-      const Walk w = walk_of(first, vectors, wave);
-      unsigned n = 0;
-      walk<8>(r, w, lane, [&](uint4v b, int) {
-        const unsigned x[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) n += ((x[j] & 0xffff) == (unsigned)at.bin) + ((x[j] >> 16) == (unsigned)at.bin);
-      });
-      unsigned up_to = n;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const unsigned x = __shfl_up(up_to, d);
-        if (lane >= d) up_to += x;
+  unsigned bits = __half_as_ushort(__float2half_rn(top));
+  int nth = 0;
+  float probability = 1.f;
+  if (hot) {
+    d.top = (double)top;
+    const bool infinite = bits == INF;
+    bool overflown = false;
+    if (!infinite) {
+      d.sum_runs(false);
+      d.scan();
+      overflown = s.count[PADDED - 1] != valid;
+    } else if (r.vocabulary > 65535) {
+      overflown = true;                                             // (how many infinite ones: by wide counts)
+    }
+    if (overflown) {
+      Drawer<true> e{r, words, s, tid, lane, wave, d.top, d.per};
+      half2v unused;
+      Held<0> none;
+      __syncthreads();
+      e.count(false, unused, none);
+      __syncthreads();
+      if (infinite) {
+        nth = infinite_of(r, words[INF], probability).n;
+      } else {
+        e.sum_runs(false);
+        __syncthreads();
+        e.count(true, unused, none);
+        __syncthreads();
+        e.sum_runs(true);
+        e.scan();
+        Border kept = e.kept();
+        if (r.min_p > 0.f) {
+          const Border m = e.below_min_p();
+          if (in_front(m, kept)) kept = m;
+        }
+        const Border t = e.drawn(kept, probability);
+        bits = bits_of(t.at);
+        nth = t.n;
+      }
+    } else {
+      // (one wave: it needs nothing of the others, which would be in its way, but for the border of min_p, which depends on none of its own)
+      Border e;
+      if (!infinite) {
+        if (wave == 1 && r.min_p > 0.f) {
+          const Border m = d.below_min_p();
+          if (lane == 0) {
+            s.below_entry = m.at.entry;
+            s.below_i = m.at.i;
+            s.below_mass = m.mass;
+          }
+        }
+        if (wave == 0) e = d.kept();
+        if (r.min_p > 0.f) __syncthreads();
+      }
+      if (wave == 0) {
+        if (r.min_p > 0.f && !infinite) {
+          const Border m{{s.below_entry, s.below_i}, 0, s.below_mass};
+          if (in_front(m, e)) e = m;
+        }
+        const Border t = infinite ? infinite_of(r, words[INF] & 0xffff, probability) : d.drawn(e, probability);
+        if (lane == 0) {
+          s.bits = infinite ? INF : (int)bits_of(t.at);
+          s.nth = t.n;
+          s.probability = probability;
+        }
       }
       __syncthreads();
-      if (lane == 63) s.found[wave] = (int)up_to;
-      __syncthreads();
-      int of = 0, before = 0;
-      while (of < WAVES - 1 && before + s.found[of] <= left) before += s.found[of++];
-      left -= before;
-      if (vectors <= WAVES * 64) {                                  // one vector to a lane: wave `of`'s lane with the token knows it
-        if (wave == of && (int)up_to > left && (int)(up_to - n) <= left) {
-          int skip = left - (int)(up_to - n);
-          const uint4v x = load8(r, w.begin + lane);
-          const unsigned b[4] = {bins_of(x.x), bins_of(x.y), bins_of(x.z), bins_of(x.w)};
+      bits = (unsigned)s.bits;
+      nth = s.nth;
+      probability = s.probability;
+    }
+  }
+
+  // Where the number's nth occurrence (from zero) is.  A half of zero bits in what `differs` leaves is the number.
+  const unsigned zeros = (bits & 0x7FFFu) == 0 ? 0x7FFF7FFFu : 0xFFFFFFFFu, both = (bits | bits << 16) & zeros;
+  auto differs = [&](uint4v x) { return (x & zeros) ^ both; };
+  auto matches = [&](uint4v x) {
+    typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+    const uint4v d = differs(x);
+    auto smaller = [](unsigned a, unsigned b) {
+      return __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
+    };
+    const unsigned least = smaller(smaller(d.x, d.y), smaller(d.z, d.w));
+    unsigned n = 0;
+    if (!(least & 0xffff) || !(least >> 16)) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if ((j & 1 ? b[j / 2] >> 16 : b[j / 2] & 0xffff) == (unsigned)at.bin && skip-- == 0) token = (w.begin + lane) * 8 + j;
-        }
-        break;
+      for (int j = 0; j < 8; ++j) n += half_at(d, j) == 0;
+    }
+    return n;
+  };
+  auto write = [&](uint4v x, int skip, int vector) {                // the lane whose vector it is
+    const uint4v d = differs(x);
+    int token = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (half_at(d, j) == 0 && skip-- == 0) token = vector * 8 + j;
+    p.tokens[row] = token;
+    if (p.probabilities) p.probabilities[row] = probability;
+  };
+  // Numbers of matches of the waves, of which the one with the nth is found; nth: what is left of it there.
+  auto wave_with_nth = [&](unsigned n_of_wave) {
+    __syncthreads();
+    if (lane == 0) s.found[wave] = (int)n_of_wave;
+    __syncthreads();
+    int of = 0;
+    while (of < WAVES - 1 && s.found[of] <= nth) nth -= s.found[of++];
+    return of;
+  };
+  const uint4v tail = tail_of(r, tid);                              // (again: it would take four registers all the way)
+  int first = 0, vectors = p.vocabulary / 8;
+  if constexpr (HELD > 0) {
+    const Walk w = walk_of(first, vectors, wave);
+    unsigned n = 0;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u)
+      if (w.begin + u * 64 + lane < w.end) n += matches(held.x[u]);
+    n += matches(tail);
+    if (wave != wave_with_nth(of_lane(sums_of(n), 63))) return;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      if (w.begin + u * 64 >= w.end) break;
+      const unsigned here = w.begin + u * 64 + lane < w.end ? matches(held.x[u]) : 0;
+      if (!__ballot(here != 0)) continue;
+      const unsigned up_to = sums_of(here);
+      if ((int)up_to > nth && (int)(up_to - here) <= nth) write(held.x[u], nth - (int)(up_to - here), w.begin + u * 64 + lane);
+      nth -= (int)of_lane(up_to, 63);
+      if (nth < 0) return;
+    }
+    if (tid == THREADS - 1) write(tail, nth, p.vocabulary / 8);
+  } else {
+    // the wave in whose part of the row it is, the part of that, the lane
+    const int of_tail = (int)of_lane(matches(tail), 63);             // (of the last wave's last lane)
+    for (bool whole = true;; whole = false) {
+      const Walk w = walk_of(first, vectors, wave);
+      unsigned n = 0;
+      uint4v mine{};
+      walk<8>(r, w, lane, [&](uint4v x) {
+        mine = x;
+        n += matches(x);
+      });
+      const unsigned up_to = sums_of(n);
+      if (whole && wave == WAVES - 1 && lane == 0) s.of_tail = of_tail;
+      const int of = wave_with_nth(of_lane(up_to, 63) + (whole ? of_tail : 0));
+      if (whole && of == WAVES - 1 && nth >= s.found[of] - s.of_tail) {      // behind the whole vectors
+        if (tid == THREADS - 1) write(tail, nth - (s.found[of] - s.of_tail), p.vocabulary / 8);
+        return;
+      }
+      if (vectors <= WAVES * 64) {                                  // one vector to a lane
+        if (wave == of && (int)up_to > nth && (int)(up_to - n) <= nth) write(mine, nth - (int)(up_to - n), w.begin + lane);
+        return;
       }
       const Walk there = walk_of(first, vectors, of);
       first = there.begin;
       vectors = there.end - there.begin;
     }
-    if (token >= 0) {
-      p.tokens[row] = token;
-      if (p.probabilities) p.probabilities[row] = probability;
-    }
-  } else if (tid == 0) {
-    p.tokens[row] = -1;
-    if (p.probabilities) p.probabilities[row] = 0.f;
   }
 }
 
 }  // namespace
 
 int launch_sample(const SampleParams &p, int rows, hipStream_t s) {
-  VQ_ALLOW_FULL_LDS(sample_kernel);
+  constexpr int HELD = 16;
+  const bool held = p.vocabulary <= HELD * 8 * THREADS;
+  VQ_ALLOW_FULL_LDS(sample_kernel<HELD>);
+  VQ_ALLOW_FULL_LDS(sample_kernel<0>);
   constexpr int MOST = 1 << 21;                                     // rows of a launch (a grid has fewer than 2^32 threads)
   for (int row0 = 0; row0 < rows; row0 += MOST) {
     SampleParams q = p;
@@ -510,7 +701,7 @@ int launch_sample(const SampleParams &p, int rows, hipStream_t s) {
     if (q.min_ps) q.min_ps += row0;
     q.tokens += row0;
     if (q.probabilities) q.probabilities += row0;
-    hipLaunchKernelGGL(sample_kernel, dim3(rows - row0 < MOST ? rows - row0 : MOST), dim3(THREADS), BINS * 2 + sizeof(Scratch), s, q);
+    hipLaunchKernelGGL(held ? sample_kernel<HELD> : sample_kernel<0>, dim3(rows - row0 < MOST ? rows - row0 : MOST), dim3(THREADS), WORDS * 4 + sizeof(Scratch), s, q);
     if (rows - row0 <= MOST) break;
   }
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
