@@ -68,10 +68,10 @@ struct Scratch {
   double mass[PADDED];
   unsigned count[PADDED];
   double wave_mass[WAVES];
-  double powers[OCTAVES][RUN / 4];    // by the power of two of a run's sizes: (the factor from a number's weight to the next one's)^(4 i)
+  double powers[OCTAVES][RUN / 4], factors[OCTAVES];      // by the power of two of a run's sizes: the factor from a number's weight to the next one's, and its (4 i)-th power
   double below_mass;
   int below_entry, below_i;
-  unsigned wave_count[WAVES], wave_valid[WAVES], wave_top[WAVES], counts[RUN];
+  unsigned wave_count[WAVES], wave_valid[WAVES], wave_top[WAVES], wave_size[WAVES], counts[RUN];
   int found[WAVES], of_tail, bits, nth;
   float probability;
 };
@@ -86,17 +86,18 @@ __device__ __forceinline__ Walk walk_of(int first, int vectors, int wave) {
 }
 constexpr unsigned NONE = 0xFC00FC00u;                              // two minus infinities
 __device__ __forceinline__ uint4v load8(const Row &r, int vector) { return *reinterpret_cast<const uint4b *>(r.logits + (long long)vector * 8); }
-// What is left of a row behind its whole vectors, in the last thread of the workgroup; minus infinities in the others.
-__device__ __forceinline__ uint4v tail_of(const Row &r, int tid) {
-  uint4v x = {NONE, NONE, NONE, NONE};
-  const int from = r.vocabulary & ~7, n = r.vocabulary & 7;
-  if (n && tid == THREADS - 1) {
-    unsigned h[8];
+// A row's last eight numbers, of which those behind the whole vectors count, in the workgroup's last thread: the others, and those of other threads, are minus infinities.
+__device__ __forceinline__ uint4v last8(const Row &r) {
+  if (r.vocabulary >= 8) return *reinterpret_cast<const uint4b *>(r.logits + r.vocabulary - 8);
+  unsigned h[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = j < n ? __half_as_ushort(r.logits[from + j]) : 0xFC00u;
-    x = uint4v{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
-  }
-  return x;
+  for (int j = 0; j < 8; ++j) h[j] = j >= 8 - r.vocabulary ? __half_as_ushort(r.logits[r.vocabulary - 8 + j]) : 0xFC00u;
+  return uint4v{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+}
+__device__ __forceinline__ uint4v tail_of(const Row &r, uint4v last, int tid) {
+  const int from = tid == THREADS - 1 ? 8 - (r.vocabulary & 7) : 8;
+  auto two = [&](unsigned w, int j) { return (j >= from ? w & 0xffff : 0xFC00u) | (j + 1 >= from ? w & 0xffff0000u : 0xFC000000u); };
+  return uint4v{two(last.x, 0), two(last.y, 2), two(last.z, 4), two(last.w, 6)};
 }
 // The first HELD of a lane's vectors stay in registers.
 template <int HELD>
@@ -169,6 +170,7 @@ struct Drawer {
   Scratch &s;
   int tid, lane, wave;
   double top, per;                 // the largest logit; one over the temperature
+  unsigned largest_size;           // of the finite logits
 
   // (1 for numbers above the largest, of which there are none)
   __device__ __forceinline__ double weight(unsigned bits) const { return exp_of(fmin(((double)number_of(bits) - top) * per, 0.0)); }
@@ -177,17 +179,19 @@ struct Drawer {
   template <int HELD>
   __device__ __forceinline__ unsigned count(bool negative, half2v &largest, Held<HELD> &held) {
     const Walk of_wave = walk_of(0, r.vocabulary / 8, wave);
+    const uint4v last = last8(r);
     if constexpr (HELD > 0) {
+      // (all of them, the last one in place of those behind it: of conditional loads the compiler would wait for all in front of the first use)
+      if (r.vocabulary >= 8) {
 #pragma unroll
-      for (int u = 0; u < HELD; ++u)
-        if (of_wave.begin + u * 64 < of_wave.end) held.x[u] = load8(r, min(of_wave.begin + u * 64 + lane, of_wave.end - 1));
+        for (int u = 0; u < HELD; ++u) held.x[u] = load8(r, min(of_wave.begin + u * 64 + lane, r.vocabulary / 8 - 1));
+      }
     }
-    const uint4v tail = tail_of(r, tid);
     uint4v *all = reinterpret_cast<uint4v *>(words);
     for (int i = tid; i < WORDS / 4; i += THREADS) all[i] = uint4v{0, 0, 0, 0};
     __syncthreads();
     const unsigned base = (unsigned)(size_t)(Lds)words;
-    unsigned valid = 0;
+    unsigned valid = 0, largest_sizes = 0;
     largest = half2v{(_Float16)-__builtin_inff(), (_Float16)-__builtin_inff()};
     auto one = [&](uint4v x) {
       const uint4v size = x & 0x7FFF7FFFu;
@@ -195,7 +199,8 @@ struct Drawer {
         typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
         return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
       };
-      const bool odd = ((larger(larger(size.x, size.y), larger(size.z, size.w)) + 0x04000400u) & 0x80008000u) != 0, alike = x.x == x.y && x.x == x.z && x.x == x.w;
+      const unsigned sizes = larger(larger(size.x, size.y), larger(size.z, size.w));
+      const bool odd = ((sizes + 0x04000400u) & 0x80008000u) != 0, alike = x.x == x.y && x.x == x.z && x.x == x.w;
       largest = __builtin_elementwise_max(largest, __builtin_elementwise_max(__builtin_elementwise_max(half2_of(x.x), half2_of(x.y)), __builtin_elementwise_max(half2_of(x.z), half2_of(x.w))));
       if (WIDE || odd || alike) {
         // what is not counted, and eight times the same, as masks leave it: one addition, where 64 lanes that add one to the same word take 64 turns
@@ -207,12 +212,14 @@ struct Drawer {
           const bool minus = bits >= 0x8000u && m;
           if (m > INF || (m == INF && minus) || (same && j)) continue;
           valid += n;
+          if (m < INF) largest_sizes = larger(largest_sizes, m);
           if (!WIDE) add(base + m * 4, bits & 0x8000u ? n << 16 : n);
           else if (minus == negative) add(base + m * 4, n);
         }
         return;
       }
       valid += 8;
+      largest_sizes = larger(largest_sizes, sizes);
       const uint4v sign = (x >> 15) & 0x00010001u;
       auto two = [&](unsigned m, unsigned minus) {
         add(of_half<false>(m, 4, base), of_half<false>(minus, 0xFFFF, 1));
@@ -227,34 +234,46 @@ struct Drawer {
     } else {
       walk<WIDE ? 2 : 8>(r, of_wave, lane, one);
     }
-    one(tail);
+    if ((r.vocabulary & 7) && tid == THREADS - 1) one(tail_of(r, last, tid));
+    largest_size = max(largest_sizes & 0xffff, largest_sizes >> 16);
     return valid;
   }
   // The sum of all threads' `valid` and the largest number, for all of them.
   __device__ __forceinline__ void tell(unsigned valid, half2v largest, unsigned &valid_of_all, float &top_of_all) {
     float x = fmaxf((float)largest.x, (float)largest.y);
     valid = sums_of(valid);
+    unsigned size = largest_size;
+#define VQ_LARGER(CTRL, ROWS) size = max(size, (unsigned)__builtin_amdgcn_update_dpp((int)size, (int)size, CTRL, ROWS, 0xF, false))
+    VQ_LARGER(0x111, 0xF); VQ_LARGER(0x112, 0xF); VQ_LARGER(0x114, 0xF); VQ_LARGER(0x118, 0xF); VQ_LARGER(0x142, 0xA); VQ_LARGER(0x143, 0xC);
+#undef VQ_LARGER
 #define VQ_LARGER(CTRL, ROWS) x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false)))
     VQ_LARGER(0x111, 0xF); VQ_LARGER(0x112, 0xF); VQ_LARGER(0x114, 0xF); VQ_LARGER(0x118, 0xF); VQ_LARGER(0x142, 0xA); VQ_LARGER(0x143, 0xC);
 #undef VQ_LARGER
     if (lane == 63) {
       s.wave_valid[wave] = valid;
       s.wave_top[wave] = __float_as_uint(x);
+      s.wave_size[wave] = size;
     }
     __syncthreads();
-    valid_of_all = 0;
+    valid_of_all = largest_size = 0;
     top_of_all = -__builtin_inff();
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       valid_of_all += s.wave_valid[w];
       top_of_all = fmaxf(top_of_all, __uint_as_float(s.wave_top[w]));
+      largest_size = max(largest_size, s.wave_size[w]);
     }
   }
 
   // How far numbers of a power of two are apart.
   __device__ __forceinline__ static double distance(int octave) { return (double)number_of((unsigned)octave * 1024 + 1) - (double)number_of((unsigned)octave * 1024); }
   __device__ __forceinline__ void make_powers() {
-    if (tid < OCTAVES * (RUN / 4)) s.powers[tid / (RUN / 4)][tid % (RUN / 4)] = exp_of(-distance(tid / (RUN / 4)) * per * (double)(tid % (RUN / 4) * 4));
+    constexpr int EACH = RUN / 4 + 1;
+    if (tid >= OCTAVES * EACH) return;
+    const int octave = tid / EACH, i = tid % EACH;
+    const double f = exp_of(-distance(octave) * per * (double)(i < EACH - 1 ? 4 * i : 1));
+    if (i < EACH - 1) s.powers[octave][i] = f;
+    else s.factors[octave] = f;
   }
   // Counts and weights of the runs of both signs (WIDE: of one), of a thread's 32 sizes, to the scratch.
   __device__ __forceinline__ void sum_runs(bool negative) {
@@ -263,6 +282,11 @@ struct Drawer {
       s.count[ENTRIES + tid] = 0;
     }
     if (tid >= RUNS) return;
+    if ((unsigned)tid * RUN > largest_size) {                       // (the same for both signs of WIDE: nothing is lost)
+      s.mass[RUNS - 1 - tid] = s.mass[RUNS + tid] = 0.0;
+      s.count[RUNS - 1 - tid] = s.count[RUNS + tid] = 0;
+      return;
+    }
     const uint4v *from = reinterpret_cast<const uint4v *>(words) + tid * (RUN / 4);
     // A run's powers of q begin at its largest number, that of largest size of the positive and of smallest size of the negative ones, and in the run of the row's largest number at
     // that one, whose weight is one without a rounding (of equal logits the sums are whole numbers then).  Lanes begin in different quarters of their runs, whose first words lie in the
@@ -271,7 +295,7 @@ struct Drawer {
     const bool has_top = top_size / RUN == (unsigned)tid, top_plus = has_top && (of_top < 0x8000u || !top_size), top_minus = has_top && !top_plus;
     const int from_plus = top_plus ? (int)(top_size % RUN) : RUN - 1, from_minus = top_minus ? (int)(top_size % RUN) : 0;
     const double(&powers)[RUN / 4] = s.powers[tid / (1024 / RUN)];
-    const double q = exp_of(-distance(tid / (1024 / RUN)) * per), q2 = q * q;
+    const double q = s.factors[tid / (1024 / RUN)], q2 = q * q;
     struct Four {
       unsigned a[4], b[4];
     };
@@ -540,7 +564,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
       overflown = true;                                             // (how many infinite ones: by wide counts)
     }
     if (overflown) {
-      Drawer<true> e{r, words, s, tid, lane, wave, d.top, d.per};
+      Drawer<true> e{r, words, s, tid, lane, wave, d.top, d.per, INF};
       half2v unused;
       Held<0> none;
       __syncthreads();
@@ -549,10 +573,12 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
       if (infinite) {
         nth = infinite_of(r, words[INF], probability).n;
       } else {
+        e.largest_size = d.largest_size;                            // (of all of the row)
         e.sum_runs(false);
         __syncthreads();
         e.count(true, unused, none);
         __syncthreads();
+        e.largest_size = d.largest_size;
         e.sum_runs(true);
         e.scan();
         Border kept = e.kept();
@@ -615,12 +641,12 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
     }
     return n;
   };
-  auto write = [&](uint4v x, int skip, int vector) {                // the lane whose vector it is
+  auto write = [&](uint4v x, int skip, int from) {                // the lane whose vector it is
     const uint4v d = differs(x);
     int token = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (half_at(d, j) == 0 && skip-- == 0) token = vector * 8 + j;
+      if (half_at(d, j) == 0 && skip-- == 0) token = from + j;
     p.tokens[row] = token;
     if (p.probabilities) p.probabilities[row] = probability;
   };
@@ -633,7 +659,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
     while (of < WAVES - 1 && s.found[of] <= nth) nth -= s.found[of++];
     return of;
   };
-  const uint4v tail = tail_of(r, tid);                              // (again: it would take four registers all the way)
+  const uint4v tail = tail_of(r, last8(r), tid);                              // (again: it would take four registers all the way)
   int first = 0, vectors = p.vocabulary / 8;
   if constexpr (HELD > 0) {
     const Walk w = walk_of(first, vectors, wave);
@@ -649,11 +675,11 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
       const unsigned here = w.begin + u * 64 + lane < w.end ? matches(held.x[u]) : 0;
       if (!__ballot(here != 0)) continue;
       const unsigned up_to = sums_of(here);
-      if ((int)up_to > nth && (int)(up_to - here) <= nth) write(held.x[u], nth - (int)(up_to - here), w.begin + u * 64 + lane);
+      if ((int)up_to > nth && (int)(up_to - here) <= nth) write(held.x[u], nth - (int)(up_to - here), (w.begin + u * 64 + lane) * 8);
       nth -= (int)of_lane(up_to, 63);
       if (nth < 0) return;
     }
-    if (tid == THREADS - 1) write(tail, nth, p.vocabulary / 8);
+    if (tid == THREADS - 1) write(tail, nth, p.vocabulary - 8);
   } else {
     // the wave in whose part of the row it is, the part of that, the lane
     const int of_tail = (int)of_lane(matches(tail), 63);             // (of the last wave's last lane)
@@ -669,11 +695,11 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
       if (whole && wave == WAVES - 1 && lane == 0) s.of_tail = of_tail;
       const int of = wave_with_nth(of_lane(up_to, 63) + (whole ? of_tail : 0));
       if (whole && of == WAVES - 1 && nth >= s.found[of] - s.of_tail) {      // behind the whole vectors
-        if (tid == THREADS - 1) write(tail, nth - (s.found[of] - s.of_tail), p.vocabulary / 8);
+        if (tid == THREADS - 1) write(tail, nth - (s.found[of] - s.of_tail), p.vocabulary - 8);
         return;
       }
       if (vectors <= WAVES * 64) {                                  // one vector to a lane
-        if (wave == of && (int)up_to > nth && (int)(up_to - n) <= nth) write(mine, nth - (int)(up_to - n), w.begin + lane);
+        if (wave == of && (int)up_to > nth && (int)(up_to - n) <= nth) write(mine, nth - (int)(up_to - n), (w.begin + lane) * 8);
         return;
       }
       const Walk there = walk_of(first, vectors, of);
@@ -686,10 +712,12 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
 }  // namespace
 
 int launch_sample(const SampleParams &p, int rows, hipStream_t s) {
-  constexpr int HELD = 16;
-  const bool held = p.vocabulary <= HELD * 8 * THREADS;
-  VQ_ALLOW_FULL_LDS(sample_kernel<HELD>);
+  // As many registers as the row needs, for rows that fit them.
+  VQ_ALLOW_FULL_LDS(sample_kernel<4>);
+  VQ_ALLOW_FULL_LDS(sample_kernel<16>);
   VQ_ALLOW_FULL_LDS(sample_kernel<0>);
+  constexpr int EACH = 8 * THREADS;
+  auto kernel = p.vocabulary <= 4 * EACH ? sample_kernel<4> : p.vocabulary <= 16 * EACH ? sample_kernel<16> : sample_kernel<0>;
   constexpr int MOST = 1 << 21;                                     // rows of a launch (a grid has fewer than 2^32 threads)
   for (int row0 = 0; row0 < rows; row0 += MOST) {
     SampleParams q = p;
@@ -701,7 +729,7 @@ int launch_sample(const SampleParams &p, int rows, hipStream_t s) {
     if (q.min_ps) q.min_ps += row0;
     q.tokens += row0;
     if (q.probabilities) q.probabilities += row0;
-    hipLaunchKernelGGL(held ? sample_kernel<HELD> : sample_kernel<0>, dim3(rows - row0 < MOST ? rows - row0 : MOST), dim3(THREADS), WORDS * 4 + sizeof(Scratch), s, q);
+    hipLaunchKernelGGL(kernel, dim3(rows - row0 < MOST ? rows - row0 : MOST), dim3(THREADS), WORDS * 4 + sizeof(Scratch), s, q);
     if (rows - row0 <= MOST) break;
   }
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;
