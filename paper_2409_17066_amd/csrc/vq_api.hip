@@ -42,7 +42,9 @@ void read_switches() {
       else if (n == 4 && !strncmp(e, "rows", 4)) sw.rows = v == '0' ? 0 : v == '1' ? 1 : -1;
       else if (n == 8 && !strncmp(e, "products", 8)) sw.products = v == '0' ? 0 : v == '1' ? 1 : -1;
       else if (n == 9 && !strncmp(e, "attention", 9)) sw.attention = v;
-      else if (n == 6 && !strncmp(e, "shared", 6)) sw.shared = v == '0' || v == '1' ? v : 0;
+      else if (n == 6 && !strncmp(e, "shared", 6)) sw.shared = v >= '0' && v <= '2' ? v : 0;
+      else if (n == 6 && !strncmp(e, "prefix", 6)) sw.prefix = v;
+      else if (n == 12 && !strncmp(e, "prefix_parts", 12)) sw.prefix_parts = v >= '0' && v <= '5' ? v - '0' : -1;
       else if (n == 5 && !strncmp(e, "parts", 5)) sw.parts = v >= '0' && v <= '6' ? v - '0' : -1;
       else if (n == 5 && !strncmp(e, "dense", 5)) sw.dense = v >= '0' && v <= '9' ? v - '0' : -1;
     }

@@ -31,8 +31,10 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
   const long long rows = (long long)c.max_new * a.group, slots = cu_count();
   float least = 0.f;
   parts_allowed = parts_allowed && attention_join_takes(c, a);
+  const int forced_parts = half == PREFIX && switches().prefix_parts >= 0 ? switches().prefix_parts : switches().parts;
+  const char forced_kernel = half == PREFIX && switches().prefix ? switches().prefix : switches().attention;
   for (const bool prompt : {false, true}) {
-    const char forced = attention_prompt_takes(c) ? switches().attention : 'd';
+    const char forced = attention_prompt_takes(c) ? forced_kernel : 'd';
     if (forced == 'd' || forced == 'p' ? prompt != (forced == 'p') : !prompt && rows > 512) continue;
     const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(c, a, half == PREFIX || c.max_new == 1), run = prompt ? PROMPT_RUN : attention_decode_run(c);
     // tokens that a tile's rows look at: a window's and the first ones, or on the average all before half of the new ones
@@ -41,7 +43,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
     const float quarters = (float)std::min((rows + 31) / 32, 4LL), size = (float)((c.head_dim + 63) / 64) / 2.f;
     const long long most = parts_allowed ? std::min((chunks + run - 1) / run, half == WHOLE ? 64LL : (long long)HALF_PARTS) : 1;
     for (long long parts = 1;; parts *= 2) {
-      if (switches().parts >= 0) parts = 1LL << switches().parts;
+      if (forced_parts >= 0) parts = 1LL << forced_parts;
       parts = std::min(parts, most);
       const float alone = (float)slots * (prompt ? 1.f : (float)run / (float)std::min(attention_decode_waves(c, (int)parts, (int)length), run));   // workgroups side by side
       const float most_at_once = prompt ? 2.f * alone : alone, work = (float)(groups * parts), rounds = prompt ? std::max(work / most_at_once, 1.f) : std::ceil(work / most_at_once);
@@ -58,7 +60,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
         best.prompt = prompt;
         best.time = time;
       }
-      if (parts == most || switches().parts >= 0) break;
+      if (parts == most || forced_parts >= 0) break;
     }
   }
   if (best.parts > 1 || half != WHOLE) {
@@ -70,30 +72,40 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
 
 Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) { return plan_of(c, a, parts_allowed, WHOLE, c.max_length); }
 
-// Attention behind shared prefixes: a launch for the prefixes, one for what lies behind, one that joins them.
+// Attention behind shared prefixes: the prefixes and what lies behind, in one launch or two, and one that joins them.
 struct SharedPlan {
   KvParams prefixes;             // as sequences
   Plan prefix, own;
-  bool shares;                   // or every sequence by itself, where that is estimated to be faster
+  bool shares, together;         // or every sequence by itself, where that is estimated to be faster; both halves in one launch
+  HalvesGrid grid;
   static size_t bytes(const Plan &half) { return (half.o_bytes + half.ml_bytes + 255) / 256 * 256; }
   size_t bytes() const { return bytes(prefix) + bytes(own); }
 };
 SharedPlan shared_plan_of(const KvParams &c, const Prefixes &x, const AttentionParams &a) {
   SharedPlan p{};
-  p.prefixes = c;
-  p.prefixes.n_seqs = x.n;
-  p.prefixes.max_new = x.rows_most;
-  p.prefixes.max_length = x.max_length;
-  p.prefixes.table_pages = x.table_pages;
-  p.prefixes.table_stride = x.table_stride;
-  p.prefixes.page_table = x.page_table;
-  p.prefixes.lengths = x.lengths;
+  p.prefixes = as_sequences(c, x);
   // (rows of a prefix: token_of()'s division and a grid's layers)
   if (!attention_join_takes(c, a) || x.max_length == 0 || (long long)x.rows_most * a.group * a.group >= 1ll << 30) return p;
   p.prefix = plan_of(p.prefixes, a, true, PREFIX, x.max_length);
   p.own = plan_of(c, a, true, OWN, std::min(x.max_own, c.max_length));
   const char forced = switches().shared;
-  p.shares = forced ? forced == '1' : p.prefix.time + p.own.time + 5.f < plan_of(c, a, true).time;
+  p.shares = forced ? forced != '0' : p.prefix.time + p.own.time + 5.f < plan_of(c, a, true).time;
+  p.together = (c.head_dim == 64 || c.head_dim == 128) && !p.own.prompt && forced != '2';
+  if (!p.together) return p;
+  const long long rows = (long long)x.rows_most * a.group, own_rows = (long long)c.max_new * a.group;
+  p.grid.prefix_tiles = (int)((rows + p.prefix.tile_rows - 1) / p.prefix.tile_rows);
+  p.grid.own_tiles = (int)((own_rows + p.own.tile_rows - 1) / p.own.tile_rows);
+  p.own.run = HALVES_WAVES;
+  if (!p.prefix.prompt) p.prefix.run = HALVES_WAVES;
+  const long long prefix_blocks = (long long)x.n * c.kv_heads * p.grid.prefix_tiles * p.prefix.parts, own_blocks = (long long)c.n_seqs * c.kv_heads * p.grid.own_tiles * p.own.parts;
+  if (prefix_blocks + own_blocks > 0x7fffffff / THREADS) {
+    p.together = false;
+    return p;
+  }
+  p.grid.prefix_blocks = (int)prefix_blocks;
+  p.grid.own_blocks = (int)own_blocks;
+  p.grid.first = std::min(p.grid.prefix_blocks, cu_count());
+  p.grid.zigzag = prefix_blocks <= 2 * cu_count();
   return p;
 }
 
@@ -114,9 +126,13 @@ int launch_attention_shared(const KvParams &c, const Prefixes &x, const Attentio
     return split;
   };
   const Split prefix = split_of(p.prefix), own = split_of(p.own);
+  if (p.together) {
+    const int rc = c.e4m3 ? launch_attention_halves<true>(c, a, own, prefix, x, p.grid, p.prefix.prompt, s) : launch_attention_halves<false>(c, a, own, prefix, x, p.grid, p.prefix.prompt, s);
+    return rc != VQ_OK ? rc : launch_attention_join_halves(c, a, own, p.own.tile_rows, prefix, x, s);
+  }
   int rc = p.prefix.prompt ? launch_attention_prompt(p.prefixes, a, prefix, x, PREFIX, s) : launch_attention_decode(p.prefixes, a, prefix, x, PREFIX, s);
   if (rc == VQ_OK) rc = p.own.prompt ? launch_attention_prompt(c, a, own, x, OWN, s) : launch_attention_decode(c, a, own, x, OWN, s);
-  return rc != VQ_OK ? rc : launch_attention_join_halves(c, a, own, p.own.tile_rows, p.prefixes, prefix, p.prefix.tile_rows, x, s);
+  return rc != VQ_OK ? rc : launch_attention_join_halves(c, a, own, p.own.tile_rows, prefix, x, s);
 }
 
 size_t attention_workspace_bytes(const KvParams &c, const AttentionParams &a) {

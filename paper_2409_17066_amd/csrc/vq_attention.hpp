@@ -26,6 +26,15 @@ struct Split {
 
 // Chunks of a run, one for each wave of the decode kernel.
 constexpr int DECODE_RUN = 8, PROMPT_RUN = 4;
+// Waves of a workgroup of the decode kernel, at most: as many as have room in LDS for what they join.
+constexpr int waves_of(bool e4m3, int dim) { return !e4m3 && dim > 192 ? DECODE_RUN / 2 : DECODE_RUN; }
+constexpr int odd_kinds(bool e4m3) { return e4m3 ? 1 : 3; }
+constexpr int decode_lds_bytes(bool e4m3, int dim, int rt, bool many, int waves) {
+  return (2 * 16 + 16 * (dim + 4) * (many ? rt : 1)) * waves * 4 + (many ? waves * odd_kinds(e4m3) * dim * 8 : 0);
+}
+// The prompt kernel: waves, threads and rows of a workgroup.
+constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = 32 * WAVES;
+constexpr int prompt_lds_bytes(bool e4m3, int dim) { return 2 * 2 * 64 * dim * 2 + 16 + 2 * odd_kinds(e4m3) * dim * 8 + (e4m3 ? 2 * (dim / 64) * WAVES * 4 : 0); }
 int attention_decode_run(const KvParams &c);                       // DECODE_RUN, or half of it
 int attention_decode_waves(const KvParams &c, int parts, int length);          // waves of a workgroup of the decode kernel, for sequences of up to `length` keys
 // The decode kernel, which takes every head: rows of a key head to a workgroup; `alike`: which see the same keys.
@@ -38,10 +47,33 @@ int attention_prompt_rows();
 bool attention_prompt_takes(const KvParams &c);
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, hipStream_t stream);
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, Half half, hipStream_t stream);
-// The launch that joins the parts of both halves (64 together at most), and of sequences without a prefix those of the second.
+// Attention behind shared prefixes (vq_attention_shared.hip).  Parts of either half, at most: a launch joins those of both.
 constexpr int HALF_PARTS = 32;
-int launch_attention_join_halves(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, const KvParams &cp, const Split &sp, int prefix_tile_rows,
-                                 const Prefixes &x, hipStream_t stream);
+// Both halves in one launch: a prefix of which either kernel takes tiles beside sequences of which the decode kernel does, of heads of 64 or 128 elements; whether it takes them, and
+// waves of a workgroup of the decode kernel.
+constexpr int HALVES_WAVES = THREADS / 64;
+struct HalvesGrid {
+  int prefix_blocks, own_blocks, first;      // workgroups; so many of the prefix's come in front of the others'
+  int prefix_tiles, own_tiles, zigzag;
+};
+int launch_attention_join_halves(const KvParams &c, const AttentionParams &a, const Split &own, int own_tile_rows, const Split &prefix, const Prefixes &x, hipStream_t stream);
+template <bool E4M3>
+int launch_attention_halves(const KvParams &c, const AttentionParams &a, const Split &own, const Split &prefix, const Prefixes &x, const HalvesGrid &g, bool prompt, hipStream_t stream);
+// The prefixes as sequences.
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline KvParams as_sequences(KvParams c, const Prefixes &x) {
+  c.n_seqs = x.n;
+  c.max_new = x.rows_most;
+  c.max_length = x.max_length;
+  c.table_pages = x.table_pages;
+  c.table_stride = x.table_stride;
+  c.page_table = x.page_table;
+  c.lengths = x.lengths;
+  return c;
+}
+
 // The launch that joins parts: whether a grid can have so many rows and sequences.
 bool attention_join_takes(const KvParams &c, const AttentionParams &a);
 int launch_attention_join(const KvParams &c, const AttentionParams &a, const Split &s, int tile_rows, hipStream_t stream);
@@ -187,7 +219,7 @@ __device__ __forceinline__ float where_seen(unsigned seen, int r, float x) {
 // out of the operands (Odd::clean) and come back as a sum that is not finite for the rows that see them: bits of 64 keys for each element and kind.
 template <bool E4M3>
 struct Odd {
-  static constexpr int KINDS = E4M3 ? 1 : 3, KEYS = E4M3 ? 16 : 8;           // NaN, and in 16 bits both infinities; keys of a 16-byte word
+  static constexpr int KINDS = odd_kinds(E4M3), KEYS = E4M3 ? 16 : 8;           // NaN, and in 16 bits both infinities; keys of a 16-byte word
   static __device__ __forceinline__ bool any(uint4v w) {
     const unsigned exponent = E4M3 ? 0x7f7f7f7fu : 0x7c007c00u, one = E4M3 ? 0x01010101u : 0x04000400u, carry = E4M3 ? 0x80808080u : 0x80008000u;
     return ((((w.x & exponent) + one) | ((w.y & exponent) + one) | ((w.z & exponent) + one) | ((w.w & exponent) + one)) & carry) != 0;
@@ -234,6 +266,26 @@ template <Half HALF = WHOLE>
 __device__ __forceinline__ unsigned long long seen64_of(const AttentionParams &a, const Sequence &s, int place, int base) {
   return (unsigned long long)(seen_of<HALF>(a, s, place, base) | seen_of<HALF>(a, s, place, base + 16) << 16) |
          (unsigned long long)(seen_of<HALF>(a, s, place, base + 32) | seen_of<HALF>(a, s, place, base + 48) << 16) << 32;
+}
+
+typedef float float16v __attribute__((ext_vector_type(16)));
+struct Sixteen {
+  float f[16];
+};
+
+// Row of LDS for key (of 64): within 32 keys, key 16 h + 4 a + i is row 8 a + 4 h + i.
+__device__ __forceinline__ int row_of_key(int key) { return (key & 32) | ((key & 12) << 1) | ((key & 16) >> 2) | (key & 3); }
+
+// The sequence that has `n` longer ones (of equal ones the first comes first; as they are numbered, where there are more than a wave has lanes).
+__device__ __forceinline__ int nth_longest(const KvParams &c, int n, int lane) {
+  if (c.n_seqs == 1 || c.n_seqs > 64) return n;
+  const int mine = lane < c.n_seqs ? max(c.lengths[lane], 0) : -1;
+  int before = 0;
+  for (int j = 0; j < c.n_seqs; ++j) {
+    const int other = __builtin_amdgcn_readlane(mine, j);
+    before += other > mine || (other == mine && j < lane);
+  }
+  return (int)__builtin_ctzll(__ballot(lane < c.n_seqs && before == n));
 }
 
 // A finite stand-in for the base of a row that has seen nothing yet.

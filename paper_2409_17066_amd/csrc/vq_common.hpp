@@ -50,11 +50,12 @@ int cu_count();
 //   dequant=g    vq_dequant: generic kernels
 //   attention=d|p vq_attention: the decode kernel / the prompt kernel wherever it can
 //   parts=0..6   vq_attention: a sequence's keys in up to 2^n parts
-//   shared=0|1   vq_attention_shared: every sequence by itself / in two halves wherever it can
+//   prefix=d|p, prefix_parts=0..5  vq_attention_shared: the same for the prefixes (attention and parts for what lies behind, and where these are not given)
+//   shared=0|1|2 vq_attention_shared: every sequence by itself / in two halves wherever it can / in a launch each
 struct Switches {
-  char gemv = 0, gemm = 0, dequant = 0, attention = 0, shared = 0;
+  char gemv = 0, gemm = 0, dequant = 0, attention = 0, prefix = 0, shared = 0;
   bool groups_loop = false, multi_off = false;
-  int dense = -1, rows = -1, products = -1, parts = -1;
+  int dense = -1, rows = -1, products = -1, parts = -1, prefix_parts = -1;
 };
 const Switches &switches();
 void read_switches();

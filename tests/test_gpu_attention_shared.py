@@ -83,7 +83,7 @@ CASES = [
 
 
 @pytest.mark.parametrize("case", CASES, ids=lambda c: str(c)[:100])
-@pytest.mark.parametrize("switches", ["", "shared=1", "shared=1,attention=d,parts=0", "shared=1,attention=d,parts=2", "shared=1,attention=p,parts=0", "shared=1,attention=p,parts=3", "shared=0"])
+@pytest.mark.parametrize("switches", ["", "shared=1", "shared=1,attention=d,parts=0", "shared=1,attention=d,parts=2", "shared=1,attention=p,parts=0", "shared=1,attention=p,parts=3", "shared=0", "shared=2", "shared=2,attention=d,parts=2", "shared=2,attention=p,parts=1"])
 def test_against_every_sequence_by_itself(gpu_lib, monkeypatch, case, switches):
     import torch
     monkeypatch.setenv("VQ_SWITCHES", switches)
