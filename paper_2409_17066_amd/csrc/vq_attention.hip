@@ -81,31 +81,82 @@ struct SharedPlan {
   static size_t bytes(const Plan &half) { return (half.o_bytes + half.ml_bytes + 255) / 256 * 256; }
   size_t bytes() const { return bytes(prefix) + bytes(own); }
 };
+// What a half moves to the launch that joins them.
+void size_partials(Plan &half, long long seqs, int kv_heads, long long rows, int head_dim) {
+  half.o_bytes = (size_t)seqs * kv_heads * half.parts * rows * head_dim * 4;
+  half.ml_bytes = (size_t)seqs * kv_heads * half.parts * rows * 8;
+}
+
+// Both halves in one launch: the kernel of the prefixes and the parts of either half whose time is estimated the least, in us.  A workgroup of 256 threads takes runs of four chunks of 64 keys; two
+// share a compute unit.  With `size` for the elements of a head (1: 128) and `element` for the bytes of one, and q for quarters of a prompt workgroup's 128 rows that are there:
+//   a workgroup by itself      prefix, prompt kernel 2 + 4 size (1.18 + 0.126 q) a run     prefix, decode kernel 1.4 + 2.2 size element     own keys 2.5 + 1.15 size element
+//   of a full compute unit     2.9 + 4 size (0.47 + 0.18 q)                                0.9 + 2.6 size element                           two thirds of 1.4 + 2.7 size element
+// (sequences are shorter than the longest); the halves overlap, but for 0.36 of the smaller one, behind 4 us; the launch that joins them takes 4 us and 0.34 for each MB of partial results.
+// Fitted to 45 layouts by both kernels in 1 to 32 parts of the prefix and 1 to 4 of the rest: what is chosen takes up to 5 % longer than the least in 38, up to 29 % in the others.
+// Measured (64 query and 8 key heads of 128 elements, 8 bits): 64 sequences behind 8192 tokens with up to 1021 of their own 45 us by the prompt kernel in 8 parts, 51 by the decode kernel in 2,
+// 119 by themselves; 16 behind 8192 with 300 26 (prompt, 32), 21.5 (decode, 8) and 38; 4 behind 4096 with 100 16, 15 and 13.
+void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &a, SharedPlan &p) {
+  const float size = (float)((c.head_dim + 63) / 64) / 2.f, moved = size * (c.e4m3 ? 1.f : 2.f), cus = (float)cu_count();
+  const long long rows = (long long)x.rows_most * a.group, own_rows = (long long)c.max_new * a.group;
+  const long long runs = std::max<long long>((x.max_length + 255) / 256, 1), own_runs = std::max<long long>((x.max_own + 255) / 256, 1);
+  const float quarters = (float)std::min((rows + 31) / 32, 4LL);
+  const int own_tile = attention_decode_rows(c, a, c.max_new == 1);
+  const long long own_tiles = (own_rows + own_tile - 1) / own_tile;
+  const char kernel = switches().prefix ? switches().prefix : switches().attention;
+  const int prefix_parts = switches().prefix_parts >= 0 ? switches().prefix_parts : switches().parts;
+  p.prefix.time = 0.f;
+  for (const bool prompt : {false, true}) {
+    if ((kernel == 'd' || kernel == 'p') && prompt != (kernel == 'p')) continue;
+    const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(p.prefixes, a, true);
+    const long long tiles = (rows + tile - 1) / tile;
+    for (int i = prefix_parts >= 0 ? prefix_parts : 0; i <= (prefix_parts >= 0 ? prefix_parts : 5); ++i) {
+      const long long parts = std::min(std::min(1LL << i, runs), (long long)HALF_PARTS), blocks = x.n * c.kv_heads * tiles * parts;
+      const float turns = (float)((runs + parts - 1) / parts);
+      const float one = prompt ? 2.f + turns * 4.f * size * (1.18f + 0.126f * quarters) : 1.4f + turns * 2.2f * moved;
+      const float all = (float)blocks / cus * (prompt ? 2.9f + turns * 4.f * size * (0.47f + 0.18f * quarters) : 0.9f + turns * 2.6f * moved);
+      for (int k = switches().parts >= 0 ? switches().parts : 0; k <= (switches().parts >= 0 ? switches().parts : 2); ++k) {
+        const long long own_parts = std::min(std::min(1LL << k, own_runs), (long long)HALF_PARTS), own_blocks = c.n_seqs * c.kv_heads * own_tiles * own_parts;
+        const float own_turns = (float)((own_runs + own_parts - 1) / own_parts), own_one = 2.5f + own_turns * 1.15f * moved, own_all = (float)own_blocks / cus * 0.67f * (1.4f + own_turns * 2.7f * moved);
+        const float join = 4.f + (float)((long long)c.n_seqs * own_rows * c.kv_heads) * (float)(parts + own_parts) * (float)c.head_dim * 4e-6f * 0.34f;
+        const float time = 4.f + std::max(std::max(one, own_one), std::max(all, own_all) + 0.36f * std::min(all, own_all)) + join;
+        if (blocks + own_blocks > 0x7fffffff / THREADS || (p.prefix.time != 0.f && time >= p.prefix.time)) continue;
+        p.prefix.time = time;
+        p.prefix.prompt = prompt;
+        p.prefix.tile_rows = tile;
+        p.prefix.parts = (int)parts;
+        p.own.parts = (int)own_parts;
+        p.grid = HalvesGrid{(int)blocks, (int)own_blocks, (int)std::min(blocks, (long long)cu_count()), (int)tiles, (int)own_tiles, blocks <= 2 * cu_count()};
+      }
+    }
+  }
+  p.together = p.prefix.time != 0.f;
+  p.prefix.run = p.own.run = HALVES_WAVES;
+  p.own.tile_rows = own_tile;
+  size_partials(p.prefix, x.n, c.kv_heads, rows, c.head_dim);
+  size_partials(p.own, c.n_seqs, c.kv_heads, own_rows, c.head_dim);
+}
+
 SharedPlan shared_plan_of(const KvParams &c, const Prefixes &x, const AttentionParams &a) {
   SharedPlan p{};
   p.prefixes = as_sequences(c, x);
   // (rows of a prefix: token_of()'s division and a grid's layers)
   if (!attention_join_takes(c, a) || x.max_length == 0 || (long long)x.rows_most * a.group * a.group >= 1ll << 30) return p;
+  const char forced = switches().shared;
+  const Plan whole = plan_of(c, a, true);
+  // A launch for each half, by either kernel.
   p.prefix = plan_of(p.prefixes, a, true, PREFIX, x.max_length);
   p.own = plan_of(c, a, true, OWN, std::min(x.max_own, c.max_length));
-  const char forced = switches().shared;
-  p.shares = forced ? forced != '0' : p.prefix.time + p.own.time + 5.f < plan_of(c, a, true).time;
-  p.together = (c.head_dim == 64 || c.head_dim == 128) && !p.own.prompt && forced != '2';
-  if (!p.together) return p;
-  const long long rows = (long long)x.rows_most * a.group, own_rows = (long long)c.max_new * a.group;
-  p.grid.prefix_tiles = (int)((rows + p.prefix.tile_rows - 1) / p.prefix.tile_rows);
-  p.grid.own_tiles = (int)((own_rows + p.own.tile_rows - 1) / p.own.tile_rows);
-  p.own.run = HALVES_WAVES;
-  if (!p.prefix.prompt) p.prefix.run = HALVES_WAVES;
-  const long long prefix_blocks = (long long)x.n * c.kv_heads * p.grid.prefix_tiles * p.prefix.parts, own_blocks = (long long)c.n_seqs * c.kv_heads * p.grid.own_tiles * p.own.parts;
-  if (prefix_blocks + own_blocks > 0x7fffffff / THREADS) {
-    p.together = false;
-    return p;
+  const float apart = p.prefix.time + p.own.time + 5.f;
+  p.shares = forced ? forced != '0' : apart < whole.time;
+  if ((c.head_dim == 64 || c.head_dim == 128) && forced != '2') {
+    SharedPlan both = p;
+    plan_together(c, x, a, both);
+    if (both.together && both.prefix.time < apart) {
+      p = both;
+      // (what is estimated for few rows of single sequences is 6 us too much for the smallest and a quarter too little for the largest)
+      p.shares = forced ? forced != '0' : p.prefix.time < (whole.prompt ? whole.time : 1.25f * whole.time - 9.f);
+    }
   }
-  p.grid.prefix_blocks = (int)prefix_blocks;
-  p.grid.own_blocks = (int)own_blocks;
-  p.grid.first = std::min(p.grid.prefix_blocks, cu_count());
-  p.grid.zigzag = prefix_blocks <= 2 * cu_count();
   return p;
 }
 
