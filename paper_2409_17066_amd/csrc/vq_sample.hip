@@ -23,6 +23,7 @@ constexpr int OCTAVES = INF / 1024;
 static_assert(ENTRIES <= PADDED && INF % RUN == 0 && 1024 % RUN == 0, "runs lie within a power of two");
 
 typedef __attribute__((address_space(3))) unsigned *Lds;
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 
 // A value's place in the order of all: the i-th of run `entry`.
 struct Place {
@@ -128,8 +129,8 @@ __device__ __forceinline__ void add(unsigned address, unsigned n) {
 template <bool UPPER>
 __device__ __forceinline__ unsigned of_half(unsigned word, unsigned factor, unsigned more) {
   unsigned r;
-  if (UPPER) asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(r) : "v"(word), "s"(factor), "v"(more));
-  else asm("v_mad_u32_u16 %0, %1, %2, %3" : "=v"(r) : "v"(word), "s"(factor), "v"(more));
+  if (UPPER) asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(r) : "v"(word), "v"(factor), "v"(more));
+  else asm("v_mad_u32_u16 %0, %1, %2, %3" : "=v"(r) : "v"(word), "v"(factor), "v"(more));
   return r;
 }
 
@@ -175,7 +176,7 @@ struct Drawer {
   // (1 for numbers above the largest, of which there are none)
   __device__ __forceinline__ double weight(unsigned bits) const { return exp_of(fmin(((double)number_of(bits) - top) * per, 0.0)); }
 
-  // Counts the row (WIDE: its numbers of one sign; zeros are positive); -> of this thread's numbers, those that are not NaN or minus infinity, and the largest ones of either half.
+  // Counts the row (WIDE: its numbers of one sign; zeros are positive); -> of this thread's numbers, those that are finite (WIDE: or infinite and positive), and the largest ones of either half.
   template <int HELD>
   __device__ __forceinline__ unsigned count(bool negative, half2v &largest, Held<HELD> &held) {
     const Walk of_wave = walk_of(0, r.vocabulary / 8, wave);
@@ -191,39 +192,51 @@ struct Drawer {
     for (int i = tid; i < WORDS / 4; i += THREADS) all[i] = uint4v{0, 0, 0, 0};
     __syncthreads();
     const unsigned base = (unsigned)(size_t)(Lds)words;
-    unsigned valid = 0, largest_sizes = 0;
+    unsigned valid = 0;
+    ushort2v largest_sizes = {0, 0}, infinities = {0, 0};
     largest = half2v{(_Float16)-__builtin_inff(), (_Float16)-__builtin_inff()};
+    // Infinities (a grammar's mask, mostly) go to a word behind the sizes that no other lane of the wave adds to: 64 lanes that add to the same one take 64 turns.
+    const unsigned aside = (1 + (unsigned)tid % 1023) * 4;
     auto one = [&](uint4v x) {
       const uint4v size = x & 0x7FFF7FFFu;
-      auto larger = [](unsigned a, unsigned b) {
-        typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
-        return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
-      };
+      auto larger = [](unsigned a, unsigned b) { return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b))); };
       const unsigned sizes = larger(larger(size.x, size.y), larger(size.z, size.w));
-      const bool odd = ((sizes + 0x04000400u) & 0x80008000u) != 0, alike = x.x == x.y && x.x == x.z && x.x == x.w;
+      const bool odd = ((sizes + 0x04000400u) & 0x80008000u) != 0, nan = ((sizes + 0x03FF03FFu) & 0x80008000u) != 0, alike = x.x == x.y && x.x == x.z && x.x == x.w;
       largest = __builtin_elementwise_max(largest, __builtin_elementwise_max(__builtin_elementwise_max(half2_of(x.x), half2_of(x.y)), __builtin_elementwise_max(half2_of(x.z), half2_of(x.w))));
-      if (WIDE || odd || alike) {
-        // what is not counted, and eight times the same, as masks leave it: one addition, where 64 lanes that add one to the same word take 64 turns
-        if (alike && x.x == NONE) return;
+      if (WIDE || nan || alike) {
+        // NaN, which is not counted, and eight times the same, as masks of a number leave it: one addition
+        if (!WIDE && alike && x.x == NONE) return;
         const bool same = alike && (x.x & 0xffff) == x.x >> 16;
 #pragma unroll 1
         for (int j = 0; j < 8; ++j) {
           const unsigned bits = half_at(x, j), m = bits & 0x7FFF, n = same ? 8 : 1;
           const bool minus = bits >= 0x8000u && m;
-          if (m > INF || (m == INF && minus) || (same && j)) continue;
+          if (m > INF || (m == INF && (!WIDE || minus)) || (same && j)) continue;
           valid += n;
-          if (m < INF) largest_sizes = larger(largest_sizes, m);
+          if (m < INF) largest_sizes = __builtin_elementwise_max(largest_sizes, (ushort2v){(unsigned short)m, 0});
           if (!WIDE) add(base + m * 4, bits & 0x8000u ? n << 16 : n);
           else if (minus == negative) add(base + m * 4, n);
         }
         return;
       }
       valid += 8;
-      largest_sizes = larger(largest_sizes, sizes);
       const uint4v sign = (x >> 15) & 0x00010001u;
+      if (!__ballot(odd)) {
+        largest_sizes = __builtin_elementwise_max(largest_sizes, __builtin_bit_cast(ushort2v, sizes));
+        auto two = [&](unsigned m, unsigned minus) {
+          add(of_half<false>(m, 4, base), of_half<false>(minus, 0xFFFF, 1));
+          add(of_half<true>(m, 4, base), of_half<true>(minus, 0xFFFF, 1));
+        };
+        two(size.x, sign.x); two(size.y, sign.y); two(size.z, sign.z); two(size.w, sign.w);
+        return;
+      }
       auto two = [&](unsigned m, unsigned minus) {
-        add(of_half<false>(m, 4, base), of_half<false>(minus, 0xFFFF, 1));
-        add(of_half<true>(m, 4, base), of_half<true>(minus, 0xFFFF, 1));
+        const ushort2v of = __builtin_bit_cast(ushort2v, m), most = {INF - 1, INF - 1}, all = {INF, INF}, infinite = __builtin_elementwise_sub_sat(of, most);     // (one or zero)
+        infinities += infinite;
+        largest_sizes = __builtin_elementwise_max(largest_sizes, of - infinite * all);
+        const unsigned which = __builtin_bit_cast(unsigned, infinite);
+        add(of_half<false>(which, aside, of_half<false>(m, 4, base)), of_half<false>(minus, 0xFFFF, 1));
+        add(of_half<true>(which, aside, of_half<true>(m, 4, base)), of_half<true>(minus, 0xFFFF, 1));
       };
       two(size.x, sign.x); two(size.y, sign.y); two(size.z, sign.z); two(size.w, sign.w);
     };
@@ -235,8 +248,8 @@ struct Drawer {
       walk<WIDE ? 2 : 8>(r, of_wave, lane, one);
     }
     if ((r.vocabulary & 7) && tid == THREADS - 1) one(tail_of(r, last, tid));
-    largest_size = max(largest_sizes & 0xffff, largest_sizes >> 16);
-    return valid;
+    largest_size = max(largest_sizes.x, largest_sizes.y);
+    return valid - infinities.x - infinities.y;
   }
   // The sum of all threads' `valid` and the largest number, for all of them.
   __device__ __forceinline__ void tell(unsigned valid, half2v largest, unsigned &valid_of_all, float &top_of_all) {
@@ -542,7 +555,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
   d.per = 1.0 / (double)r.temperature;
   if (hot) d.make_powers();
   d.tell(valid, largest, valid, top);
-  if (valid == 0) {
+  if (valid == 0 && !(top > 0.f)) {                                  // (infinite logits are not counted, but there)
     if (tid == 0) {
       p.tokens[row] = -1;
       if (p.probabilities) p.probabilities[row] = 0.f;
@@ -555,13 +568,11 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
   if (hot) {
     d.top = (double)top;
     const bool infinite = bits == INF;
-    bool overflown = false;
+    bool overflown = infinite;                                      // (infinite ones: by wide counts)
     if (!infinite) {
       d.sum_runs(false);
       d.scan();
       overflown = s.count[PADDED - 1] != valid;
-    } else if (r.vocabulary > 65535) {
-      overflown = true;                                             // (how many infinite ones: by wide counts)
     }
     if (overflown) {
       Drawer<true> e{r, words, s, tid, lane, wave, d.top, d.per, INF};
@@ -593,26 +604,24 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
     } else {
       // (one wave: it needs nothing of the others, which would be in its way, but for the border of min_p, which depends on none of its own)
       Border e;
-      if (!infinite) {
-        if (wave == 1 && r.min_p > 0.f) {
-          const Border m = d.below_min_p();
-          if (lane == 0) {
-            s.below_entry = m.at.entry;
-            s.below_i = m.at.i;
-            s.below_mass = m.mass;
-          }
+      if (wave == 1 && r.min_p > 0.f) {
+        const Border m = d.below_min_p();
+        if (lane == 0) {
+          s.below_entry = m.at.entry;
+          s.below_i = m.at.i;
+          s.below_mass = m.mass;
         }
-        if (wave == 0) e = d.kept();
-        if (r.min_p > 0.f) __syncthreads();
       }
+      if (wave == 0) e = d.kept();
+      if (r.min_p > 0.f) __syncthreads();
       if (wave == 0) {
-        if (r.min_p > 0.f && !infinite) {
+        if (r.min_p > 0.f) {
           const Border m{{s.below_entry, s.below_i}, 0, s.below_mass};
           if (in_front(m, e)) e = m;
         }
-        const Border t = infinite ? infinite_of(r, words[INF] & 0xffff, probability) : d.drawn(e, probability);
+        const Border t = d.drawn(e, probability);
         if (lane == 0) {
-          s.bits = infinite ? INF : (int)bits_of(t.at);
+          s.bits = (int)bits_of(t.at);
           s.nth = t.n;
           s.probability = probability;
         }
@@ -628,7 +637,6 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
   const unsigned zeros = (bits & 0x7FFFu) == 0 ? 0x7FFF7FFFu : 0xFFFFFFFFu, both = (bits | bits << 16) & zeros;
   auto differs = [&](uint4v x) { return (x & zeros) ^ both; };
   auto matches = [&](uint4v x) {
-    typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
     const uint4v d = differs(x);
     auto smaller = [](unsigned a, unsigned b) {
       return __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
