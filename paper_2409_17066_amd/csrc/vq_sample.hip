@@ -68,11 +68,11 @@ struct Row {
 struct Scratch {
   double mass[PADDED];
   unsigned count[PADDED];
-  double wave_mass[WAVES];
+  double wave_mass[WAVES], mass_up_to[WAVES];
   double powers[OCTAVES][RUN / 4], factors[OCTAVES];      // by the power of two of a run's sizes: the factor from a number's weight to the next one's, and its (4 i)-th power
   double below_mass;
   int below_entry, below_i;
-  unsigned wave_count[WAVES], wave_valid[WAVES], wave_top[WAVES], wave_size[WAVES], counts[RUN];
+  unsigned wave_count[WAVES], count_up_to[WAVES], wave_valid[WAVES], wave_top[WAVES], wave_size[WAVES], counts[RUN];
   int found[WAVES], of_tail, bits, nth;
   float probability;
 };
@@ -288,86 +288,69 @@ struct Drawer {
     if (i < EACH - 1) s.powers[octave][i] = f;
     else s.factors[octave] = f;
   }
-  // Counts and weights of the runs of both signs (WIDE: of one), of a thread's 32 sizes, to the scratch.
+  // Counts and weights of the runs of both signs (WIDE: of one), of a thread's 32 sizes, to the scratch.  That of the row's largest number is summed value by value by the last wave, half of which has
+  // no other: weights relative to its neighbours could be too large for a number there, and of equal logits the sums are whole numbers so, whose weight is one without a rounding.
   __device__ __forceinline__ void sum_runs(bool negative) {
-    if (tid < PADDED - ENTRIES) {                                   // (entries behind the last run)
-      s.mass[ENTRIES + tid] = 0.0;
-      s.count[ENTRIES + tid] = 0;
+    const unsigned of_top = __half_as_ushort(__float2half_rn((float)top)), top_size = of_top & 0x7FFFu;
+    const bool top_minus = of_top >= 0x8000u && top_size;
+    if (wave == WAVES - 1) {
+      s.mass[ENTRIES + lane] = 0.0;                                 // (entries behind the last run)
+      s.count[ENTRIES + lane] = 0;
+      if (!WIDE || negative == top_minus) {
+        const int entry = place_of(of_top).entry;
+        const unsigned bits = bits_of(Place{entry, lane & (RUN - 1)}), w = words[bits & 0x7FFFu];
+        unsigned n = WIDE ? w : bits & 0x8000u ? w >> 16 : bits ? w & 0xffff : (w & 0xffff) + (w >> 16);
+        if (lane >= RUN || bits == 0x8000u) n = 0;                  // (minus zero is counted as zero)
+        const double m = sums_of((double)n * weight(bits));
+        n = sums_of(n);
+        if (lane == 63) {
+          s.mass[entry] = m;
+          s.count[entry] = n;
+        }
+      }
     }
     if (tid >= RUNS) return;
-    if ((unsigned)tid * RUN > largest_size) {                       // (the same for both signs of WIDE: nothing is lost)
-      s.mass[RUNS - 1 - tid] = s.mass[RUNS + tid] = 0.0;
-      s.count[RUNS - 1 - tid] = s.count[RUNS + tid] = 0;
-      return;
-    }
-    const uint4v *from = reinterpret_cast<const uint4v *>(words) + tid * (RUN / 4);
-    // A run's powers of q begin at its largest number, that of largest size of the positive and of smallest size of the negative ones, and in the run of the row's largest number at
-    // that one, whose weight is one without a rounding (of equal logits the sums are whole numbers then).  Lanes begin in different quarters of their runs, whose first words lie in the
-    // same bank of LDS for every second lane.
-    const unsigned least = (unsigned)tid * RUN, of_top = __half_as_ushort(__float2half_rn((float)top)), top_size = of_top & 0x7FFFu;
-    const bool has_top = top_size / RUN == (unsigned)tid, top_plus = has_top && (of_top < 0x8000u || !top_size), top_minus = has_top && !top_plus;
-    const int from_plus = top_plus ? (int)(top_size % RUN) : RUN - 1, from_minus = top_minus ? (int)(top_size % RUN) : 0;
-    const double(&powers)[RUN / 4] = s.powers[tid / (1024 / RUN)];
-    const double q = s.factors[tid / (1024 / RUN)], q2 = q * q;
-    struct Four {
-      unsigned a[4], b[4];
-    };
-    auto four = [&](int c) {
-      const uint4v w = from[c];
-      Four f = WIDE ? Four{{w.x, w.y, w.z, w.w}, {w.x, w.y, w.z, w.w}}
-                    : Four{{w.x & 0xffff, w.y & 0xffff, w.z & 0xffff, w.w & 0xffff}, {w.x >> 16, w.y >> 16, w.z >> 16, w.w >> 16}};
-      if (!WIDE && tid == 0 && c == 0) {                            // zeros
-        f.a[0] += f.b[0];
-        f.b[0] = 0;
-      }
-      return f;
-    };
+    const unsigned least = (unsigned)tid * RUN;
+    const bool has_top = top_size / RUN == (unsigned)tid, plus_too = (!WIDE || !negative) && !(has_top && !top_minus), minus_too = (!WIDE || negative) && !(has_top && top_minus);
     double plus = 0.0, minus = 0.0;
     unsigned n_plus = 0, n_minus = 0;
+    if (least <= largest_size) {
+      // A run's powers of q begin at its largest number, that of largest size of the positive and of smallest size of the negative ones.  Lanes begin in different quarters of their runs,
+      // whose first words lie in the same bank of LDS for every second lane.
+      const uint4v *from = reinterpret_cast<const uint4v *>(words) + tid * (RUN / 4);
+      const double *powers = s.powers[tid / (1024 / RUN)];
+      const double q = s.factors[tid / (1024 / RUN)];
+      int c = (lane >> 1) & 7;
+      uint4v w = from[c];
+      // (one after the other: there are few registers beside those of a row that is kept)
 #pragma unroll 1
-    for (int j = 0; j < RUN / 4; ++j) {
-      const int c = (j + (lane >> 1)) & 7;
-      const Four f = four(c);
-      auto power = [&](int e) {                                     // q^e
-        double p = powers[e >> 2];
-        if (has_top) p *= (e & 1 ? q : 1.0) * (e & 2 ? q2 : 1.0);
-        return p;
-      };
-      if (!WIDE || !negative) {
-        n_plus += (f.a[0] + f.a[1]) + (f.a[2] + f.a[3]);
-        const int e = from_plus - 4 * c - 3;
-        if (e >= 0) plus = __fma_rn(__fma_rn(__fma_rn(__fma_rn((double)f.a[0], q, (double)f.a[1]), q, (double)f.a[2]), q, (double)f.a[3]), power(e), plus);
+      for (int j = 0; j < RUN / 4; ++j) {
+        const int next = (c + 1) & 7;
+        const uint4v ahead = from[next];
+        const double p_plus = powers[7 - c], p_minus = powers[c];
+        unsigned a0 = WIDE ? w.x : w.x & 0xffff, b0 = WIDE ? w.x : w.x >> 16;
+        const unsigned a1 = WIDE ? w.y : w.y & 0xffff, a2 = WIDE ? w.z : w.z & 0xffff, a3 = WIDE ? w.w : w.w & 0xffff;
+        const unsigned b1 = WIDE ? w.y : w.y >> 16, b2 = WIDE ? w.z : w.z >> 16, b3 = WIDE ? w.w : w.w >> 16;
+        if (!WIDE && (tid | c) == 0) {                              // zeros
+          a0 += b0;
+          b0 = 0;
+        }
+        n_plus += (a0 + a1) + (a2 + a3);
+        n_minus += (b0 + b1) + (b2 + b3);
+        plus = __fma_rn(__fma_rn(__fma_rn(__fma_rn((double)a0, q, (double)a1), q, (double)a2), q, (double)a3), p_plus, plus);
+        minus = __fma_rn(__fma_rn(__fma_rn(__fma_rn((double)b3, q, (double)b2), q, (double)b1), q, (double)b0), p_minus, minus);
+        c = next;
+        w = ahead;
       }
-      if (!WIDE || negative) {
-        n_minus += (f.b[0] + f.b[1]) + (f.b[2] + f.b[3]);
-        const int e = 4 * c - from_minus;
-        if (e >= 0) minus = __fma_rn(__fma_rn(__fma_rn(__fma_rn((double)f.b[3], q, (double)f.b[2]), q, (double)f.b[1]), q, (double)f.b[0]), power(e), minus);
-      }
+      if (n_plus) plus *= weight(least + RUN - 1);
+      if (n_minus) minus *= weight(least | 0x8000u);
     }
-    if (has_top) {                                                  // the four around the largest number, where the powers begin among them
-      const int c = (int)(top_size % RUN) / 4, at = (int)(top_size % 4);
-      const Four f = four(c);
-      double sum = 0.0;
-      if (top_plus && at < 3) {
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-          if (i <= at) sum = __fma_rn(sum, q, (double)f.a[i]);
-        plus += sum;
-      }
-      if (top_minus && at > 0) {
-#pragma unroll
-        for (int i = 3; i > 0; --i)
-          if (i >= at) sum = __fma_rn(sum, q, (double)f.b[i]);
-        minus += sum;
-      }
-    }
-    const double w_plus = weight(least + RUN - 1), w_minus = weight(least | 0x8000u);
-    if (!WIDE || !negative) {
-      s.mass[RUNS - 1 - tid] = n_plus ? plus * w_plus : 0.0;
+    if (plus_too) {
+      s.mass[RUNS - 1 - tid] = plus;
       s.count[RUNS - 1 - tid] = n_plus;
     }
-    if (!WIDE || negative) {
-      s.mass[RUNS + tid] = n_minus ? minus * w_minus : 0.0;
+    if (minus_too) {
+      s.mass[RUNS + tid] = minus;
       s.count[RUNS + tid] = n_minus;
     }
   }
@@ -384,11 +367,14 @@ struct Drawer {
       s.wave_count[wave] = c;
     }
     __syncthreads();
-    double before = 0.0;
-    unsigned count_before = 0;
-    for (int w = 0; w < wave; ++w) {
-      before += s.wave_mass[w];
-      count_before += s.wave_count[w];
+    // lane w: the sums up to wave w's end
+    const double up_to = sums_of(lane < WAVES ? s.wave_mass[lane] : 0.0);
+    const unsigned count_up_to = sums_of(lane < WAVES ? s.wave_count[lane] : 0u);
+    const double before = wave ? of_lane(up_to, wave - 1) : 0.0;
+    const unsigned count_before = wave ? of_lane(count_up_to, wave - 1) : 0;
+    if (wave == 0 && lane < WAVES) {
+      s.mass_up_to[lane] = up_to;
+      s.count_up_to[lane] = count_up_to;
     }
     s.mass[2 * tid + 1] = before + m;
     s.count[2 * tid + 1] = count_before + c;
@@ -450,13 +436,17 @@ struct Drawer {
   // The first run whose sums `is` says yes to; -1: none.
   template <typename Is>
   __device__ __forceinline__ int entry_where(Is is) const {
-    constexpr int EACH = PADDED / 64;
-    const unsigned long long coarse = __ballot(is(s.count[lane * EACH + EACH - 1], s.mass[lane * EACH + EACH - 1]));
-    if (!coarse) return -1;
-    const int from = __builtin_ctzll(coarse) * EACH, at = from + (lane & (EACH - 1));
-    // (sums that rounding leaves in no order: the last one has been seen)
-    const unsigned long long fine = __ballot(is(s.count[at], s.mass[at]));
-    return from + __builtin_ctzll(fine);
+    // (of the sixteen stretches that the waves have added up, then two runs a lane; where rounding leaves the sums in no order, the stretch's last one)
+    constexpr int EACH = PADDED / WAVES;
+    static_assert(EACH == 128, "two runs a lane");
+    const unsigned long long stretch = __ballot(lane < WAVES && is(s.count_up_to[lane & (WAVES - 1)], s.mass_up_to[lane & (WAVES - 1)]));
+    if (!stretch) return -1;
+    const int from = __builtin_ctzll(stretch) * EACH, at = from + 2 * lane;
+    const bool first = is(s.count[at], s.mass[at]), second = is(s.count[at + 1], s.mass[at + 1]);
+    const unsigned long long both = __ballot(first || second);
+    if (!both) return from + EACH - 1;
+    const int l = __builtin_ctzll(both);
+    return from + 2 * l + (__ballot(first) >> l & 1 ? 0 : 1);
   }
 
   __device__ __forceinline__ Border end() const { return Border{{PADDED, 0}, 0, s.mass[PADDED - 1]}; }
