@@ -6,7 +6,7 @@ One layer is eight calls on one stream (prompts of more than sixteen tokens take
     x += h; z = norm(x)             residual_norm      (h: what the layer before left)
     q, k, v = products of z         gemv_multi / gemm
     rotate q and k, store k and v   kv_append
-    a = attention(q, cache)         attention
+    a = attention(q, cache)         attention          (attention_shared where the sequences begin with the same tokens)
     h = product of a                gemv / gemm
     x += h; z = norm(x)             residual_norm
     g, u = products of z            gemv_multi / gemm
@@ -39,15 +39,29 @@ class PagedCache:
 
 
 class Sequences:
-    """Which pages each sequence has, how long it is, and which rows are its new tokens; shared by all layers."""
+    """Which pages each sequence has, how long it is, and which rows are its new tokens; shared by all layers.  shared: so many tokens, whole pages of them, that all sequences
+    begin with, in pages that they have in common; first() is the sequence of these alone, whose tokens come first."""
 
-    def __init__(self, n_seqs, page_tokens, longest):
-        each = -(-longest // page_tokens)
+    def __init__(self, n_seqs, page_tokens, longest, shared=0):
+        assert shared % page_tokens == 0
+        common, each = shared // page_tokens, -(-(longest - shared) // page_tokens)
         self.page_tokens, self.n_seqs, self.longest = page_tokens, n_seqs, longest
         # (a server hands pages out as sequences grow; here each gets its own beforehand, interleaved as they would come to lie)
-        self.table = torch.arange(n_seqs * each, dtype=torch.int32, device="cuda").reshape(each, n_seqs).t().contiguous()
-        self.lengths = torch.zeros(n_seqs, dtype=torch.int32, device="cuda")
+        own = common + torch.arange(n_seqs * each, dtype=torch.int32, device="cuda").reshape(each, n_seqs).t()
+        prefix = torch.arange(common, dtype=torch.int32, device="cuda").expand(n_seqs, -1)
+        self.table = torch.cat((prefix, own), 1).contiguous()
+        self.pages = common + n_seqs * each
+        self.lengths = torch.full((n_seqs,), shared, dtype=torch.int32, device="cuda")
         self.starts, self.max_new, self.max_length = None, 1, longest
+        self.prefix = None
+        if shared:
+            self.prefix = dict(prefix_table=prefix[:1].contiguous(), prefix_lengths=self.lengths[:1].clone(), max_prefix=shared, max_own=longest - shared)
+
+    def first(self):
+        """The tokens that all sequences begin with as a sequence of its own, without a length so far."""
+        alone = Sequences(1, self.page_tokens, self.prefix["max_prefix"])
+        alone.table = self.prefix["prefix_table"]
+        return alone
 
     def begin(self, news):
         """news: how many new tokens each sequence brings."""
@@ -80,7 +94,7 @@ class DecoderLayer:
         q, k, v = products([w["q"], w["k"], w["v"]], z)
         q, k, v = (t.unflatten(1, (-1, self.head_dim)) for t in (q, k, v))
         vq.kv_append(k, v, q=q, q_out=q, cos=cos, sin=sin, **where)
-        a = vq.attention(q, **where)
+        a = vq.attention(q, **where) if seqs.prefix is None else vq.attention_shared(q, **seqs.prefix, **where)
         h, = products([w["o"]], a.flatten(1))
         _, z = vq.residual_norm(h, x, pre=self.norm2, y=x)
         gate, up = products([w["gate"], w["up"]], z)
@@ -92,14 +106,15 @@ class Decoder:
     """Layers, their caches and the last norm: new tokens' rows in, normalised rows out."""
 
     def __init__(self, layers, last_norm, cos, sin, seqs, bits):
-        pages = seqs.table.numel()
+        pages = seqs.pages
         self.layers, self.last_norm, self.cos, self.sin, self.seqs = layers, last_norm, cos, sin, seqs
         self.caches = [PagedCache(pages, l.kv_heads, seqs.page_tokens, l.head_dim, bits) for l in layers]
 
-    def __call__(self, x):
+    def __call__(self, x, seqs=None):
+        """seqs: the sequences that x's rows are of (None: the decoder's)."""
         x, h = x.float(), None
         for layer, cache in zip(self.layers, self.caches):
-            h = layer(h, x, self.seqs, cache, self.cos, self.sin)
+            h = layer(h, x, seqs or self.seqs, cache, self.cos, self.sin)
         return vq.residual_norm(h, x, pre=self.last_norm, y=x)[1]
 
     def capture(self, x):
