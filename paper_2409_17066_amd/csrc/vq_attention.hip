@@ -72,7 +72,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
 
 Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed) { return plan_of(c, a, parts_allowed, WHOLE, c.max_length); }
 
-// Attention behind shared prefixes: the prefixes and what lies behind, in one launch or two, and one that joins them.
+// Attention behind shared prefixes: the prefixes and what lies behind, in one launch or one each, and one that joins them.
 struct SharedPlan {
   KvParams prefixes;             // as sequences
   Plan prefix, own;
@@ -136,18 +136,26 @@ void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &
   size_partials(p.own, c.n_seqs, c.kv_heads, own_rows, c.head_dim);
 }
 
+// (a call is launched whole or refused: a launch that a grid has no room for, and partial results whose bytes 64 bits do not count, are found before the first launch)
+bool half_fits(const KvParams &c, const AttentionParams &a, const Plan &half) {
+  const long long rows = (long long)c.max_new * a.group;
+  return (!half.prompt || (long long)c.n_seqs * c.kv_heads * ((rows + half.tile_rows - 1) / half.tile_rows) * half.parts <= 0xffffffffll / THREADS) &&
+         (double)c.n_seqs * c.kv_heads * half.parts * (double)rows * (c.head_dim * 4 + 8) < 4e18;
+}
+
 SharedPlan shared_plan_of(const KvParams &c, const Prefixes &x, const AttentionParams &a) {
   SharedPlan p{};
   p.prefixes = as_sequences(c, x);
-  // (rows of a prefix: token_of()'s division and a grid's layers)
-  if (!attention_join_takes(c, a) || x.max_length == 0 || (long long)x.rows_most * a.group * a.group >= 1ll << 30) return p;
+  // (rows of a prefix: token_of()'s division and a grid's layers; rows of a sequence: threads of the launch that joins, up to 64 a row)
+  if (!attention_join_takes(c, a) || x.max_length == 0 || (long long)x.rows_most * a.group * a.group >= 1ll << 30 || (long long)c.max_new * a.q_heads >= 1ll << 25) return p;
   const char forced = switches().shared;
   const Plan whole = plan_of(c, a, true);
   // A launch for each half, by either kernel.
   p.prefix = plan_of(p.prefixes, a, true, PREFIX, x.max_length);
   p.own = plan_of(c, a, true, OWN, std::min(x.max_own, c.max_length));
   const float apart = p.prefix.time + p.own.time + 5.f;
-  p.shares = forced ? forced != '0' : apart < whole.time;
+  const bool fit = half_fits(p.prefixes, a, p.prefix) && half_fits(c, a, p.own);
+  p.shares = fit && (forced ? forced != '0' : apart < whole.time);
   if ((c.head_dim == 64 || c.head_dim == 128) && forced != '2') {
     SharedPlan both = p;
     plan_together(c, x, a, both);
