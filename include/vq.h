@@ -42,7 +42,8 @@
  * The environment variable VQ_SWITCHES ("name=value,..."; read once at the
  * start of every call) forces kernel choices for tests and measurements:
  * gemv=g|m|d (generic / matrix-core / dot-product kernels), rows=0|1, products=0|1, groups=loop,
- * multi=0, gemm=g|f|w|r|6|c, dense=0..9, dequant=g; unset, every choice is the library's own.
+ * multi=0, gemm=g|f|w|r|6|c, dense=0..9, dequant=g, attention=d|p, parts=0..6, shared=0|1|2, prefix=d|p, prefix_parts=0..5;
+ * unset, every choice is the library's own.
  */
 #ifndef VQ_H
 #define VQ_H
@@ -398,7 +399,7 @@ int vq_residual_norm(const void *h, int64_t ldh, const void *x, int64_t ldx, con
 /* ---- in front of the first layer and behind the last --------------------------------------------------------------------
  * Embedding lookup: y[r] = scale * table[ids[r]], r < rows.  table: fp16 [vocabulary][ld], y: fp16, or binary32 with stream32 != 0, [rows][ldy]; the product is binary32,
  * rounded once.  A row whose id is outside [0, vocabulary) gets zeros (vq_sample's -1, a padded batch).  ids and y in 32 bits are 4-byte aligned, the rest to 2
- * bytes; width and vocabulary up to 2^24.                                                                        */
+ * bytes; y must not overlap the table or ids; width and vocabulary up to 2^24.                                                                        */
 int vq_embed(const int32_t *ids, int32_t rows, const void *table, int64_t ld, int32_t vocabulary, int32_t width, float scale, int32_t stream32, void *y, int64_t ldy,
              void *hip_stream);
 

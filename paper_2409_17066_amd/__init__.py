@@ -580,7 +580,7 @@ def embed(ids, table, scale=1.0, dtype=None, out=None):
 
 
 def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, return_prob=False):
-    """The next token of each row: logits: fp16 [rows][vocabulary], uniform: fp32 [rows] numbers in [0, 1) -> int32 [rows], -1 for a row without finite logits; with
+    """The next token of each row: logits: fp16 [rows][vocabulary], uniform: fp32 [rows] numbers in [0, 1) -> int32 [rows], -1 for a row of nothing but minus infinity and NaN; with
     return_prob also its probability among what is kept, fp32 [rows].  temperature (0: the largest logit), top_k (0: all), top_p (1: all), min_p (0: all): numbers,
     or device tensors [rows] (fp32, top_k int32)."""
     r = (_bound or _native()).sample(logits, uniform, temperature, top_k, top_p, min_p, out, return_prob)

@@ -61,7 +61,7 @@ SETTINGS = [dict(), dict(temperature=0.7), dict(top_k=1), dict(top_k=50, tempera
             dict(top_k=40, top_p=0.95, min_p=0.02, temperature=0.8), dict(temperature=0.0), dict(top_k=10 ** 9), dict(temperature=100.0), dict(temperature=1e-3), dict(temperature=float("inf"), top_p=0.5)]
 
 
-@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 63, 511, 513, 1000, 8191, 8192, 8193, 32000, 65536, 100003])
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 63, 511, 513, 1000, 8191, 8192, 8193, 32000, 65536, 100003, 131079, 300001])
 def test_vocabularies(gpu_lib, n):
     import torch
     rng = np.random.default_rng(n)
