@@ -8,6 +8,11 @@
 // 32 neighbouring values of a sign (a run) lie a constant distance apart, so that their weights are w q^i, one exponential and a polynomial in q with the counts as coefficients.
 // Sums are of 64 bits, in an order that depends on nothing: which token a number falls on is decided by sums over the vocabulary, whose rounding in 32 bits (2^-24 times a sum's
 // terms) is as large as a rare token's share.
+//
+// Latency bounds it: few rows, each the work of one compute unit, in phases behind one another (clocks of a row of 32000: counts 9400, sums of the runs 6500, over the runs 2000, borders and the number's
+// place 3000 to 6400, its occurrence 3000); of many long rows the counts, 12 to 19 clocks for 64 additions to LDS.  Measured: one row of 32000 with all settings 14 us, 20 rows of 50261
+// with 40 % masked 18, 64 rows of 128000 with top_p 23, 256 of 131072 30 (2.2 TB/s).  Rows on odd addresses are read from the first multiple of sixteen bytes on: 20 rows of 50261 16 us, of which
+// such reads without took 21.
 #include "vq_kv.hpp"
 
 namespace vq {
@@ -57,9 +62,10 @@ __device__ __forceinline__ double exp_of(double y) {
   return ldexp(p, (int)n);
 }
 
+// Vectors of eight numbers are read from addresses of sixteen bytes: `head` numbers stand in front of a row's first one, and fewer than eight behind its last.
 struct Row {
-  const __half *logits;
-  int vocabulary;
+  const __half *logits;          // the first vector
+  int vocabulary, head, vectors;
   float temperature, top_p, min_p, uniform;
   int top_k;
 };
@@ -73,7 +79,7 @@ struct Scratch {
   double below_mass;
   int below_entry, below_i;
   unsigned wave_count[WAVES], count_up_to[WAVES], wave_valid[WAVES], wave_top[WAVES], wave_size[WAVES], counts[RUN];
-  int found[WAVES], of_tail, bits, nth;
+  int found[WAVES], at_front, behind_all, bits, nth;
   float probability;
 };
 
@@ -87,19 +93,23 @@ __device__ __forceinline__ Walk walk_of(int first, int vectors, int wave) {
 }
 constexpr unsigned NONE = 0xFC00FC00u;                              // two minus infinities
 __device__ __forceinline__ uint4v load8(const Row &r, int vector) { return *reinterpret_cast<const uint4b *>(r.logits + (long long)vector * 8); }
-// A row's last eight numbers, of which those behind the whole vectors count, in the workgroup's last thread: the others, and those of other threads, are minus infinities.
-__device__ __forceinline__ uint4v last8(const Row &r) {
-  if (r.vocabulary >= 8) return *reinterpret_cast<const uint4b *>(r.logits + r.vocabulary - 8);
+// What stands in front of the vectors, in the workgroup's first thread, and what stands behind them, in its last: the row's first and last eight numbers, of which the others, and those of other
+// threads, are minus infinities.
+__device__ __forceinline__ uint4v ends_read(const Row &r, int tid) {
+  const __half *row = r.logits - r.head;
+  if (r.vocabulary >= 8) return *reinterpret_cast<const uint4b *>(tid ? row + r.vocabulary - 8 : row);
   unsigned h[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) h[j] = j >= 8 - r.vocabulary ? __half_as_ushort(r.logits[r.vocabulary - 8 + j]) : 0xFC00u;
+  for (int j = 0; j < 8; ++j) h[j] = j >= 8 - r.vocabulary ? __half_as_ushort(row[r.vocabulary - 8 + j]) : 0xFC00u;
   return uint4v{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
 }
-__device__ __forceinline__ uint4v tail_of(const Row &r, uint4v last, int tid) {
-  const int from = tid == THREADS - 1 ? 8 - (r.vocabulary & 7) : 8;
-  auto two = [&](unsigned w, int j) { return (j >= from ? w & 0xffff : 0xFC00u) | (j + 1 >= from ? w & 0xffff0000u : 0xFC000000u); };
-  return uint4v{two(last.x, 0), two(last.y, 2), two(last.z, 4), two(last.w, 6)};
+__device__ __forceinline__ int behind(const Row &r) { return r.vocabulary - r.head - r.vectors * 8; }
+__device__ __forceinline__ uint4v ends_of(const Row &r, uint4v read, int tid) {
+  const int from = tid == THREADS - 1 ? 8 - behind(r) : tid ? 8 : 0, to = tid ? 8 : r.head;
+  auto two = [&](unsigned w, int j) { return (j >= from && j < to ? w & 0xffff : 0xFC00u) | (j + 1 >= from && j + 1 < to ? w & 0xffff0000u : 0xFC000000u); };
+  return uint4v{two(read.x, 0), two(read.y, 2), two(read.z, 4), two(read.w, 6)};
 }
+__device__ __forceinline__ bool has_end(const Row &r, int tid) { return (tid == 0 && r.head) || (tid == THREADS - 1 && behind(r)); }
 // The first HELD of a lane's vectors stay in registers.
 template <int HELD>
 struct Held {
@@ -179,13 +189,13 @@ struct Drawer {
   // Counts the row (WIDE: its numbers of one sign; zeros are positive); -> of this thread's numbers, those that are finite (WIDE: or infinite and positive), and the largest ones of either half.
   template <int HELD>
   __device__ __forceinline__ unsigned count(bool negative, half2v &largest, Held<HELD> &held) {
-    const Walk of_wave = walk_of(0, r.vocabulary / 8, wave);
-    const uint4v last = last8(r);
+    const Walk of_wave = walk_of(0, r.vectors, wave);
+    const uint4v ends = ends_read(r, tid);
     if constexpr (HELD > 0) {
       // (all of them, the last one in place of those behind it: of conditional loads the compiler would wait for all in front of the first use)
-      if (r.vocabulary >= 8) {
+      if (r.vectors > 0) {
 #pragma unroll
-        for (int u = 0; u < HELD; ++u) held.x[u] = load8(r, min(of_wave.begin + u * 64 + lane, r.vocabulary / 8 - 1));
+        for (int u = 0; u < HELD; ++u) held.x[u] = load8(r, min(of_wave.begin + u * 64 + lane, r.vectors - 1));
       }
     }
     uint4v *all = reinterpret_cast<uint4v *>(words);
@@ -247,7 +257,7 @@ struct Drawer {
     } else {
       walk<WIDE ? 2 : 8>(r, of_wave, lane, one);
     }
-    if ((r.vocabulary & 7) && tid == THREADS - 1) one(tail_of(r, last, tid));
+    if (has_end(r, tid)) one(ends_of(r, ends, tid));
     largest_size = max(largest_sizes.x, largest_sizes.y);
     return valid - infinities.x - infinities.y;
   }
@@ -402,7 +412,7 @@ struct Drawer {
       auto flush = [&] {
         if (n) atomicAdd(&s.counts[of], n);
       };
-      walk<1>(r, walk_of(0, r.vocabulary / 8, wave), lane, [&](uint4v x) {
+      auto one = [&](uint4v x) {
 #pragma unroll 1
         for (int j = 0; j < 8; ++j) {
           const unsigned bits = half_at(x, j);
@@ -416,7 +426,9 @@ struct Drawer {
           }
           ++n;
         }
-      });
+      };
+      walk<1>(r, walk_of(0, r.vectors, wave), lane, one);
+      if (has_end(r, tid)) one(ends_of(r, ends_read(r, tid), tid));
       flush();
       __syncthreads();
       v.n = s.counts[p.i];
@@ -529,6 +541,9 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
   Row r;
   r.logits = p.logits + row * p.ld;
   r.vocabulary = p.vocabulary;
+  r.head = p.vocabulary < 16 ? 0 : (int)(-((unsigned)(size_t)r.logits >> 1) & 7);
+  r.logits += r.head;
+  r.vectors = (r.vocabulary - r.head) / 8;
   r.temperature = p.temperatures ? p.temperatures[row] : p.temperature;
   r.top_k = p.top_ks ? p.top_ks[row] : p.top_k;
   r.top_p = p.top_ps ? p.top_ps[row] : p.top_p;
@@ -657,30 +672,38 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
     while (of < WAVES - 1 && s.found[of] <= nth) nth -= s.found[of++];
     return of;
   };
-  const uint4v tail = tail_of(r, last8(r), tid);                              // (again: it would take four registers all the way)
-  int first = 0, vectors = p.vocabulary / 8;
+  const uint4v ends = ends_of(r, ends_read(r, tid), tid);                     // (again: they would take four registers all the way)
+  const unsigned at_end = matches(ends);
+  const int at_front = (int)of_lane(at_end, 0), behind_all = (int)of_lane(at_end, 63);      // (of the first wave and of the last)
+  int first = 0, vectors = r.vectors;
   if constexpr (HELD > 0) {
     const Walk w = walk_of(first, vectors, wave);
     unsigned n = 0;
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
       if (w.begin + u * 64 + lane < w.end) n += matches(held.x[u]);
-    n += matches(tail);
+    n += at_end;
     if (wave != wave_with_nth(of_lane(sums_of(n), 63))) return;
+    if (wave == 0) {
+      if (nth < at_front) {
+        if (tid == 0) write(ends, nth, 0);
+        return;
+      }
+      nth -= at_front;
+    }
 #pragma unroll
     for (int u = 0; u < HELD; ++u) {
       if (w.begin + u * 64 >= w.end) break;
       const unsigned here = w.begin + u * 64 + lane < w.end ? matches(held.x[u]) : 0;
       if (!__ballot(here != 0)) continue;
       const unsigned up_to = sums_of(here);
-      if ((int)up_to > nth && (int)(up_to - here) <= nth) write(held.x[u], nth - (int)(up_to - here), (w.begin + u * 64 + lane) * 8);
+      if ((int)up_to > nth && (int)(up_to - here) <= nth) write(held.x[u], nth - (int)(up_to - here), r.head + (w.begin + u * 64 + lane) * 8);
       nth -= (int)of_lane(up_to, 63);
       if (nth < 0) return;
     }
-    if (tid == THREADS - 1) write(tail, nth, p.vocabulary - 8);
+    if (tid == THREADS - 1) write(ends, nth, p.vocabulary - 8);
   } else {
     // the wave in whose part of the row it is, the part of that, the lane
-    const int of_tail = (int)of_lane(matches(tail), 63);             // (of the last wave's last lane)
     for (bool whole = true;; whole = false) {
       const Walk w = walk_of(first, vectors, wave);
       unsigned n = 0;
@@ -690,14 +713,22 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
         n += matches(x);
       });
       const unsigned up_to = sums_of(n);
-      if (whole && wave == WAVES - 1 && lane == 0) s.of_tail = of_tail;
-      const int of = wave_with_nth(of_lane(up_to, 63) + (whole ? of_tail : 0));
-      if (whole && of == WAVES - 1 && nth >= s.found[of] - s.of_tail) {      // behind the whole vectors
-        if (tid == THREADS - 1) write(tail, nth - (s.found[of] - s.of_tail), p.vocabulary - 8);
+      if (whole && tid == 0) s.at_front = at_front;
+      if (whole && tid == THREADS - 1) s.behind_all = behind_all;
+      const int of = wave_with_nth(of_lane(up_to, 63) + (whole ? at_front + behind_all : 0));
+      if (whole && of == 0) {
+        if (nth < s.at_front) {
+          if (tid == 0) write(ends, nth, 0);
+          return;
+        }
+        nth -= s.at_front;
+      }
+      if (whole && of == WAVES - 1 && nth >= s.found[of] - s.behind_all) {
+        if (tid == THREADS - 1) write(ends, nth - (s.found[of] - s.behind_all), p.vocabulary - 8);
         return;
       }
       if (vectors <= WAVES * 64) {                                  // one vector to a lane
-        if (wave == of && (int)up_to > nth && (int)(up_to - n) <= nth) write(mine, nth - (int)(up_to - n), (w.begin + lane) * 8);
+        if (wave == of && (int)up_to > nth && (int)(up_to - n) <= nth) write(mine, nth - (int)(up_to - n), r.head + (w.begin + lane) * 8);
         return;
       }
       const Walk there = walk_of(first, vectors, of);
@@ -710,12 +741,14 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleParams p) {
 }  // namespace
 
 int launch_sample(const SampleParams &p, int rows, hipStream_t s) {
-  // As many registers as the row needs, for rows that fit them.
+  // As many registers as the row needs, for rows that fit them: 20 rows of 32000 logits 12.7 us with 4 vectors a lane; of 32776 13.7 with 8 and 15.3 with 16; of 65536 15.9 and 17.3; of
+  // 131072 22.4 with 16, of 131080, read twice, 25.1.
   VQ_ALLOW_FULL_LDS(sample_kernel<4>);
+  VQ_ALLOW_FULL_LDS(sample_kernel<8>);
   VQ_ALLOW_FULL_LDS(sample_kernel<16>);
   VQ_ALLOW_FULL_LDS(sample_kernel<0>);
   constexpr int EACH = 8 * THREADS;
-  auto kernel = p.vocabulary <= 4 * EACH ? sample_kernel<4> : p.vocabulary <= 16 * EACH ? sample_kernel<16> : sample_kernel<0>;
+  auto kernel = p.vocabulary <= 4 * EACH ? sample_kernel<4> : p.vocabulary <= 8 * EACH ? sample_kernel<8> : p.vocabulary <= 16 * EACH ? sample_kernel<16> : sample_kernel<0>;
   constexpr int MOST = 1 << 21;                                     // rows of a launch (a grid has fewer than 2^32 threads)
   for (int row0 = 0; row0 < rows; row0 += MOST) {
     SampleParams q = p;

@@ -124,6 +124,37 @@ def test_values_that_occur_more_than_65535_times(gpu_lib):
         _check(gpu_lib, logits, rng.random(len(rows), dtype=np.float32), **how)
 
 
+@pytest.mark.parametrize("n", [15, 16, 17, 70003, 140008, 140015])
+def test_first_and_last_of_equal_logits(gpu_lib, n):
+    """Each of the first and last tokens of a row of equal logits, at each distance from sixteen bytes."""
+    import torch
+    asked = np.array(sorted({i % n for i in range(-17, 17)}))
+    uniform = ((asked + 0.5) / n).astype(np.float32)
+    wide = torch.full((len(asked), n + 16), 3.0, dtype=torch.float16, device="cuda")
+    for first in range(8):
+        for how in (dict(), dict(temperature=0.25, top_p=1.0 - 2.0 ** -24)):
+            token, p = gpu_lib.sample(wide[:, first: first + n], torch.from_numpy(uniform).cuda(), return_prob=True, **how)
+            assert token.tolist() == asked.tolist(), (first, how)
+            assert np.abs(p.cpu().numpy() * n - 1).max() <= 2.0 ** -22        # (binary32, rounded once, and this product)
+
+
+@pytest.mark.parametrize("n", [129, 4000, 40005, 131100])
+def test_where_vectors_begin(gpu_lib, n):
+    """Rows at each distance from sixteen bytes, with what lies around them larger than anything in them."""
+    import torch
+    rng = np.random.default_rng(n)
+    wide = torch.full((4, n + 17), 60000.0, dtype=torch.float16, device="cuda")
+    for first in range(9):
+        wide.fill_(60000.0)
+        view = wide[:, first: first + n]
+        x = _logits(rng, 4, n)
+        x[1, 0] = x[2, -1] = 20.0
+        x[3, 1:9] = x[3, -9:-1] = 17.0
+        view.copy_(torch.from_numpy(x))
+        for how in (dict(temperature=0.8), dict(top_k=12, top_p=0.97, min_p=0.001)):
+            _check(gpu_lib, view, rng.random(4, dtype=np.float32), **how)
+
+
 def test_logits_that_are_not_finite(gpu_lib):
     import torch
     rng = np.random.default_rng(6)
