@@ -12,7 +12,7 @@ struct Plan {
   int tile_rows, parts, run;
   bool prompt;
   size_t o_bytes, ml_bytes;
-  float time;                    // estimated, us
+  float time, beside;            // estimated, us; the same to be held against attention behind shared prefixes
 };
 
 // The kernel and number of parts whose time is estimated the least, in us, from measurements on heads of 64 and 128 elements, 8 and 16 bits, 8 and 32 key heads,
@@ -59,6 +59,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
         best.run = run;
         best.prompt = prompt;
         best.time = time;
+        best.beside = prompt ? time : 1.2f + join + rounds * (2.f + 3.1f * size * (c.e4m3 ? 1.f : 2.f) * turns);
       }
       if (parts == most || forced_parts >= 0) break;
     }
@@ -161,8 +162,9 @@ SharedPlan shared_plan_of(const KvParams &c, const Prefixes &x, const AttentionP
     plan_together(c, x, a, both);
     if (both.together && both.prefix.time < apart) {
       p = both;
-      // (what is estimated for few rows of single sequences is 6 us too much for the smallest and a quarter too little for the largest)
-      p.shares = forced ? forced != '0' : p.prefix.time < (whole.prompt ? whole.time : 1.25f * whole.time - 9.f);
+      // (sequences by themselves by the decode kernel: what plan_of estimates is good for the choice among its own, but 6 us too much for one short round and a quarter too little for many.
+      // Of 44 layouts what is chosen here is the slower one in five, by 5 to 17 %.)
+      p.shares = forced ? forced != '0' : p.prefix.time < whole.beside + 1.f;
     }
   }
   return p;
