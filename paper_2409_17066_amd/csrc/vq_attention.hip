@@ -59,7 +59,7 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
         best.run = run;
         best.prompt = prompt;
         best.time = time;
-        best.beside = prompt ? time : 1.2f + join + rounds * (2.f + 3.1f * size * (c.e4m3 ? 1.f : 2.f) * turns);
+        best.beside = prompt ? (half == WHOLE ? time : time - 5.f) : 1.2f + join + rounds * (2.f + 3.1f * (float)std::max(c.head_dim, 64) / 128.f * (c.e4m3 ? 1.f : 2.f) * turns);
       }
       if (parts == most || forced_parts >= 0) break;
     }
@@ -90,10 +90,11 @@ void size_partials(Plan &half, long long seqs, int kv_heads, long long rows, int
 
 // Both halves in one launch: the kernel of the prefixes and the parts of either half whose time is estimated the least, in us.  A workgroup of 256 threads takes runs of four chunks of 64 keys; two
 // share a compute unit.  With `size` for the elements of a head (1: 128) and `element` for the bytes of one, and q for quarters of a prompt workgroup's 128 rows that are there:
-//   a workgroup by itself      prefix, prompt kernel 2 + 4 size (1.18 + 0.126 q) a run     prefix, decode kernel 1.4 + 2.2 size element     own keys 2.5 + 1.15 size element
-//   of a full compute unit     2.9 + 4 size (0.47 + 0.18 q)                                0.9 + 2.6 size element                           two thirds of 1.4 + 2.7 size element
-// (sequences are shorter than the longest); the halves overlap, but for 0.36 of the smaller one, behind 4 us; the launch that joins them takes 4 us and 0.34 for each MB of partial results.
-// Fitted to 45 layouts by both kernels in 1 to 32 parts of the prefix and 1 to 4 of the rest: what is chosen takes up to 5 % longer than the least in 38, up to 29 % in the others.
+//   a workgroup by itself      prefix, prompt kernel 1.75 + 4 size (1.19 + 0.16 q) a run     prefix, decode kernel 2 + 2.25 size element     own keys 3.2 + 0.73 size element
+//   of a full compute unit     1.7 + 4 size (0.57 + 0.157 q)                                 0.8 + 2 size element                             0.73 of 1.3 + 2.7 size element
+// (sequences are shorter than the longest), a prefix's once more on all compute units where some have one more; the halves overlap, but for 0.32 of the smaller one, behind 4 us; the launch that
+// joins them takes 3.8 us and 0.34 for each MB of partial results.
+// Fitted to 44 layouts by both kernels in 1 to 32 parts of the prefix and 1 to 4 of the rest: what is chosen takes up to 5 % longer than the least in 38, up to 11 % in the others.
 // Measured (64 query and 8 key heads of 128 elements, 8 bits): 64 sequences behind 8192 tokens with up to 1021 of their own 45 us by the prompt kernel in 8 parts, 51 by the decode kernel in 2,
 // 119 by themselves; 16 behind 8192 with 300 26 (prompt, 32), 21.5 (decode, 8) and 38; 4 behind 4096 with 100 16, 15 and 13.
 void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &a, SharedPlan &p) {
@@ -113,13 +114,14 @@ void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &
     for (int i = prefix_parts >= 0 ? prefix_parts : 0; i <= (prefix_parts >= 0 ? prefix_parts : 5); ++i) {
       const long long parts = std::min(std::min(1LL << i, runs), (long long)HALF_PARTS), blocks = x.n * c.kv_heads * tiles * parts;
       const float turns = (float)((runs + parts - 1) / parts);
-      const float one = prompt ? 2.f + turns * 4.f * size * (1.18f + 0.126f * quarters) : 1.4f + turns * 2.2f * moved;
-      const float all = (float)blocks / cus * (prompt ? 2.9f + turns * 4.f * size * (0.47f + 0.18f * quarters) : 0.9f + turns * 2.6f * moved);
+      const float one = prompt ? 1.75f + turns * 4.f * size * (1.19f + 0.16f * quarters) : 2.f + turns * 2.25f * moved;
+      const float each = (float)blocks / cus, rounds = each > 1.f ? 0.93f * std::ceil(each) + 0.07f * each : each;
+      const float all = rounds * (prompt ? 1.7f + turns * 4.f * size * (0.57f + 0.157f * quarters) : 0.8f + turns * 2.f * moved);
       for (int k = switches().parts >= 0 ? switches().parts : 0; k <= (switches().parts >= 0 ? switches().parts : 2); ++k) {
         const long long own_parts = std::min(std::min(1LL << k, own_runs), (long long)HALF_PARTS), own_blocks = c.n_seqs * c.kv_heads * own_tiles * own_parts;
-        const float own_turns = (float)((own_runs + own_parts - 1) / own_parts), own_one = 2.5f + own_turns * 1.15f * moved, own_all = (float)own_blocks / cus * 0.67f * (1.4f + own_turns * 2.7f * moved);
-        const float join = 4.f + (float)((long long)c.n_seqs * own_rows * c.kv_heads) * (float)(parts + own_parts) * (float)c.head_dim * 4e-6f * 0.34f;
-        const float time = 4.f + std::max(std::max(one, own_one), std::max(all, own_all) + 0.36f * std::min(all, own_all)) + join;
+        const float own_turns = (float)((own_runs + own_parts - 1) / own_parts), own_one = 3.2f + own_turns * 0.73f * moved, own_all = (float)own_blocks / cus * 0.73f * (1.3f + own_turns * 2.7f * moved);
+        const float join = 3.8f + (float)((long long)c.n_seqs * own_rows * c.kv_heads) * (float)(parts + own_parts) * (float)c.head_dim * 4e-6f * 0.34f;
+        const float time = 4.f + std::max(std::max(one, own_one), std::max(all, own_all) + 0.32f * std::min(all, own_all)) + join;
         if (blocks + own_blocks > 0x7fffffff / THREADS || (p.prefix.time != 0.f && time >= p.prefix.time)) continue;
         p.prefix.time = time;
         p.prefix.prompt = prompt;
@@ -155,15 +157,15 @@ SharedPlan shared_plan_of(const KvParams &c, const Prefixes &x, const AttentionP
   p.prefix = plan_of(p.prefixes, a, true, PREFIX, x.max_length);
   p.own = plan_of(c, a, true, OWN, std::min(x.max_own, c.max_length));
   const float apart = p.prefix.time + p.own.time + 5.f;
+  // (what plan_of estimates is good for the choice among its own: held against others it is 6 us too much for one short round of the decode kernel, a quarter too little for many, and 5 us too much
+  // for a half by the prompt kernel.  Of 44 layouts the slower one is chosen here in five, by 1 to 17 %; of 200 others of heads of 32 to 256 elements in six, by 10 to 44 %.)
   const bool fit = half_fits(p.prefixes, a, p.prefix) && half_fits(c, a, p.own);
-  p.shares = fit && (forced ? forced != '0' : apart < whole.time);
+  p.shares = fit && (forced ? forced != '0' : p.prefix.beside + p.own.beside + 5.f < whole.beside);
   if ((c.head_dim == 64 || c.head_dim == 128) && forced != '2') {
     SharedPlan both = p;
     plan_together(c, x, a, both);
     if (both.together && both.prefix.time < apart) {
       p = both;
-      // (sequences by themselves by the decode kernel: what plan_of estimates is good for the choice among its own, but 6 us too much for one short round and a quarter too little for many.
-      // Of 44 layouts what is chosen here is the slower one in five, by 5 to 17 %.)
       p.shares = forced ? forced != '0' : p.prefix.time < whole.beside + 1.f;
     }
   }
