@@ -31,7 +31,7 @@ class Problem:
         gain = np.exp(rng.standard_normal((heads, dim)) * 0.5) * spread
 
         def rows(n):
-            return (rng.standard_normal((n, heads, dim)) * gain).astype(np.float16), rng.standard_normal((n, heads, dim)).astype(np.float16)
+            return (rng.standard_normal((n, heads, dim)) * gain).clip(-50000, 50000).astype(np.float16), rng.standard_normal((n, heads, dim)).astype(np.float16)
         for g, n in enumerate(commons):
             cache.append(*rows(n), self.prefix_table[g: g + 1], [n], [n])
         for b, (g, own, _) in enumerate(flat):
