@@ -49,8 +49,8 @@ int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const S
 int launch_attention_prompt(const KvParams &c, const AttentionParams &a, const Split &s, const Prefixes &x, Half half, hipStream_t stream);
 // Attention behind shared prefixes (vq_attention_shared.hip).  Parts of either half, at most: a launch joins those of both.
 constexpr int HALF_PARTS = 32;
-// Both halves in one launch: a prefix of which either kernel takes tiles beside sequences of which the decode kernel does, of heads of 64 or 128 elements; whether it takes them, and
-// waves of a workgroup of the decode kernel.
+// Both halves in one launch, for heads of 64 or 128 elements: prefixes of which either kernel takes tiles (`prompt`: that one) beside sequences of which the decode kernel does, in workgroups of so
+// many waves.
 constexpr int HALVES_WAVES = THREADS / 64;
 struct HalvesGrid {
   int prefix_blocks, own_blocks, first;      // workgroups; so many of the prefix's come in front of the others'
