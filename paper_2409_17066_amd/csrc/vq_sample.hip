@@ -493,17 +493,18 @@ struct Drawer {
     const double n = fmin(fmax(BEHIND ? ceil(ahead) - 1.0 : floor(ahead), 0.0), (double)of_lane(v.n, i) - 1.0);
     return border_at(entry, v, i, (int)n + BEHIND);
   }
-  // In front of the first value that weighs less than min_p: about max + T log(min_p), and which of 64 there by their weights.
+  // In front of the first value that weighs less than min_p: among every 1024th one, every sixteenth of those in front of that, each of those in front of that.  By the weights themselves: around
+  // max + T log(min_p) it is not to be looked for, as at high temperatures any number of weights round to the same (all of them to 1, which min_p = 1 keeps).
   __device__ __forceinline__ Border below_min_p() {
-    const double x = top + log((double)r.min_p) / per;
-    if (!(x > -65504.0)) return end();
-    const int about = order_of(place_of(__half_as_ushort(__float2half_rn((float)x)))) - 32 + lane;
-    static_assert(RUN == 32, "");
-    const bool below = about >= 0 && (about >= ENTRIES * RUN || weight(bits_of(Place{about >> 5, about & (RUN - 1)})) < (double)r.min_p);
-    const unsigned long long b = __ballot(below);
-    const int first = about - lane + (b ? (int)__builtin_ctzll(b) : 64);
-    if (first >= ENTRIES * RUN) return end();
-    return border_at(first >> 5, values_of(first >> 5), first & (RUN - 1), 0);
+    constexpr int VALUES = ENTRIES * RUN, FAR = 1024, NEAR = 16;
+    static_assert(VALUES <= 63 * FAR && FAR == 64 * NEAR, "three steps of 64 lanes");
+    auto below = [&](int order) { return order >= VALUES || weight(bits_of(Place{order / RUN, order % RUN})) < (double)r.min_p; };
+    // (the largest number is never below, as no weight is more than 1 and min_p at most that; behind the values everything is)
+    const int far_end = (int)__builtin_ctzll(__ballot(lane > 0 && below(lane * FAR))) * FAR;
+    const int near_end = far_end - FAR + ((int)__builtin_ctzll(__ballot(lane == 63 || below(far_end - FAR + (lane + 1) * NEAR))) + 1) * NEAR;
+    const int first = near_end - NEAR + (int)__builtin_ctzll(__ballot(lane >= NEAR - 1 || below(near_end - NEAR + lane + 1))) + 1;
+    if (first >= VALUES) return end();
+    return border_at(first / RUN, values_of(first / RUN), first % RUN, 0);
   }
 
   // What top_k and top_p keep.

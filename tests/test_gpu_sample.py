@@ -233,3 +233,16 @@ def test_what_the_package_refuses(gpu_lib):
             gpu_lib.sample(**dict(dict(logits=x, uniform=u), **bad))
     with pytest.raises(gpu_lib.VQError):
         gpu_lib.sample(x[:0], u[:0])
+
+
+def test_min_p_where_many_weights_are_alike(gpu_lib):
+    """Temperatures at which weights far apart in the order of the values are still within min_p of one another: up to all of them, where every weight rounds to 1 in binary64."""
+    import torch
+    rng = np.random.default_rng(10)
+    n = 3001
+    x = np.concatenate([_logits(rng, 2, n), rng.uniform(-30000, 30000, (2, n)).astype(np.float16), (rng.standard_normal((2, n)) * 1e-4).astype(np.float16)])
+    long = np.concatenate([np.full((6, 70000), -65504, np.float16), x], 1)         # (counted in 32 bits)
+    for logits in (torch.from_numpy(x).cuda(), torch.from_numpy(long).cuda()):
+        for how in (dict(temperature=1e30, min_p=1.0), dict(temperature=3e38, min_p=7.0), dict(temperature=1e25, min_p=1 - 2.0 ** -24), dict(temperature=1e30, min_p=1.0, top_k=2000),
+                    dict(temperature=1e30, min_p=1.0, top_p=0.7), dict(temperature=1e10, min_p=1 - 2.0 ** -24), dict(temperature=1e6, min_p=0.997), dict(temperature=1e-30, min_p=1e-38)):
+            _check(gpu_lib, logits, rng.random(6, dtype=np.float32), **how)
