@@ -429,7 +429,7 @@ static int make_prefixes(const vq_prefix_desc *d, const KvParams &c, Prefixes *x
   if (!d->lengths || (!d->page_table && d->table_pages)) return VQ_ERR_NULL;
   if (!aligned(d->lengths, 4) || !aligned(d->page_table, 4) || !aligned(d->members, 4)) return VQ_ERR_ALIGNMENT;
   *x = Prefixes{};
-  x->n = d->n_prefixes; x->most = std::min(d->max_members, c.n_seqs); x->max_length = d->max_length; x->max_own = std::min(d->max_own, c.max_length);
+  x->n = d->n_prefixes; x->most = std::min(d->max_members, c.n_seqs); x->max_length = std::min(d->max_length, c.max_length); x->max_own = std::min(d->max_own, c.max_length);
   x->n_seqs = c.n_seqs; x->table_pages = d->table_pages; x->table_stride = d->table_stride;
   x->rows_most = (int)std::min<long long>((long long)x->most * c.max_new, c.n_tokens);
   x->page_table = d->page_table; x->lengths = d->lengths; x->members = d->members;

@@ -241,3 +241,19 @@ def test_what_the_package_refuses(gpu_lib):
     for bad in (dict(max_prefix=10 ** 6), dict(max_members=0), dict(max_own=-1), dict(max_prefix=-1), dict(scale=-1.0)):
         with pytest.raises(gpu_lib.VQError):
             gpu_lib.attention_shared(**dict(good, **bad))
+
+
+@pytest.mark.parametrize("switches", ["shared=0", "shared=1", "shared=1,prefix=p", "shared=2"])
+def test_tokens_beyond_max_length_are_left_out(gpu_lib, monkeypatch, switches):
+    """A bound of the sequences' lengths inside of the prefix: what the prefix has behind it is seen by no token, as in vq_attention."""
+    import torch
+    monkeypatch.setenv("VQ_SWITCHES", switches)
+    p = Problem(29, [(256, 256, [(30, 1), (100, 1), (2, 1)])], [(150, 1)], 8, 2, 128, 16, 8)
+    dev, prefix = p.up()
+    table = p.table.copy()
+    table[:, 192 // 16:] = -1
+    want = ref.attention(p.q, p.cache, table, p.lengths, p.news, p.dim ** -0.5)
+    out, lse = gpu_lib.attention_shared(torch.from_numpy(p.q).cuda(), dev.k, dev.v, dev.table, dev.lengths, k_scales=dev.k_scales, v_scales=dev.v_scales, return_lse=True, max_length=192,
+                                        max_prefix=256, **prefix)
+    torch.cuda.synchronize()
+    _check(out.cpu().numpy(), lse.cpu().numpy(), *want, p.dim)
