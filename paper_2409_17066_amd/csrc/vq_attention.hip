@@ -106,23 +106,24 @@ void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &
   const long long own_tiles = (own_rows + own_tile - 1) / own_tile;
   const char kernel = switches().prefix ? switches().prefix : switches().attention;
   const int prefix_parts = switches().prefix_parts >= 0 ? switches().prefix_parts : switches().parts;
+  constexpr long long most = 0x7fffffff / THREADS;               // workgroups of a launch
   p.prefix.time = 0.f;
   for (const bool prompt : {false, true}) {
     if ((kernel == 'd' || kernel == 'p') && prompt != (kernel == 'p')) continue;
     const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(p.prefixes, a, true);
     const long long tiles = (rows + tile - 1) / tile;
     for (int i = prefix_parts >= 0 ? prefix_parts : 0; i <= (prefix_parts >= 0 ? prefix_parts : 5); ++i) {
-      const long long parts = std::min(std::min(1LL << i, runs), (long long)HALF_PARTS), blocks = x.n * c.kv_heads * tiles * parts;
+      const long long parts = std::min(std::min(1LL << i, runs), (long long)HALF_PARTS), blocks = (long long)x.n * c.kv_heads * tiles * parts;
       const float turns = (float)((runs + parts - 1) / parts);
       const float one = prompt ? 1.75f + turns * 4.f * size * (1.19f + 0.16f * quarters) : 2.f + turns * 2.25f * moved;
       const float each = (float)blocks / cus, rounds = each > 1.f ? 0.93f * std::ceil(each) + 0.07f * each : each;
       const float all = rounds * (prompt ? 1.7f + turns * 4.f * size * (0.57f + 0.157f * quarters) : 0.8f + turns * 2.f * moved);
       for (int k = switches().parts >= 0 ? switches().parts : 0; k <= (switches().parts >= 0 ? switches().parts : 2); ++k) {
-        const long long own_parts = std::min(std::min(1LL << k, own_runs), (long long)HALF_PARTS), own_blocks = c.n_seqs * c.kv_heads * own_tiles * own_parts;
+        const long long own_parts = std::min(std::min(1LL << k, own_runs), (long long)HALF_PARTS), own_blocks = (long long)c.n_seqs * c.kv_heads * own_tiles * own_parts;
         const float own_turns = (float)((own_runs + own_parts - 1) / own_parts), own_one = 3.2f + own_turns * 0.73f * moved, own_all = (float)own_blocks / cus * 0.73f * (1.3f + own_turns * 2.7f * moved);
         const float join = 3.8f + (float)((long long)c.n_seqs * own_rows * c.kv_heads) * (float)(parts + own_parts) * (float)c.head_dim * 4e-6f * 0.34f;
         const float time = 4.f + std::max(std::max(one, own_one), std::max(all, own_all) + 0.32f * std::min(all, own_all)) + join;
-        if (blocks + own_blocks > 0x7fffffff / THREADS || (p.prefix.time != 0.f && time >= p.prefix.time)) continue;
+        if (blocks > most || own_blocks > most - blocks || (p.prefix.time != 0.f && time >= p.prefix.time)) continue;
         p.prefix.time = time;
         p.prefix.prompt = prompt;
         p.prefix.tile_rows = tile;

@@ -129,3 +129,10 @@ def test_rows_of_a_table(tmp_path, width):
     for call, answer in zip(calls, run(calls, tmp_path)):
         assert answer["status"] == 0
         check_grids(call, answer)
+
+
+def test_as_many_sequences_prefixes_and_key_heads_as_there_may_be(tmp_path):
+    calls = [shared(seqs=seqs, heads=65535, prefixes=prefixes, switches=switches) for seqs, prefixes in ((65535, 65535), (65535, 1), (2, 65535)) for switches in ("", "shared=1", "shared=1,prefix=p")]
+    for call, answer in zip(calls, run(calls, tmp_path)):
+        assert answer["status"] == 0 and not any("halves_kernel<true, 64" in launch["name"] for launch in answer["launches"]), answer
+        check_grids(call, answer)
