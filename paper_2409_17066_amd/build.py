@@ -18,7 +18,8 @@ SOURCES = ["vq_api.hip", "vq_dequant.hip", "vq_gemv.hip", "vq_gemv_fast.hip", "v
            "vq_attention_shared.hip", "vq_attention_halves_e4m3.hip", "vq_attention_halves_fp16.hip"]
 # packed-FP32 VALU forms are switched off for every device compile (they are not trusted on the test machines)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
-         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-command-line-argument"]
+         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-command-line-argument",
+         "-Werror=align-mismatch"]       # (a vector's address handed on as one that is aligned to all of it)
 # Kernels in these files load registers asynchronously from inline assembly and wait for them with counted
 # s_waitcnt.  The compiler does not know such a register is pending: if it spilled one, it would save the old
 # contents.  Their kernels must therefore not spill at all; the build reads the compiler's resource remarks.

@@ -12,13 +12,6 @@ namespace {
 
 constexpr int THREADS = 256, AHEAD = 4;
 
-// ONCE: written past the caches.
-template <bool ONCE, typename T>
-__device__ __forceinline__ void store(T *to, T x) {
-  if (ONCE) __builtin_nontemporal_store(x, to);
-  else *to = x;
-}
-
 // What a lane takes of a row.
 template <typename Stream>
 struct Piece;
@@ -46,7 +39,7 @@ struct Piece<__half> {
 __device__ __forceinline__ void store1(float *to, float e) { *to = e; }
 __device__ __forceinline__ void store1(__half *to, float e) { *to = __float2half_rn(e); }
 
-// 2^shift threads to a row, the workgroup's rows next to each other.
+// 2^shift threads to a row, the workgroup's rows next to each other.  ONCE: written past the caches.
 template <typename Stream, bool ONCE>
 __global__ __launch_bounds__(THREADS) void embed_kernel(const int *ids, int rows, const __half *table, long long ld, int vocabulary, int width, float scale, Stream *y,
                                                         long long ldy, int shift) {
@@ -60,7 +53,10 @@ __global__ __launch_bounds__(THREADS) void embed_kernel(const int *ids, int rows
   Stream *to = y + row * ldy;
   auto read = [&](int i) { return *reinterpret_cast<const typename P::Words *>(from + i); };
   auto write = [&](int i, typename P::Words w) {
-    store<ONCE>(reinterpret_cast<typename P::Out *>(to + i), there ? P::scaled(w, scale) : typename P::Out{0, 0, 0, 0});
+    // (stored here, where the type says how little its address may be aligned: a template's argument would be the type without)
+    typename P::Out *at = reinterpret_cast<typename P::Out *>(to + i), x = there ? P::scaled(w, scale) : typename P::Out{0, 0, 0, 0};
+    if (ONCE) __builtin_nontemporal_store(x, at);
+    else *at = x;
   };
   int i = (int)(threadIdx.x & ((1 << shift) - 1)) * N;
   for (; i + (AHEAD - 1) * step + N <= width; i += AHEAD * step) {

@@ -128,3 +128,14 @@ def test_files_with_loads_on_their_way_may_not_spill_and_are_audited():
     with_loads = {n for n in sources if any(_statements_with_loads_on_their_way(text[f]) for f in closure(n, set()))}
     assert len(with_loads) >= 8
     assert with_loads <= set(build.AUDITED) and with_loads <= set(build.NO_SPILL), sorted(with_loads - (set(build.AUDITED) & set(build.NO_SPILL)))
+
+
+def test_addresses_are_not_said_to_be_more_aligned_than_they_are():
+    """The operators around a serving step's layers take tensors that are aligned to their elements: no vector of them is accessed by a type that promises sixteen bytes."""
+    import subprocess
+    import build as native
+    assert "-Werror=align-mismatch" in native.FLAGS
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    for source in ("vq_embed.hip", "vq_sample.hip", "vq_attention_shared.hip"):
+        done = subprocess.run([hipcc] + native.FLAGS + ["-fsyntax-only", os.path.join(native.CSRC, source)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert done.returncode == 0, done.stdout

@@ -81,3 +81,37 @@ def test_what_the_package_refuses(gpu_lib):
     for bad in (dict(ids=ids[:0]), dict(scale=float("nan")), dict(scale=float("inf"))):
         with pytest.raises(gpu_lib.VQError):
             gpu_lib.embed(**dict(dict(ids=ids, table=table), **bad))
+
+
+@pytest.mark.parametrize("stream", ["fp16", "fp32"])
+@pytest.mark.parametrize("width", [4099, 4096])
+def test_results_of_more_than_the_caches_hold(gpu_lib, stream, width):
+    """Results of 192 MB and more are written past the caches: from addresses of no more than an element's alignment on, of odd widths too, with ids that name no row."""
+    import torch
+    kind, element = (torch.float16, 2) if stream == "fp16" else (torch.float32, 4)
+    rows, vocabulary = (192 << 20) // (width * element) + 5, 70
+    g = torch.Generator(device="cuda").manual_seed(width)
+    table = torch.randn((vocabulary, width + 1), device="cuda", generator=g).half()[:, 1:]
+    ids = torch.randint(-2, vocabulary + 2, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    there = (ids >= 0) & (ids < vocabulary)
+    want = torch.where(there[:, None], table[ids.clamp(0, vocabulary - 1).long()].float() * torch.tensor(0.3, dtype=torch.float32, device="cuda"), torch.zeros((), device="cuda")).to(kind)
+    out = torch.full((rows, width + 3), 7.0, dtype=kind, device="cuda")
+    got, given = gpu_lib.embed(ids, table, scale=0.3, dtype=kind), gpu_lib.embed(ids, table, scale=0.3, out=out[:, 1: 1 + width])
+    torch.cuda.synchronize()
+    bits = torch.int16 if stream == "fp16" else torch.int32
+    assert torch.equal(got.view(bits), want.view(bits)) and torch.equal(given.contiguous().view(bits), want.view(bits))
+    assert (out[:, 0] == 7).all() and (out[:, 1 + width:] == 7).all()
+
+
+@pytest.mark.parametrize("stream", ["fp16", "fp32"])
+def test_rows_of_the_result_past_32_bits(gpu_lib, stream):
+    import torch
+    kind = torch.float16 if stream == "fp16" else torch.float32
+    rows, width, pitch = 4, 100, (1 << 30) + 3
+    out = torch.empty((rows - 1) * pitch + width, dtype=kind, device="cuda").as_strided((rows, width), (pitch, 1))
+    table, ids = torch.randn((9, width), device="cuda").half(), torch.tensor([3, 8, 9, 1], dtype=torch.int32, device="cuda")
+    gpu_lib.embed(ids, table, out=out)
+    torch.cuda.synchronize()
+    want = table[ids.clamp(max=8).long()].to(kind)
+    want[2] = 0
+    assert torch.equal(out, want)
