@@ -372,7 +372,8 @@ typedef struct vq_prefix_desc {
   uint32_t struct_size;                    /* = sizeof(vq_prefix_desc)                                     */
   int32_t n_prefixes;                      /* 1 .. 65535                                                   */
   int32_t max_members, max_length;         /* sequences and tokens of one prefix, at most; max_length <= table_pages * page_tokens and 2^30 */
-  int32_t max_own;                         /* of a sequence's tokens behind its prefix, about (for the choice of kernels: more are looked at all the same) */
+  int32_t max_own;                         /* of a sequence's tokens behind its prefix, about (for the choice of kernels: more are looked at all the same; with a whole
+                                              sequence's length here every sequence by itself looks faster) */
   int32_t table_pages;                     /* entries of a row of page_table                               */
   const int32_t *page_table; int64_t table_stride;   /* [n_prefixes][table_stride]                         */
   const int32_t *lengths;                  /* [n_prefixes]                                                 */

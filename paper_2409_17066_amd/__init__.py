@@ -559,8 +559,10 @@ def attention_shared(q, k_pages, v_pages, page_table, lengths, prefix_table, pre
                      max_new=None, max_length=None, max_prefix=None, max_members=None, max_own=None, out=None, return_lse=False, workspace=None):
     """attention() of sequences that begin with the same tokens, whose attention to those is computed once for all.  prefix_table: int32 [prefixes][pages of one],
     prefix_lengths: int32 [prefixes], members: int32 [prefixes + 1], the first sequence of each prefix and the end of the last (None: one prefix, of all
-    sequences); page_table and lengths: the whole sequences, prefixes included, as for attention().  max_prefix, max_members, max_own: bounds of a prefix's length
-    and number of sequences, and about how much a sequence holds behind it (None: the tables' size, all, max_length).  The rest as for attention(), without a window."""
+    sequences); page_table and lengths: the whole sequences, prefixes included, as for attention().  max_length, max_prefix, max_members: bounds of a sequence's and of a prefix's length and of its
+    number of sequences (None: the tables' sizes, all sequences); max_own: about how much a sequence holds behind its prefix (None: max_length - max_prefix).  By these, not by what the
+    tensors hold, it is judged whether prefixes are computed once or every sequence by itself: a prefix table as wide as the sequences' leaves nothing to judge by, and one that is much
+    wider than its prefixes makes what lies behind them look short.  The rest as for attention(), without a window."""
     r = (_bound or _native()).attention_shared(k_pages, v_pages, page_table, lengths, k_scales, v_scales, starts, max_new, max_length, prefix_table, prefix_lengths,
                                                members, max_prefix, max_members, max_own, q, scale, out, return_lse, workspace)
     if r.__class__ is int:

@@ -473,7 +473,8 @@ PyObject *attention_shared(PyObject *, PyObject *const *args, Py_ssize_t n) {
   x.table_pages = narrow(table.size(1), "prefix_table");
   x.max_length = args[12] != Py_None ? whole(args[12], "max_prefix") : narrow(table.size(1) * d.page_tokens, "max_prefix");
   x.max_members = args[13] != Py_None ? whole(args[13], "max_members") : d.n_seqs;
-  x.max_own = args[14] != Py_None ? whole(args[14], "max_own") : d.max_length;
+  // (what the bounds of the lengths leave; where they say nothing of it, all: a prefix is not worth a launch of its own then)
+  x.max_own = args[14] != Py_None ? whole(args[14], "max_own") : x.max_length >= 0 && x.max_length < d.max_length ? std::max(d.max_length - x.max_length, d.max_new) : d.max_length;
   x.page_table = static_cast<const int32_t *>(table.data_ptr());
   x.table_stride = leading(table);
   x.lengths = static_cast<const int32_t *>(lengths.data_ptr());

@@ -257,3 +257,19 @@ def test_tokens_beyond_max_length_are_left_out(gpu_lib, monkeypatch, switches):
                                         max_prefix=256, **prefix)
     torch.cuda.synchronize()
     _check(out.cpu().numpy(), lse.cpu().numpy(), *want, p.dim)
+
+
+@pytest.mark.parametrize("prefixes,members,common,own", [(1, 16, 2048, 60)])
+def test_prefixes_are_computed_once_without_bounds(gpu_lib, monkeypatch, prefixes, members, common, own):
+    """Without max_own, max_members and max_prefix, which only the tables' sizes bound then, the results are those of the shared halves, bit for bit, and not vq_attention's."""
+    import torch
+    monkeypatch.setenv("VQ_SWITCHES", "")
+    p = Problem(30, [(common, common, [(own, 1)] * members)] * prefixes, [], 64, 8, 128, 16, 8)
+    dev, prefix = p.up()
+    q, cache, scales = torch.from_numpy(p.q).cuda(), (dev.k, dev.v, dev.table, dev.lengths), dict(k_scales=dev.k_scales, v_scales=dev.v_scales)
+    got, plain = gpu_lib.attention_shared(q, *cache, **scales, **prefix), gpu_lib.attention(q, *cache, **scales)
+    monkeypatch.setenv("VQ_SWITCHES", "shared=1")
+    length, of_prefix = (16 * t.shape[1] for t in (p.table, p.prefix_table))
+    shared = gpu_lib.attention_shared(q, *cache, **scales, **prefix, max_length=length, max_prefix=of_prefix, max_members=prefixes * members, max_own=length - of_prefix)
+    torch.cuda.synchronize()
+    assert torch.equal(got, shared) and not torch.equal(got, plain)
