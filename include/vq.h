@@ -371,7 +371,8 @@ int vq_attention(const vq_kv_desc *cache, const void *q, int64_t ldq, int32_t q_
 typedef struct vq_prefix_desc {
   uint32_t struct_size;                    /* = sizeof(vq_prefix_desc)                                     */
   int32_t n_prefixes;                      /* 1 .. 65535                                                   */
-  int32_t max_members, max_length;         /* sequences and tokens of one prefix, at most; max_length <= table_pages * page_tokens and 2^30 */
+  int32_t max_members, max_length;         /* sequences and tokens of one prefix, at most; max_length <= table_pages * page_tokens and 2^30; max_members may be all
+                                              (it bounds the launch; of several prefixes each is then judged by an even share of the new tokens) */
   int32_t max_own;                         /* of a sequence's tokens behind its prefix, about (for the choice of kernels: more are looked at all the same; with a whole
                                               sequence's length here every sequence by itself looks faster) */
   int32_t table_pages;                     /* entries of a row of page_table                               */

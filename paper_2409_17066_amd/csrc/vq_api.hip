@@ -432,6 +432,8 @@ static int make_prefixes(const vq_prefix_desc *d, const KvParams &c, Prefixes *x
   x->n = d->n_prefixes; x->most = std::min(d->max_members, c.n_seqs); x->max_length = std::min(d->max_length, c.max_length); x->max_own = std::min(d->max_own, c.max_length);
   x->n_seqs = c.n_seqs; x->table_pages = d->table_pages; x->table_stride = d->table_stride;
   x->rows_most = (int)std::min<long long>((long long)x->most * c.max_new, c.n_tokens);
+  x->partial_tokens = std::min((long long)x->n * x->rows_most, (long long)c.n_tokens);
+  x->by_token = (long long)x->n * x->rows_most > c.n_tokens;
   x->page_table = d->page_table; x->lengths = d->lengths; x->members = d->members;
   return VQ_OK;
 }

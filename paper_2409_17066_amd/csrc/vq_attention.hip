@@ -15,6 +15,14 @@ struct Plan {
   float time, beside;            // estimated, us; the same to be held against attention behind shared prefixes
 };
 
+// Rows that a prefix is taken to have, of up to `rows`: an even share of the call's.  Where max_members bounds little (by default each prefix may have all of the call's sequences) most
+// workgroups find no rows and end at once, of which a compute unit takes one in EMPTY us.  (Counted as work, ten prefixes of twelve sequences each without that bound were not computed once at all.
+// Measured, 4096 tokens each, 64 query and 8 key heads of 128 elements, 8 bits: 46.6 us with the bound, 47.0 without, 93 by themselves.)
+constexpr float EMPTY = 0.2f;
+long long even_rows(const KvParams &c, const AttentionParams &a, long long prefixes, long long rows) {
+  return std::min(rows, ((long long)c.n_tokens * a.group + prefixes - 1) / prefixes);
+}
+
 // The kernel and number of parts whose time is estimated the least, in us, from measurements on heads of 64 and 128 elements, 8 and 16 bits, 8 and 32 key heads,
 // 1 to 200 sequences of 15 to 32768 tokens with 1 to 4144 rows a key head (heads of other sizes count as the next multiple of 64, as the kernels take them; every sequence as the longest):
 //   decode: a workgroup of eight waves to a compute unit (more of smaller ones), rounds of 3.2 us for eight chunks of 16 KB behind 9 us;
@@ -28,7 +36,8 @@ struct Plan {
 // A prefix is a sequence all of whose rows see all of it; of what lies behind there are `length` keys at most.  Both always leave parts for another launch, which is not counted here.
 Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Half half, long long length) {
   Plan best{};
-  const long long rows = (long long)c.max_new * a.group, slots = cu_count();
+  const long long rows = (long long)c.max_new * a.group, slots = cu_count(), even = half == PREFIX ? even_rows(c, a, c.n_seqs, rows) : rows;
+  const long long all_rows = half == PREFIX ? std::min(c.n_seqs * rows, (long long)c.n_tokens * a.group) : c.n_seqs * rows;
   float least = 0.f;
   parts_allowed = parts_allowed && attention_join_takes(c, a);
   const int forced_parts = half == PREFIX && switches().prefix_parts >= 0 ? switches().prefix_parts : switches().parts;
@@ -39,8 +48,9 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
     const int tile = prompt ? attention_prompt_rows() : attention_decode_rows(c, a, half == PREFIX || c.max_new == 1), run = prompt ? PROMPT_RUN : attention_decode_run(c);
     // tokens that a tile's rows look at: a window's and the first ones, or on the average all before half of the new ones
     const long long all = length - (rows > tile && half != PREFIX ? c.max_new / 2 : 0), reach = a.window > 0 ? (long long)a.window + a.sinks + tile / a.group + 64 : all;
-    const long long chunks = (std::max(std::min(all, reach), 1LL) + 63) / 64, groups = (long long)c.n_seqs * c.kv_heads * ((rows + tile - 1) / tile);
-    const float quarters = (float)std::min((rows + 31) / 32, 4LL), size = (float)((c.head_dim + 63) / 64) / 2.f;
+    const long long chunks = (std::max(std::min(all, reach), 1LL) + 63) / 64;
+    const long long heads = (long long)c.n_seqs * c.kv_heads, all_groups = heads * ((rows + tile - 1) / tile), groups = heads * ((even + tile - 1) / tile);
+    const float quarters = (float)std::min((even + 31) / 32, 4LL), size = (float)((c.head_dim + 63) / 64) / 2.f;
     const long long most = parts_allowed ? std::min((chunks + run - 1) / run, half == WHOLE ? 64LL : (long long)HALF_PARTS) : 1;
     for (long long parts = 1;; parts *= 2) {
       if (forced_parts >= 0) parts = 1LL << forced_parts;
@@ -50,8 +60,9 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
       const float turns = parts > 1 ? (float)(((chunks + run - 1) / run + parts - 1) / parts) : prompt ? (float)chunks / (float)run : (float)((chunks + run - 1) / run);
       const float one = 1.2f + 0.1f * quarters, two = 0.7f + 0.6f * quarters, shared = std::min(std::max(work / alone - 1.f, 0.f), 1.f);
       const float step = !prompt ? 3.2f * size * (c.e4m3 ? 1.f : 2.f) : run * size * (one + (two - one) * shared);
-      const float join = parts > 1 ? (half == WHOLE ? 5.f : 0.f) + (float)((long long)c.n_seqs * c.kv_heads * rows) * (0.3e-3f + (float)parts * size * 1024.f / 4.5e6f) : 0.f;
-      const float time = (prompt ? 12.f + 5.f * size * (rounds - 1.f) : 9.f) + join + rounds * turns * step;
+      const float join = parts > 1 ? (half == WHOLE ? 5.f : 0.f) + (float)(c.kv_heads * all_rows) * (0.3e-3f + (float)parts * size * 1024.f / 4.5e6f) : 0.f;
+      const float empty = (float)((all_groups - groups) * parts) / (float)slots * EMPTY;
+      const float time = (prompt ? 12.f + 5.f * size * (rounds - 1.f) : 9.f) + join + rounds * turns * step + empty;
       if (least == 0.f || time < least) {
         least = time;
         best.tile_rows = tile;
@@ -59,14 +70,14 @@ Plan plan_of(const KvParams &c, const AttentionParams &a, bool parts_allowed, Ha
         best.run = run;
         best.prompt = prompt;
         best.time = time;
-        best.beside = prompt ? (half == WHOLE ? time : time - 5.f) : 1.2f + join + rounds * (2.f + 3.1f * (float)std::max(c.head_dim, 64) / 128.f * (c.e4m3 ? 1.f : 2.f) * turns);
+        best.beside = prompt ? (half == WHOLE ? time : time - 5.f) : 1.2f + empty + join + rounds * (2.f + 3.1f * (float)std::max(c.head_dim, 64) / 128.f * (c.e4m3 ? 1.f : 2.f) * turns);
       }
       if (parts == most || forced_parts >= 0) break;
     }
   }
   if (best.parts > 1 || half != WHOLE) {
-    best.o_bytes = (size_t)c.n_seqs * c.kv_heads * best.parts * rows * c.head_dim * 4;
-    best.ml_bytes = (size_t)c.n_seqs * c.kv_heads * best.parts * rows * 8;
+    best.o_bytes = (size_t)c.kv_heads * best.parts * all_rows * c.head_dim * 4;
+    best.ml_bytes = (size_t)c.kv_heads * best.parts * all_rows * 8;
   }
   return best;
 }
@@ -83,9 +94,9 @@ struct SharedPlan {
   size_t bytes() const { return bytes(prefix) + bytes(own); }
 };
 // What a half moves to the launch that joins them.
-void size_partials(Plan &half, long long seqs, int kv_heads, long long rows, int head_dim) {
-  half.o_bytes = (size_t)seqs * kv_heads * half.parts * rows * head_dim * 4;
-  half.ml_bytes = (size_t)seqs * kv_heads * half.parts * rows * 8;
+void size_partials(Plan &half, int kv_heads, long long rows, int head_dim) {
+  half.o_bytes = (size_t)kv_heads * half.parts * rows * head_dim * 4;
+  half.ml_bytes = (size_t)kv_heads * half.parts * rows * 8;
 }
 
 // Both halves in one launch: the kernel of the prefixes and the parts of either half whose time is estimated the least, in us.  A workgroup of 256 threads takes runs of four chunks of 64 keys; two
@@ -101,7 +112,8 @@ void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &
   const float size = (float)((c.head_dim + 63) / 64) / 2.f, moved = size * (c.e4m3 ? 1.f : 2.f), cus = (float)cu_count();
   const long long rows = (long long)x.rows_most * a.group, own_rows = (long long)c.max_new * a.group;
   const long long runs = std::max<long long>((x.max_length + 255) / 256, 1), own_runs = std::max<long long>((x.max_own + 255) / 256, 1);
-  const float quarters = (float)std::min((rows + 31) / 32, 4LL);
+  const long long even = even_rows(c, a, x.n, rows);
+  const float quarters = (float)std::min((even + 31) / 32, 4LL);
   const int own_tile = attention_decode_rows(c, a, c.max_new == 1);
   const long long own_tiles = (own_rows + own_tile - 1) / own_tile;
   const char kernel = switches().prefix ? switches().prefix : switches().attention;
@@ -114,10 +126,11 @@ void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &
     const long long tiles = (rows + tile - 1) / tile;
     for (int i = prefix_parts >= 0 ? prefix_parts : 0; i <= (prefix_parts >= 0 ? prefix_parts : 5); ++i) {
       const long long parts = std::min(std::min(1LL << i, runs), (long long)HALF_PARTS), blocks = (long long)x.n * c.kv_heads * tiles * parts;
+      const long long with_rows = (long long)x.n * c.kv_heads * ((even + tile - 1) / tile) * parts;
       const float turns = (float)((runs + parts - 1) / parts);
       const float one = prompt ? 1.75f + turns * 4.f * size * (1.19f + 0.16f * quarters) : 2.f + turns * 2.25f * moved;
-      const float each = (float)blocks / cus, rounds = each > 1.f ? 0.93f * std::ceil(each) + 0.07f * each : each;
-      const float all = rounds * (prompt ? 1.7f + turns * 4.f * size * (0.57f + 0.157f * quarters) : 0.8f + turns * 2.f * moved);
+      const float each = (float)with_rows / cus, rounds = each > 1.f ? 0.93f * std::ceil(each) + 0.07f * each : each;
+      const float all = rounds * (prompt ? 1.7f + turns * 4.f * size * (0.57f + 0.157f * quarters) : 0.8f + turns * 2.f * moved) + (float)(blocks - with_rows) / cus * EMPTY;
       for (int k = switches().parts >= 0 ? switches().parts : 0; k <= (switches().parts >= 0 ? switches().parts : 2); ++k) {
         const long long own_parts = std::min(std::min(1LL << k, own_runs), (long long)HALF_PARTS), own_blocks = (long long)c.n_seqs * c.kv_heads * own_tiles * own_parts;
         const float own_turns = (float)((own_runs + own_parts - 1) / own_parts), own_one = 3.2f + own_turns * 0.73f * moved, own_all = (float)own_blocks / cus * 0.73f * (1.3f + own_turns * 2.7f * moved);
@@ -129,15 +142,15 @@ void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &
         p.prefix.tile_rows = tile;
         p.prefix.parts = (int)parts;
         p.own.parts = (int)own_parts;
-        p.grid = HalvesGrid{(int)blocks, (int)own_blocks, (int)std::min(blocks, (long long)cu_count()), (int)tiles, (int)own_tiles, blocks <= 2 * cu_count()};
+        p.grid = HalvesGrid{(int)blocks, (int)own_blocks, (int)std::min(blocks, (long long)cu_count()), (int)tiles, (int)own_tiles, blocks <= 2 * cu_count() || x.by_token};
       }
     }
   }
   p.together = p.prefix.time != 0.f;
   p.prefix.run = p.own.run = HALVES_WAVES;
   p.own.tile_rows = own_tile;
-  size_partials(p.prefix, x.n, c.kv_heads, rows, c.head_dim);
-  size_partials(p.own, c.n_seqs, c.kv_heads, own_rows, c.head_dim);
+  size_partials(p.prefix, c.kv_heads, x.partial_tokens * a.group, c.head_dim);
+  size_partials(p.own, c.kv_heads, c.n_seqs * own_rows, c.head_dim);
 }
 
 // (a call is launched whole or refused: a launch that a grid has no room for, and partial results whose bytes 64 bits do not count, are found before the first launch)

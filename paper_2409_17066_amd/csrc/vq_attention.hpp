@@ -21,7 +21,7 @@ PrefixesOf<HALF> prefixes_of(const Prefixes &x) {
 // looks at first does not depend on the sequence's length.
 struct Split {
   int parts, run;
-  float *o, *ml;               // partial outputs [seq][kv head][part][row][head_dim], maxima and sums [seq][kv head][part][row][2]
+  float *o, *ml;               // partial outputs [seq][kv head][part][row][head_dim], maxima and sums [seq][kv head][part][row][2]; of prefixes [kv head][part][row of all of them]
 };
 
 // Chunks of a run, one for each wave of the decode kernel.
@@ -110,6 +110,8 @@ __device__ __forceinline__ Behind behind(const KvParams &c, const Prefixes &x, c
   }
   return h;
 }
+// Where the partial results of a prefix's rows begin in those of a key head's part: row0 is the prefix's first row (of the call's), g its number.
+__device__ __forceinline__ long long prefix_partials(const Prefixes &x, int g, int row0) { return x.by_token ? row0 : (long long)g * x.rows_most; }
 template <Half HALF>
 __device__ __forceinline__ Sequence sequence_of(const KvParams &c, const PrefixesOf<HALF> &x, int b) {
   if constexpr (HALF == WHOLE) return sequence(c, b);

@@ -28,7 +28,7 @@ int launch(const KvParams &c, const AttentionParams &a, const Split &s, const Pr
   const int tiles = (c.max_new * a.group + ROWS - 1) / ROWS;
   const long long blocks = (long long)c.n_seqs * c.kv_heads * tiles * s.parts;
   if (blocks > 0xffffffffll / THREADS) return VQ_ERR_SHAPE;        // (threads of a grid)
-  const int lds = prompt_lds_bytes(E4M3, D), zigzag = blocks <= 2 * cu_count();
+  const int lds = prompt_lds_bytes(E4M3, D), zigzag = blocks <= 2 * cu_count() || (HALF == PREFIX && x.by_token);
   VQ_ALLOW_FULL_LDS((attention_prompt_kernel<E4M3, D, EXACT, HALF>));
   hipLaunchKernelGGL((attention_prompt_kernel<E4M3, D, EXACT, HALF>), dim3((unsigned)blocks), dim3(THREADS), lds, stream, c, a, s, tiles, zigzag, prefixes_of<HALF>(x));
   return hipGetLastError() == hipSuccess ? VQ_OK : VQ_ERR_HIP;

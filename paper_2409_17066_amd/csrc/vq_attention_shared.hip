@@ -27,7 +27,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void attention_join_halves_kernel(con
   const int before = h.prefix < 0 ? 0 : parts_of(prefix, (h.length + 63) >> 6);
   const int parts = there ? before + parts_of(own, span_of<OWN>(a, behind_prefix, of_head / own_tile_rows * own_tile_rows, own_tile_rows).chunks) : 0;
   const long long own_most = (long long)c.max_new * a.group, own_from = ((long long)b * c.kv_heads + kv_head) * own.parts * own_most + of_head;
-  const long long prefix_most = (long long)x.rows_most * a.group, prefix_from = ((long long)max(h.prefix, 0) * c.kv_heads + kv_head) * prefix.parts * prefix_most + (long long)h.row * a.group + of_head;
+  const long long prefix_most = x.partial_tokens * a.group, prefix_from = (long long)kv_head * prefix.parts * prefix_most + (prefix_partials(x, max(h.prefix, 0), s.row0 - h.row) + h.row) * a.group + of_head;
   auto from = [&](int w) { return w < before ? prefix_from + w * prefix_most : own_from + (long long)(w - before) * own_most; };
   float2v ml[EACH];
 #pragma unroll

@@ -44,6 +44,8 @@ struct Prefixes {
   int n, most, max_length, max_own;  // prefixes; sequences of one, tokens of one and of what a sequence holds behind its own, at most
   int n_seqs, table_pages;           // sequences of the call; entries of a row of page_table
   int rows_most;                     // new tokens of one prefix's sequences, at most
+  int by_token;                      // partial results lie where the call's new tokens do, or each prefix's behind the other's: what needs less
+  long long partial_tokens;          // new tokens that these have room for, n_tokens or n * rows_most
   const int *page_table, *lengths, *members;
   long long table_stride;
 };

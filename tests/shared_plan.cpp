@@ -57,6 +57,8 @@ int main(int, char **argv) {
   x.max_length = atoi(argv[5]);
   x.max_own = atoi(argv[6]);
   x.rows_most = c.n_tokens;
+  x.by_token = x.n > 1;
+  x.partial_tokens = c.n_tokens;
   vq::AttentionParams a{};
   a.group = 1;
   a.q_heads = c.kv_heads;

@@ -259,7 +259,7 @@ def test_tokens_beyond_max_length_are_left_out(gpu_lib, monkeypatch, switches):
     _check(out.cpu().numpy(), lse.cpu().numpy(), *want, p.dim)
 
 
-@pytest.mark.parametrize("prefixes,members,common,own", [(1, 16, 2048, 60)])
+@pytest.mark.parametrize("prefixes,members,common,own", [(1, 16, 2048, 60), (3, 12, 2048, 50), (10, 6, 1024, 20)])
 def test_prefixes_are_computed_once_without_bounds(gpu_lib, monkeypatch, prefixes, members, common, own):
     """Without max_own, max_members and max_prefix, which only the tables' sizes bound then, the results are those of the shared halves, bit for bit, and not vq_attention's."""
     import torch

@@ -136,3 +136,12 @@ def test_as_many_sequences_prefixes_and_key_heads_as_there_may_be(tmp_path):
     for call, answer in zip(calls, run(calls, tmp_path)):
         assert answer["status"] == 0 and not any("halves_kernel<true, 64" in launch["name"] for launch in answer["launches"]), answer
         check_grids(call, answer)
+
+
+@pytest.mark.parametrize("prefixes,members,length,own", [(2, 30, 8192, 300), (3, 8, 2048, 50), (10, 12, 4096, 104), (32, 8, 2048, 100)])
+def test_sequences_of_a_prefix_without_a_bound(tmp_path, prefixes, members, length, own):
+    """Each prefix may have all of the call's sequences: they are computed once all the same, and their partial results take no more room than the call's rows."""
+    layout = dict(seqs=prefixes * members, heads=8, group=8, dim=128, length=length + own, prefixes=prefixes, prefix_length=length, own=own)
+    free, bound, free_in_parts, bound_in_parts = run([shared(**layout, members=m, switches=s) for s in ("", "shared=1,prefix=d,prefix_parts=2,parts=0") for m in (None, members)], tmp_path)
+    assert all(len(a["launches"]) == 2 and "halves" in a["launches"][0]["name"] for a in (free, bound)), (free, bound)
+    assert free_in_parts["asked"] == bound_in_parts["asked"] > 0
