@@ -105,7 +105,8 @@ void size_partials(Plan &half, int kv_heads, long long rows, int head_dim) {
 //   of a full compute unit     1.7 + 4 size (0.57 + 0.157 q)                                 0.8 + 2 size element                             0.73 of 1.3 + 2.7 size element
 // (sequences are shorter than the longest), a prefix's once more on all compute units where some have one more; the halves overlap, but for 0.32 of the smaller one, behind 4 us; the launch that
 // joins them takes 3.8 us and 0.34 for each MB of partial results.
-// Fitted to 44 layouts by both kernels in 1 to 32 parts of the prefix and 1 to 4 of the rest: what is chosen takes up to 5 % longer than the least in 38, up to 11 % in the others.
+// Fitted to 44 layouts by both kernels in 1 to 32 parts of the prefix and 1 to 4 of the rest.  Of the 60 in the first table of profiles/shared_plan.txt, these among them, what is chosen takes up to 5 % longer
+// than the least in 49, up to 10 % in 55, up to 19 % in the others.
 // Measured (64 query and 8 key heads of 128 elements, 8 bits): 64 sequences behind 8192 tokens with up to 1021 of their own 45 us by the prompt kernel in 8 parts, 51 by the decode kernel in 2,
 // 119 by themselves; 16 behind 8192 with 300 26 (prompt, 32), 21.5 (decode, 8) and 38; 4 behind 4096 with 100 16, 15 and 13.
 void plan_together(const KvParams &c, const Prefixes &x, const AttentionParams &a, SharedPlan &p) {
@@ -172,7 +173,8 @@ SharedPlan shared_plan_of(const KvParams &c, const Prefixes &x, const AttentionP
   p.own = plan_of(c, a, true, OWN, std::min(x.max_own, c.max_length));
   const float apart = p.prefix.time + p.own.time + 5.f;
   // (what plan_of estimates is good for the choice among its own: held against others it is 6 us too much for one short round of the decode kernel, a quarter too little for many, and 5 us too much
-  // for a half by the prompt kernel.  Of 44 layouts the slower one is chosen here in five, by 1 to 17 %; of 200 others of heads of 32 to 256 elements in six, by 10 to 44 %.)
+  // for a half by the prompt kernel.  Of 44 layouts the slower one is chosen here in five, by 1 to 17 %.  Of 200 others of heads of 32 to 256 elements, drawn at random, which profiles/shared_plan.txt
+  // lists, what is chosen takes up to 5 % longer than the least of all ways in 158, up to 20 % in 185, and up to 56 % in the others, of which ten are calls of 9 to 17 us.)
   const bool fit = half_fits(p.prefixes, a, p.prefix) && half_fits(c, a, p.own);
   p.shares = fit && (forced ? forced != '0' : p.prefix.beside + p.own.beside + 5.f < whole.beside);
   if ((c.head_dim == 64 || c.head_dim == 128) && forced != '2') {

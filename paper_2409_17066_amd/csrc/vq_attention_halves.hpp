@@ -1,7 +1,8 @@
 // Both halves of attention behind shared prefixes in one launch: what the matrix cores bound (many rows over a prefix) and what memory bounds (few rows over each sequence's own keys) share
 // the compute units.  Workgroups of four waves, two to a compute unit, as the prompt kernel's are.
-// Measured (64 query and 8 key heads of 128 elements, 8 bits): 16 sequences behind 2048 tokens 10.6 us (with a launch for each half 18), 64 behind 8192 41.5 (a chunk of 64 keys in 2.5 us for the
-// two workgroups of a compute unit, as in long prompts; 56), 128 behind 32768 168 (209).  (Internal; instantiated for each type of cache by a file of its own.)
+// Measured (64 query and 8 key heads of 128 elements, 8 bits): 16 sequences behind 2048 tokens 10.6 us (with a launch for each half 18), 64 behind 8192 41.5 (56): one workgroup of the prefix on each
+// compute unit, 16 chunks of 64 keys one behind the other at about 1.8 us by itself and 2.5 beside a workgroup of the own keys, so that a chunk's latency bounds it (matrix cores busy 17 % of the
+// clocks); 128 behind 32768 168 (209): two workgroups of the prefix on each, a chunk of both in 2.5 us, as in long prompts.  (Internal; instantiated for each type of cache by a file of its own.)
 #pragma once
 #include "vq_attention.hpp"
 

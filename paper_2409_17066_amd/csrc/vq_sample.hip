@@ -11,8 +11,10 @@
 //
 // Latency bounds it: few rows, each the work of one compute unit, in phases behind one another (clocks of a row of 32000: counts 9400, sums of the runs 6500, over the runs 2000, borders and the number's
 // place 3000 to 6400, its occurrence 3000); of many long rows the counts, 12 to 19 clocks for 64 additions to LDS.  Measured: one row of 32000 with all settings 14 us, 20 rows of 50261
-// with 40 % masked 18, 64 rows of 128000 with top_p 23, 256 of 131072 30 (2.2 TB/s).  Rows on odd addresses are read from the first multiple of sixteen bytes on: 20 rows of 50261 16 us, of which
-// such reads without took 21.
+// with 40 % masked 18, 64 rows of 128000 with top_p 24, 256 of 131072 30 (2.2 TB/s), which keep a row in registers; 256 of 151936, read twice, 39, of 256000 54.  Rows on odd addresses are read from
+// the first multiple of sixteen bytes on: 20 rows of 50261 16 us, of which such reads without took 21.
+// That is with masks of minus infinity, which are counted aside.  A mask of a finite number (-65504, say) is counted like others, 64 lanes in turn at the same word, and beyond 65535 of them the row is
+// counted again in 32 bits: 64 rows of 128000 60 us with 40 % masked so, 233 with 70 %, in place of 26.
 #include "vq_kv.hpp"
 
 namespace vq {
