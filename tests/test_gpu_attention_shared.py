@@ -273,3 +273,26 @@ def test_prefixes_are_computed_once_without_bounds(gpu_lib, monkeypatch, prefixe
     shared = gpu_lib.attention_shared(q, *cache, **scales, **prefix, max_length=length, max_prefix=of_prefix, max_members=prefixes * members, max_own=length - of_prefix)
     torch.cuda.synchronize()
     assert torch.equal(got, shared) and not torch.equal(got, plain)
+
+
+@pytest.mark.parametrize("q_heads,heads,dim,bits", [(4, 2, 16, 16), (6, 2, 80, 8), (8, 2, 64, 16), (14, 2, 128, 8), (4, 2, 192, 8), (2, 1, 256, 16)])
+@pytest.mark.parametrize("switches", ["shared=1", "shared=2", "shared=1,prefix=p,prefix_parts=1", "shared=2,attention=d,parts=2", "shared=2,attention=p,parts=1"])
+def test_several_prefixes_without_bounds(gpu_lib, monkeypatch, q_heads, heads, dim, bits, switches):
+    """Prefixes of which each may have all of the sequences, whose partial results lie by the call's new tokens: of one sequence, of none, of most, with sequences in front of, between and behind them."""
+    import torch
+    monkeypatch.setenv("VQ_SWITCHES", switches)
+    p = Problem(31, [(128, 128, [(9, 2)]), (64, 64, []), (320, 317, [(20, 3)] * 11 + [("330", 1), ("0", 2)]), (96, 96, [(70, 5), (4, 4)])], [(33, 2), (1, 1)], q_heads, heads, dim, 16, bits)
+    dev, prefix = p.up()
+    args = dict(k_scales=dev.k_scales, v_scales=dev.v_scales, starts=dev.starts, max_new=max(p.news), return_lse=True)
+    want = p.want(dim ** -0.5)
+
+    def check(**kw):
+        out, lse = gpu_lib.attention_shared(torch.from_numpy(p.q).cuda(), dev.k, dev.v, dev.table, dev.lengths, **args, **prefix, **kw)
+        torch.cuda.synchronize()
+        _check(out.cpu().numpy(), lse.cpu().numpy(), *want, dim)
+    check()
+    check(max_members=12)
+    # the first sequence as one without a prefix, the third prefix's last ones too
+    prefix["members"] = torch.tensor([1, 1, 1, 9, 14], dtype=torch.int32, device="cuda")
+    prefix["prefix_lengths"] = torch.tensor([128, 64, 317, 0], dtype=torch.int32, device="cuda")
+    check()
